@@ -400,7 +400,7 @@ def _plain_scan(case: dict, s: dict):
     before = torch.cat((torch.zeros_like(h[:1]), h[:-1]))
     before[first] = h0[which]
     del h, drive
-    dh = s["dh"].float()
+    dh = s["dh"].float().clone()                                      # a pass leaves its inputs as they are
     d_last = s["dh_last"] if s["dh_last"] is not None else torch.zeros_like(h0)
     dh[last] += d_last[which]
     # the gradient runs the other way: g_t = dh_t + a_{t+1} g_{t+1}
