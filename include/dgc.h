@@ -430,6 +430,130 @@ dgc_status dgc_decode_accumulate(dgc_handle* h, float* dense, int64_t n, int32_t
                                  void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * ---- A distilled recurrent language model: what makes the gradients -------------------------
+ *
+ * The operators below need no handle: everything they have to know stands in their arguments.  They follow the
+ * conventions above (status codes, the caller's stream and buffers, nothing allocated, nothing waited for, fit for
+ * capture into a HIP graph).  Their workspaces hold nothing from one call to the next and need no preparation;
+ * calls that share one must be ordered.  Elements are of one of the types below; sums, softmax statistics and states
+ * are kept in binary32, and what is written in 16 bits is rounded once, to the nearest (ties to even).
+ */
+enum {
+  DGC_F32 = 0,
+  DGC_F16 = 1,  /* IEEE binary16                    */
+  DGC_BF16 = 2  /* binary32 without its low 16 bits */
+};
+
+#define DGC_TOP_MAX 256 /* pairs of a row at most */
+
+/* rows x vocab logits, element (r, j) at r * row_stride + j */
+typedef struct dgc_logits {
+  int32_t dtype;      /* DGC_F32, DGC_F16, DGC_BF16       */
+  int32_t reserved;   /* zero                             */
+  int64_t rows;       /* >= 0, < 2^31                     */
+  int64_t vocab;      /* >= 1, < 2^31                     */
+  int64_t row_stride; /* >= vocab, in elements            */
+} dgc_logits;
+
+/* Bytes of device workspace dgc_top_logits and dgc_distill_loss need for logits of this shape (any k). */
+dgc_status dgc_logits_workspace_bytes(const dgc_logits* shape, size_t* bytes);
+
+/*
+ * A teacher's payload: the k largest logits of every row as pairs, largest first, equal ones by ascending index.
+ *   logits   device, as `shape` says
+ *   k        1 .. DGC_TOP_MAX
+ *   out_idx  device, int32[rows * k], out_val device, float[rows * k]: pair p of row r at r * k + p.  NaN and -inf are
+ *            never chosen; where fewer than k others are left, the pairs behind them are (-1, -inf)
+ *   out_lse  device, float[rows], or NULL: log sum_j exp(logits[r][j] / temperature) over the whole row (-inf
+ *            where the row is nothing but -inf, NaN where it holds a NaN or +inf)
+ *   temperature  > 0, finite; changes out_lse only
+ *   workspace    device, >= dgc_logits_workspace_bytes, 256-byte aligned
+ * Errors: INVALID_ARG, ALIGNMENT (an element straddles its own size; workspace), CAPACITY (workspace, rows), HIP.
+ */
+dgc_status dgc_top_logits(const dgc_logits* shape, const void* logits, float temperature, int32_t k, int32_t* out_idx,
+                          float* out_val, float* out_lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Loss and gradient of a student's logits z against a teacher's pairs (i_p, t_p), temperature T, hard weight a:
+ *   q   = softmax(z / T) over the row,     P_p = exp(t_p / T - c),
+ *         c = top_lse[r] (the teacher's whole row, as dgc_top_logits leaves it for the same temperature), or, with
+ *         top_lse = NULL, the log-sum-exp of the t_p / T themselves, so that the P_p add up to one
+ *   KL  = sum_p P_p (log P_p - log q[i_p]),     CE = log sum_j exp(z_j) - z_y
+ *   loss[r]    = w_r ((1 - a) T^2 KL + a CE)
+ *   grad[r][j] = w_r ((1 - a) T (q_j sum_p P_p - [j = i_p] P_p) + a (softmax(z)_j - [j = y]))
+ *   top_idx, top_val  device, int32 / float[rows * k], k from 0 to DGC_TOP_MAX; the indices of a row are distinct; a
+ *               negative one stands for no pair.  A row without pairs has no KL term
+ *   labels      device, int32[rows], or NULL when hard_weight = 0; a negative one stands for no label (no CE term)
+ *   row_weight  device, float[rows], or NULL for ones: a mask, a mean's 1 / rows, an incoming gradient.  A row of
+ *               weight zero, and one whose logits are all -inf, has loss and gradient zero, whatever else it holds
+ *   loss        device, float[rows], or NULL; grad device, of the logits' type, rows grad_stride elements apart, or
+ *               NULL.  grad may be the logits themselves (the same address and stride): a training step needs them no more
+ *   diag_flags_dev    device uint32 or NULL: DGC_DIAG_BAD_INDEX is ORed in for an index or a label >= vocab, which
+ *               counts as none
+ * The gradient is the whole backward pass: it is formed from the logits alone, in the call that gives the loss or in
+ * one of its own (loss = NULL), and no statistics have to be kept for it.
+ * Errors: as dgc_top_logits; INVALID_ARG also for hard_weight outside [0, 1].
+ */
+dgc_status dgc_distill_loss(const dgc_logits* shape, const void* logits, int32_t k, const int32_t* top_idx,
+                            const float* top_val, const float* top_lse, const int32_t* labels,
+                            const float* row_weight, float temperature, float hard_weight, float* loss, void* grad,
+                            int64_t grad_stride, uint32_t* diag_flags_dev, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
+/* dgc_scan.flags */
+enum { DGC_SCAN_FREE_INPUT = 1u << 0 /* b = 1 instead of 1 - a */ };
+#define DGC_SCAN_STATE_ROWS 64 /* steps between two states that are kept for the backward pass */
+
+/*
+ * Sequences of a gated linear recurrence.  Row t of sequence s is row s * max_length + t of the arrays, or, with
+ * row_offsets, row row_offsets[s] + t: sequences of different lengths, none among them, lie behind each other.
+ */
+typedef struct dgc_scan {
+  int32_t dtype;      /* of gate, x, h and their gradients                                     */
+  uint32_t flags;     /* DGC_SCAN_*                                                            */
+  int64_t rows;       /* rows of the arrays, >= 0                                              */
+  int64_t sequences;  /* >= 0                                                                  */
+  int64_t max_length; /* >= 0; without row_offsets, sequences * max_length = rows              */
+  int64_t channels;   /* >= 1                                                                  */
+  const int64_t* row_offsets; /* device, sequences + 1 ascending rows, no two further apart than max_length, or NULL.
+                         Read on the device: rows outside [0, rows) or beyond max_length of a sequence are left out,
+                         never touched                                                         */
+} dgc_scan;
+
+/* Bytes of device workspace the two calls below need, and rows (of `channels` floats) of the states between them. */
+dgc_status dgc_gated_scan_workspace_bytes(const dgc_scan* shape, size_t* bytes);
+dgc_status dgc_gated_scan_state_rows(const dgc_scan* shape, int64_t* state_rows);
+
+/*
+ *   a = sigmoid(gate),  b = 1 - a (or 1),  h_t = a_t h_{t-1} + b_t x_t    for every channel of every sequence
+ * A gate of -inf starts the state again, one of +inf keeps it.
+ *   gate, x, h  device, rows gate_stride, x_stride, h_stride elements apart (each >= channels)
+ *   h0          device, float[sequences * channels], or NULL for zeros
+ *   h_last      device, float[same], or NULL: the state behind the last step (h0 where a sequence has no step); may
+ *               be h0 itself: a serving loop calls this with max_length = 1 and one state array
+ *   states      device, float[state_rows * channels], or NULL: what dgc_gated_scan_backward needs
+ * h must not overlap gate or x unless it is one of them, address and stride.
+ * Errors: INVALID_ARG, ALIGNMENT, CAPACITY (workspace; more than 2^31 - 1 workgroups), HIP.
+ */
+dgc_status dgc_gated_scan_forward(const dgc_scan* shape, const void* gate, int64_t gate_stride, const void* x,
+                                  int64_t x_stride, const float* h0, void* h, int64_t h_stride, float* h_last,
+                                  float* states, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradients.  With g_t = dh_t + a_{t+1} g_{t+1} (behind the last step dh_last):
+ *   dx_t = b_t g_t,   dgate_t = g_t (h_{t-1} - x_t) a_t (1 - a_t)   (free input: g_t h_{t-1} a_t (1 - a_t)),
+ *   dh0 = a_0 g_0
+ * The states in between are formed again from the kept ones, in binary32; h is not read.
+ *   dh_last  device, float[sequences * channels], or NULL for zeros;  dh0 device, float[same], or NULL; may be dh_last
+ *   dgate, dx   must not overlap an input unless it is that input, address and stride
+ */
+dgc_status dgc_gated_scan_backward(const dgc_scan* shape, const void* gate, int64_t gate_stride, const void* x,
+                                   int64_t x_stride, const float* states, const void* dh, int64_t dh_stride,
+                                   const float* dh_last, void* dgate, int64_t dgate_stride, void* dx,
+                                   int64_t dx_stride, float* dh0, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+
+/*
  * Kernel timing for measurement harnesses.  After dgc_profile_enable the next
  * `max_calls` dgc_compress calls record HIP events on the caller's stream before
  * the norm kernel, after it, after the select kernel, after the streaming kernel

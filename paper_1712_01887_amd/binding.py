@@ -34,6 +34,13 @@ DGC_DIAG_NONFINITE = 1 << 1
 DGC_DIAG_BAD_INDEX = 1 << 2
 DGC_DIAG_UNSORTED = 1 << 3
 
+DGC_F32 = 0
+DGC_F16 = 1
+DGC_BF16 = 2
+DGC_TOP_MAX = 256
+DGC_SCAN_FREE_INPUT = 1 << 0
+DGC_SCAN_STATE_ROWS = 64
+
 EXPORTS = [
     "dgc_config_default", "dgc_status_string", "dgc_create", "dgc_destroy", "dgc_invalidate_workspace",
     "dgc_set_scale_override", "dgc_set_density",
@@ -44,6 +51,8 @@ EXPORTS = [
     "dgc_version", "dgc_last_error_string", "dgc_profile_enable", "dgc_profile_collect",
     "dgc_profile_disable", "dgc_sparse_sgd_apply", "dgc_sparse_sgd_apply_regions",
     "dgc_encode_max_entries", "dgc_encode", "dgc_decode_accumulate", "dgc_profile_stream_ceiling",
+    "dgc_logits_workspace_bytes", "dgc_top_logits", "dgc_distill_loss", "dgc_gated_scan_workspace_bytes",
+    "dgc_gated_scan_state_rows", "dgc_gated_scan_forward", "dgc_gated_scan_backward",
 ]
 
 
@@ -67,6 +76,16 @@ class DgcConfig(C.Structure):
 
 class DgcDiagnostics(C.Structure):
     _fields_ = [("norm", C.c_double), ("scale", C.c_float), ("flags", C.c_uint32)]
+
+
+class DgcLogits(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_int64), ("vocab", C.c_int64),
+                ("row_stride", C.c_int64)]
+
+
+class DgcScan(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("flags", C.c_uint32), ("rows", C.c_int64), ("sequences", C.c_int64),
+                ("max_length", C.c_int64), ("channels", C.c_int64), ("row_offsets", C.c_void_p)]
 
 
 class DgcError(RuntimeError):
@@ -158,6 +177,23 @@ def load() -> C.CDLL:
     lib.dgc_profile_collect.argtypes = [vp, P(i32), P(dbl), P(dbl), P(dbl), P(dbl)]
     lib.dgc_profile_disable.restype = i32
     lib.dgc_profile_disable.argtypes = [vp]
+    f32 = C.c_float
+    lib.dgc_logits_workspace_bytes.restype = i32
+    lib.dgc_logits_workspace_bytes.argtypes = [P(DgcLogits), P(C.c_size_t)]
+    lib.dgc_top_logits.restype = i32
+    lib.dgc_top_logits.argtypes = [P(DgcLogits), vp, f32, i32, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.dgc_distill_loss.restype = i32
+    lib.dgc_distill_loss.argtypes = [P(DgcLogits), vp, i32, vp, vp, vp, vp, vp, f32, f32, vp, vp, i64, vp, vp,
+                                     C.c_size_t, vp]
+    lib.dgc_gated_scan_workspace_bytes.restype = i32
+    lib.dgc_gated_scan_workspace_bytes.argtypes = [P(DgcScan), P(C.c_size_t)]
+    lib.dgc_gated_scan_state_rows.restype = i32
+    lib.dgc_gated_scan_state_rows.argtypes = [P(DgcScan), P(i64)]
+    lib.dgc_gated_scan_forward.restype = i32
+    lib.dgc_gated_scan_forward.argtypes = [P(DgcScan), vp, i64, vp, i64, vp, vp, i64, vp, vp, vp, C.c_size_t, vp]
+    lib.dgc_gated_scan_backward.restype = i32
+    lib.dgc_gated_scan_backward.argtypes = [P(DgcScan), vp, i64, vp, i64, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp,
+                                            C.c_size_t, vp]
     _lib = lib
     return lib
 
@@ -405,3 +441,181 @@ class Dgc:
         _check(self.lib.dgc_dense_clear_regions(
             self._h, _ptr(dense), len(idx_list), _ptr_array(idx_list), _ptr_array(count_list),
             self._layout_c, self._ws_ptr, self._ws_bytes, _stream()), "dgc_dense_clear_regions")
+
+
+# ---------------------------------------------------------------------------
+# Operators on logits and sequences
+# ---------------------------------------------------------------------------
+def _dtype_code(dtype) -> int:
+    import torch
+    codes = {torch.float32: DGC_F32, torch.float16: DGC_F16, torch.bfloat16: DGC_BF16}
+    if dtype not in codes:
+        raise DgcError(DGC_ERR_INVALID_ARG, f"element type {dtype} (float32, float16 and bfloat16 are known)")
+    return codes[dtype]
+
+
+def _rows_of(t, name: str, dtype, rows: int, columns: int, device) -> int:
+    """The row stride of a rows x columns tensor whose rows are contiguous."""
+    if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != columns or t.device != device:
+        raise DgcError(DGC_ERR_INVALID_ARG, f"{name}: {tuple(t.shape)} of {t.dtype} on {t.device} where "
+                                            f"({rows}, {columns}) of {dtype} on {device} is needed")
+    if columns > 1 and t.stride(1) != 1:
+        raise DgcError(DGC_ERR_INVALID_ARG, f"{name}: the elements of a row must be contiguous")
+    stride = t.stride(0) if rows > 1 else columns
+    if stride < columns:
+        raise DgcError(DGC_ERR_INVALID_ARG, f"{name}: rows overlap")
+    return stride
+
+
+def _dense(t, name: str, dtype, shape, device) -> int:
+    """The address of a contiguous tensor of this type and shape; 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
+        raise DgcError(DGC_ERR_INVALID_ARG, f"{name}: {tuple(t.shape)} of {t.dtype} on {t.device} where a contiguous "
+                                            f"{shape} of {dtype} on {device} is needed")
+    return t.data_ptr()
+
+
+class _Workspace:
+    """A device workspace of the caller's size, aligned as the library wants it, for one device's current stream."""
+
+    def __init__(self, nbytes: int, device):
+        import torch
+        self.tensor = torch.empty(nbytes + 256, dtype=torch.uint8, device=device) if nbytes else None
+        self.ptr = (self.tensor.data_ptr() + 255) // 256 * 256 if nbytes else 0
+        self.nbytes = nbytes
+
+
+def _device(device):
+    import torch
+    device = torch.device(device)
+    if device.type != "cuda":
+        raise DgcError(DGC_ERR_INVALID_ARG, f"device {device}: the kernels run on a GPU")
+    return torch.device("cuda", torch.cuda.current_device() if device.index is None else device.index)
+
+
+class Distillation:
+    """Rows of logits over one vocabulary: a teacher's pairs, and a student's loss and gradient against such pairs.
+
+    `rows`: of a call at most.  The plan owns a workspace: its calls belong on one stream (or are ordered by events)."""
+
+    def __init__(self, rows: int, vocab: int, dtype, device="cuda"):
+        self.lib = load()
+        self.rows, self.vocab, self.dtype = int(rows), int(vocab), dtype
+        self._shape = DgcLogits(_dtype_code(dtype), 0, self.rows, self.vocab, self.vocab)
+        b = C.c_size_t()
+        _check(self.lib.dgc_logits_workspace_bytes(C.byref(self._shape), C.byref(b)), "dgc_logits_workspace_bytes")
+        self.device = _device(device)
+        self.workspace = _Workspace(int(b.value), self.device)
+
+    def alloc_top_logits(self, k: int):
+        """(out_idx, out_val, out_lse) for `rows` rows of k pairs."""
+        import torch
+        return (torch.empty(self.rows, k, dtype=torch.int32, device=self.device),
+                torch.empty(self.rows, k, dtype=torch.float32, device=self.device),
+                torch.empty(self.rows, dtype=torch.float32, device=self.device))
+
+    def _set_shape(self, logits) -> int:
+        rows = logits.shape[0]
+        if rows > self.rows:
+            raise DgcError(DGC_ERR_CAPACITY, f"{rows} rows in a plan for {self.rows}")
+        self._shape.rows = rows
+        self._shape.row_stride = _rows_of(logits, "logits", self.dtype, rows, self.vocab, self.device)
+        return rows
+
+    def dgc_top_logits(self, logits, out_idx, out_val, out_lse=None, temperature: float = 1.0) -> None:
+        """The k largest logits of every row (k = out_idx.shape[1]) and, if wanted, the rows' log-sum-exp."""
+        import torch
+        rows, k, dev = self._set_shape(logits), out_idx.shape[-1], self.device
+        _check(self.lib.dgc_top_logits(
+            C.byref(self._shape), logits.data_ptr(), temperature, k,
+            _dense(out_idx, "out_idx", torch.int32, (rows, k), dev),
+            _dense(out_val, "out_val", torch.float32, (rows, k), dev),
+            _dense(out_lse, "out_lse", torch.float32, (rows,), dev),
+            self.workspace.ptr, self.workspace.nbytes, _stream()), "dgc_top_logits")
+
+    def dgc_distill_loss(self, logits, top_idx, top_val, loss, grad=None, top_lse=None, labels=None, row_weight=None,
+                         temperature: float = 1.0, hard_weight: float = 0.0, diag_flags=None) -> None:
+        """loss (or None) and grad (or None; may be `logits`) of every row; see the header for the formulas.
+        top_idx and top_val may both be None: no teacher, hard labels alone."""
+        import torch
+        rows, dev = self._set_shape(logits), self.device
+        k = 0 if top_idx is None else top_idx.shape[-1]
+        if (top_idx is None) != (top_val is None):
+            raise DgcError(DGC_ERR_INVALID_ARG, "top_idx and top_val: one without the other")
+        stride = self.vocab if grad is None else _rows_of(grad, "grad", self.dtype, rows, self.vocab, dev)
+        _check(self.lib.dgc_distill_loss(
+            C.byref(self._shape), logits.data_ptr(), k,
+            _dense(top_idx, "top_idx", torch.int32, (rows, k), dev),
+            _dense(top_val, "top_val", torch.float32, (rows, k), dev),
+            _dense(top_lse, "top_lse", torch.float32, (rows,), dev),
+            _dense(labels, "labels", torch.int32, (rows,), dev),
+            _dense(row_weight, "row_weight", torch.float32, (rows,), dev), temperature, hard_weight,
+            _dense(loss, "loss", torch.float32, (rows,), dev), _ptr(grad), stride,
+            _dense(diag_flags, "diag_flags", torch.int32, (1,), dev),
+            self.workspace.ptr, self.workspace.nbytes, _stream()), "dgc_distill_loss")
+
+
+class GatedScan:
+    """Sequences of one shape (or, with `row_offsets`, of different lengths behind each other in `rows` rows) under the
+    gated linear recurrence.  row_offsets: int64 on the device, sequences + 1 ascending row numbers.  The plan owns a
+    workspace: its calls belong on one stream (or are ordered by events)."""
+
+    def __init__(self, sequences: int, max_length: int, channels: int, dtype, free_input: bool = False,
+                 row_offsets=None, rows: int = None, device="cuda"):
+        import torch
+        self.lib = load()
+        self.device = _device(device)
+        self.sequences, self.channels, self.dtype = int(sequences), int(channels), dtype
+        if row_offsets is None:
+            if rows is not None and rows != sequences * max_length:
+                raise DgcError(DGC_ERR_INVALID_ARG, f"{rows} rows are not {sequences} sequences of {max_length}")
+            self.rows = int(sequences) * int(max_length)
+        else:
+            if rows is None:
+                raise DgcError(DGC_ERR_INVALID_ARG, "row_offsets without rows")
+            self.rows = int(rows)
+        self.row_offsets = row_offsets                                # kept alive: its address is in the shape
+        self._shape = DgcScan(_dtype_code(dtype), DGC_SCAN_FREE_INPUT if free_input else 0, self.rows, self.sequences,
+                              int(max_length), self.channels,
+                              _dense(row_offsets, "row_offsets", torch.int64, (self.sequences + 1,), self.device))
+        b, n = C.c_size_t(), C.c_int64()
+        _check(self.lib.dgc_gated_scan_workspace_bytes(C.byref(self._shape), C.byref(b)),
+               "dgc_gated_scan_workspace_bytes")
+        _check(self.lib.dgc_gated_scan_state_rows(C.byref(self._shape), C.byref(n)), "dgc_gated_scan_state_rows")
+        self.state_rows = int(n.value)
+        self.workspace = _Workspace(int(b.value), self.device)
+
+    def alloc_states(self):
+        """What a forward call leaves for the backward call of the same inputs."""
+        import torch
+        return torch.empty(self.state_rows, self.channels, dtype=torch.float32, device=self.device)
+
+    def _rows(self, t, name: str) -> int:
+        return _rows_of(t, name, self.dtype, self.rows, self.channels, self.device)
+
+    def _carried(self, t, name: str) -> int:
+        import torch
+        return _dense(t, name, torch.float32, (self.sequences, self.channels), self.device)
+
+    def _kept(self, t) -> int:
+        import torch
+        return _dense(t, "states", torch.float32, (self.state_rows, self.channels), self.device)
+
+    def dgc_gated_scan_forward(self, gate, x, h0, h, h_last=None, states=None) -> None:
+        """h, and h_last (may be h0 itself) and states where given; h0 = None: zeros."""
+        _check(self.lib.dgc_gated_scan_forward(
+            C.byref(self._shape), gate.data_ptr(), self._rows(gate, "gate"), x.data_ptr(), self._rows(x, "x"),
+            self._carried(h0, "h0"), h.data_ptr(), self._rows(h, "h"), self._carried(h_last, "h_last"),
+            self._kept(states), self.workspace.ptr, self.workspace.nbytes, _stream()), "dgc_gated_scan_forward")
+
+    def dgc_gated_scan_backward(self, gate, x, states, dh, dh_last, dgate, dx, dh0=None) -> None:
+        """dgate, dx, and dh0 (may be dh_last itself) where given, from the states of the forward call; dh_last = None:
+        zeros."""
+        _check(self.lib.dgc_gated_scan_backward(
+            C.byref(self._shape), gate.data_ptr(), self._rows(gate, "gate"), x.data_ptr(), self._rows(x, "x"),
+            self._kept(states), dh.data_ptr(), self._rows(dh, "dh"), self._carried(dh_last, "dh_last"),
+            dgate.data_ptr(), self._rows(dgate, "dgate"), dx.data_ptr(), self._rows(dx, "dx"),
+            self._carried(dh0, "dh0"), self.workspace.ptr, self.workspace.nbytes, _stream()),
+            "dgc_gated_scan_backward")

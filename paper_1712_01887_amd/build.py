@@ -18,9 +18,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB_PATH = os.path.join(HERE, "libdgc.so")
 SOURCES = [os.path.join(HERE, "csrc", name) for name in
-           ("dgc_api.hip", "dgc_compress.hip", "dgc_receive.hip", "dgc_wire.hip")]
+           ("dgc_api.hip", "dgc_compress.hip", "dgc_receive.hip", "dgc_wire.hip",
+            "dgc_operators_api.hip", "dgc_logits.hip", "dgc_scan.hip")]
 HEADERS = [os.path.join(HERE, "csrc", "dgc_internal.h"), os.path.join(HERE, "csrc", "dgc_device.h"),
-           os.path.join(HERE, "csrc", "dgc_probe.h"),
+           os.path.join(HERE, "csrc", "dgc_probe.h"), os.path.join(HERE, "csrc", "dgc_operators.h"),
            os.path.join(HERE, "csrc", "dgc_band.h"), os.path.join(ROOT, "include", "dgc.h")]
 
 

@@ -66,12 +66,16 @@ namespace {
 // Text of the most recent failed HIP call on this thread (for dgc_last_error_string).
 thread_local char g_last_error[256] = "";
 
-bool hip_ok(hipError_t e, const char* what) {
+}  // namespace
+
+bool dgc::hip_ok(hipError_t e, const char* what) {
   if (e == hipSuccess) return true;
   std::snprintf(g_last_error, sizeof(g_last_error), "%s: %s (%d)", what, hipGetErrorString(e), (int)e);
   (void)hipGetLastError();  // clear the sticky launch error so later calls start clean
   return false;
 }
+
+namespace {
 
 // Which handle's tables a workspace holds.  A handle keeps host-side flags for what it has
 // uploaded into the workspace it used last; they mean something only while no other handle has

@@ -15,6 +15,9 @@ namespace dgc {
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Whether a HIP call succeeded; if not, its text is kept for dgc_last_error_string (dgc_api.hip).
+bool hip_ok(hipError_t e, const char* what);
+
 // ---- launch geometry -------------------------------------------------------
 // Streaming pass: one wavefront owns a contiguous run of kWaveTile elements and
 // reads it as kStreamUnroll rounds of one float4 per lane (64 lanes x 16 B =

@@ -1,0 +1,284 @@
+"""The gated linear recurrence, forward and backward, against its definition in 64 bits (tests/operators_reference.py),
+element by element.  Run with `-m gpu` on an MI355X."""
+
+import numpy as np
+import pytest
+
+from paper_1712_01887_amd import binding as B
+from tests import operators_reference as R
+from tests.parity import capture, say
+
+pytestmark = pytest.mark.gpu
+SENTINEL = 12345.0
+
+
+def dtype_of(name):
+    import torch
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[name]
+
+
+def array(rows, channels, dtype, stride, shift, values=None):
+    """A rows x channels tensor inside a buffer of sentinels: rows `stride` apart, the first one `shift` elements in."""
+    import torch
+    buffer = torch.full((rows * stride + shift + 64,), SENTINEL, dtype=dtype_of(dtype), device="cuda")
+    view = buffer[shift:shift + rows * stride].view(rows, stride)[:, :channels]
+    if values is not None:
+        view.copy_(torch.from_numpy(values))
+    return buffer, view
+
+
+def untouched(buffer, view, rows, channels, stride, shift):
+    """Whether every element outside the rows still is what it was."""
+    import torch
+    mask = torch.ones_like(buffer, dtype=torch.bool)
+    mask[shift:shift + rows * stride].view(rows, stride)[:, :channels] = False
+    return bool((buffer[mask] == SENTINEL).all())
+
+
+def close(got, value, bound, dtype, what):
+    got = got.detach().cpu().double().numpy()
+    allowed = R.rounded(bound, value, dtype)
+    same = np.isfinite(value)
+    assert np.array_equal(np.isfinite(got), same), what
+    worst = np.max(np.where(same, np.abs(got - value) - allowed, -1.0), initial=-1.0)
+    assert worst <= 0.0, (what, worst, np.unravel_index(np.argmax(np.abs(got - value) - allowed), value.shape))
+
+
+def inputs(rows, sequences, channels, dtype, seed, extremes=False):
+    rng = np.random.default_rng(seed)
+    import torch
+    def cast(v):
+        return torch.from_numpy(v).to(dtype_of(dtype)).double().numpy()
+    gate = rng.normal(2.0, 1.5, (rows, channels))
+    if extremes and rows:
+        pick = rng.random((rows, channels))
+        gate[pick < 0.05] = -np.inf
+        gate[(pick > 0.05) & (pick < 0.1)] = np.inf
+        gate[(pick > 0.1) & (pick < 0.13)] = 30.0
+        gate[(pick > 0.13) & (pick < 0.16)] = -30.0
+    return dict(gate=cast(gate), x=cast(rng.normal(size=(rows, channels))), dh=cast(rng.normal(size=(rows, channels)) * 0.1),
+                h0=rng.normal(size=(sequences, channels)).astype(np.float32),
+                dh_last=rng.normal(size=(sequences, channels)).astype(np.float32))
+
+
+def check(lengths, channels, dtype, free=False, packed=True, max_length=None, stride=None, shift=0, carried=True, seed=0,
+          extremes=False, gap=0):
+    import torch
+    rows, n = sum(lengths), len(lengths)
+    total = rows + gap
+    stride = stride or channels
+    say(f"[scan] lengths {lengths[:6]}{'...' if n > 6 else ''} x {channels} {dtype} free={free} packed={packed} "
+        f"stride={stride} shift={shift} carried={carried}")
+    v = inputs(rows, n, channels, dtype, seed, extremes)
+    pad = lambda w: np.concatenate([w, np.full((gap, channels), 1.0)]) if gap else w
+    offsets = np.concatenate([[0], np.cumsum(lengths)])
+    plan = B.GatedScan(n, max(lengths) if max_length is None else max_length, channels, dtype_of(dtype), free_input=free,
+                       row_offsets=torch.from_numpy(offsets).cuda() if packed else None, rows=total)
+    _, gate = array(total, channels, dtype, stride, shift, pad(v["gate"]))
+    _, x = array(total, channels, dtype, stride, shift, pad(v["x"]))
+    _, dh = array(total, channels, dtype, stride, shift, pad(v["dh"]))
+    out = {name: array(total, channels, dtype, stride, shift) for name in ("h", "dgate", "dx")}
+    h0 = torch.from_numpy(v["h0"]).cuda() if carried else None
+    dh_last = torch.from_numpy(v["dh_last"]).cuda() if carried else None
+    h_last, dh0 = (torch.full((n, channels), SENTINEL, device="cuda") for _ in range(2))
+    states = plan.alloc_states().fill_(float("nan"))
+    plan.dgc_gated_scan_forward(gate, x, h0, out["h"][1], h_last, states)
+    plan.dgc_gated_scan_backward(gate, x, states, dh, dh_last, out["dgate"][1], out["dx"][1], dh0)
+    torch.cuda.synchronize()
+    f = R.scan_forward(v["gate"], v["x"], lengths, v["h0"] if carried else None, free)
+    b = R.scan_backward(v["gate"], v["x"], lengths, v["h0"] if carried else None, v["dh"],
+                        v["dh_last"] if carried else None, free)
+    close(out["h"][1][:rows], f["h"], f["h_bound"], dtype, "h")
+    close(h_last, f["last"], f["last_bound"], "f32", "h_last")
+    close(out["dx"][1][:rows], b["dx"], b["dx_bound"], dtype, "dx")
+    close(out["dgate"][1][:rows], b["dgate"], b["dgate_bound"], dtype, "dgate")
+    close(dh0, b["dh0"], b["dh0_bound"], "f32", "dh0")
+    for name, (buffer, view) in out.items():
+        assert untouched(buffer, view, rows, channels, stride, shift), name
+        assert bool((view[rows:] == SENTINEL).all()), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("free", [False, True])
+@pytest.mark.parametrize("length", [1, 2, 63, 64, 65, 130, 1025])
+def test_lengths(length, free, dtype):
+    check([length] * 3, 72, dtype, free=free, packed=False, seed=length)
+
+
+@pytest.mark.parametrize("channels", [1, 3, 29, 64, 65, 250, 256, 257, 1500])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_channels(channels, dtype):
+    check([77, 77], channels, dtype, packed=False, seed=channels)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("lengths", [[0], [0, 0, 5], [5, 0, 0], [1, 64, 0, 63, 65, 128, 129, 7], [300, 1, 1, 1, 299, 64]])
+def test_sequences_of_different_lengths(lengths, dtype):
+    check(lengths, 40, dtype, seed=len(lengths))
+    check(lengths, 40, dtype, seed=len(lengths), carried=False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("stride,shift", [(200, 0), (201, 0), (200, 1), (203, 3), (200, 2), (200, 4), (208, 8)])
+def test_strides_and_alignment(stride, shift, dtype):
+    check([70, 3, 64], 96, dtype, stride=stride, shift=shift, seed=stride + shift)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_gates_at_their_ends(dtype):
+    check([200, 65], 130, dtype, extremes=True, seed=5)
+    check([200, 65], 130, dtype, extremes=True, seed=6, free=True)
+
+
+@pytest.mark.parametrize("lengths,channels", [([9000], 64), ([5000, 3001], 72), ([4097] * 2, 520), ([20011], 32)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_sequences(lengths, channels, dtype):
+    check(lengths, channels, dtype, packed=len(set(lengths)) > 1, seed=7)
+
+
+def test_rows_behind_the_last_sequence_stay():
+    check([33, 70], 50, "f32", gap=9, seed=8)
+    check([33, 700], 50, "bf16", gap=130, seed=9)
+
+
+def test_one_step_with_the_state_in_place():
+    import torch
+    for dtype in ("f32", "bf16"):
+        v = inputs(12 * 4, 12, 100, dtype, 3)
+        plan = B.GatedScan(12, 1, 100, dtype_of(dtype))
+        state = torch.from_numpy(v["h0"]).cuda()
+        gate, x = (torch.from_numpy(v[k]).cuda().to(dtype_of(dtype)).view(4, 12, 100) for k in ("gate", "x"))
+        h = torch.empty(4, 12, 100, dtype=dtype_of(dtype), device="cuda")
+        for t in range(4):
+            plan.dgc_gated_scan_forward(gate[t], x[t], state, h[t], state)
+        # the same as four steps of twelve sequences, one behind the other
+        order = np.arange(48).reshape(4, 12).T.reshape(-1)
+        f = R.scan_forward(v["gate"][order], v["x"][order], [4] * 12, v["h0"], False)
+        close(h.view(48, 100)[torch.from_numpy(order).cuda()], f["h"], f["h_bound"], dtype, "h")
+        close(state, f["last"], f["last_bound"], "f32", "state")
+
+
+def test_outputs_in_the_place_of_inputs():
+    import torch
+    v = inputs(500, 2, 64, "f32", 4)
+    t = {k: torch.from_numpy(v[k]).float().cuda() for k in ("gate", "x", "dh")}
+    flow = torch.from_numpy(v["dh_last"]).cuda()
+    plan = B.GatedScan(2, 250, 64, torch.float32)
+    states = plan.alloc_states()
+    h = t["x"].clone()
+    plan.dgc_gated_scan_forward(t["gate"], h, None, h, None, states)
+    plan.dgc_gated_scan_backward(t["gate"], t["x"], states, t["dh"], flow, t["gate"], t["dh"], flow)
+    f = R.scan_forward(v["gate"], v["x"], [250] * 2, None, False)
+    b = R.scan_backward(v["gate"], v["x"], [250] * 2, None, v["dh"], v["dh_last"], False)
+    close(h, f["h"], f["h_bound"], "f32", "h")
+    close(t["gate"], b["dgate"], b["dgate_bound"], "f32", "dgate")
+    close(t["dh"], b["dx"], b["dx_bound"], "f32", "dx")
+    close(flow, b["dh0"], b["dh0_bound"], "f32", "dh0")
+
+
+def test_nan_stays_in_its_channel():
+    import torch
+    for length in (100, 6000):
+        v = inputs(2 * length, 2, 70, "f32", 11)
+        gate, x = (torch.from_numpy(v[k]).float().cuda() for k in ("gate", "x"))
+        gate[20, 5] = float("nan")
+        x[length + 3, 64] = float("nan")
+        h = torch.empty_like(x)
+        B.GatedScan(2, length, 70, torch.float32).dgc_gated_scan_forward(gate, x, None, h)
+        bad = torch.isnan(h)
+        want = torch.zeros_like(bad)
+        want[20:length, 5] = True
+        want[length + 3:, 64] = True
+        assert torch.equal(bad, want)
+
+
+def test_offsets_outside_the_arrays_touch_nothing_else():
+    """Offsets that point behind the arrays, or further apart than max_length, are cut."""
+    import torch
+    rows, d = 100, 48
+    gate, x = torch.zeros(rows, d, device="cuda"), torch.ones(rows, d, device="cuda")
+    buffer, h = array(rows, d, "f32", d, 0)
+    offsets = torch.tensor([-5, 10, 60, 40, 1000], device="cuda")     # 15 rows, 50 of at most 20, none, 60 of at most 20
+    plan = B.GatedScan(4, 20, d, torch.float32, row_offsets=offsets, rows=rows)
+    plan.dgc_gated_scan_forward(gate, x, None, h, None, plan.alloc_states())
+    done = (h != SENTINEL).all(1).cpu().numpy()
+    want = np.zeros(rows, bool)
+    want[0:10] = True
+    want[10:30] = True
+    want[40:60] = True
+    assert np.array_equal(done, want)
+    assert untouched(buffer, h, rows, d, d, 0)
+
+
+def test_gradient_against_differences():
+    """Central differences of L = sum dh h + sum dh_last h_last with steps of e = 2^-5.  L is linear in x and h0 (only
+    rounding: two sums of `terms` values of h's bound, over 2 e); in a gate its third derivative is at most |g (h - x)| times
+    that of a sigmoid, 1/8, and the powers of it that later steps do not see: e^2 / 6 / 8 relative to |g| |h - x|."""
+    import torch
+    length, d, e = 40, 6, 2.0 ** -5
+    v = inputs(2 * length, 2, d, "f32", 12)
+    v = {k: w.astype(np.float32).astype(np.float64) for k, w in v.items()}
+    plan = B.GatedScan(2, length, d, torch.float32)
+
+    def loss(gate, x, h0):
+        t = [torch.from_numpy(w.astype(np.float32)).cuda() for w in (gate, x, h0)]
+        h, last = torch.empty_like(t[0]), torch.empty_like(t[2])
+        plan.dgc_gated_scan_forward(*t, h, last)
+        return (h.double().cpu().numpy() * v["dh"]).sum(0), (last.double().cpu().numpy() * v["dh_last"]).sum(0)
+
+    t = {k: torch.from_numpy(w.astype(np.float32)).cuda() for k, w in v.items()}
+    h, states = torch.empty_like(t["x"]), plan.alloc_states()
+    grads = {k: torch.empty_like(t[k]) for k in ("gate", "x", "h0")}
+    plan.dgc_gated_scan_forward(t["gate"], t["x"], t["h0"], h, None, states)
+    plan.dgc_gated_scan_backward(t["gate"], t["x"], states, t["dh"], t["dh_last"], grads["gate"], grads["x"], grads["h0"])
+    f = R.scan_forward(v["gate"], v["x"], [length] * 2, v["h0"], False)
+    rounding = (f["h_bound"] * np.abs(v["dh"])).sum(0) + (f["last_bound"] * np.abs(v["dh_last"])).sum(0)
+    for name in ("gate", "x", "h0"):
+        for r in ((0, 7, 39, 40, 66, 79) if name != "h0" else (0, 1)):
+            up, down = ({k: w.copy() for k, w in v.items()} for _ in range(2))
+            up[name][r] += e
+            down[name][r] -= e
+            step = up[name][r].astype(np.float32).astype(np.float64) - down[name][r].astype(np.float32)
+            a, b = (loss(w["gate"], w["x"], w["h0"]) for w in (up, down))
+            slope = ((a[0] - b[0]) + (a[1] - b[1])) / step
+            got = grads[name][r].double().cpu().numpy()
+            curve = 0.0
+            if name == "gate":
+                flow = R.scan_backward(v["gate"], v["x"], [length] * 2, v["h0"], v["dh"], v["dh_last"], True)["dx"]
+                # with a free input dx is g itself
+                curve = e * e / 6 / 8 * np.abs(flow[r]) * np.abs(f["before"][r] - v["x"][r])
+            assert np.all(np.abs(slope - got) <= curve + 4 * rounding / (2 * e) + 1e-7 * np.abs(got)), (name, r)
+
+
+def test_capture_and_another_stream():
+    import torch
+    v = inputs(3000, 1, 96, "bf16", 13)
+    t = {k: torch.from_numpy(v[k]).cuda().to(torch.bfloat16) for k in ("gate", "x", "dh")}
+    plan = B.GatedScan(1, 3000, 96, torch.bfloat16)
+    states = plan.alloc_states()
+    out = [torch.empty_like(t["x"]) for _ in range(3)]
+
+    def both():
+        plan.dgc_gated_scan_forward(t["gate"], t["x"], None, out[0], None, states)
+        plan.dgc_gated_scan_backward(t["gate"], t["x"], states, t["dh"], None, out[1], out[2])
+
+    both()
+    torch.cuda.synchronize()
+    want = [o.clone() for o in out]
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        for o in out:
+            o.zero_()
+        both()
+    stream.synchronize()
+    assert all(torch.equal(o, w) for o, w in zip(out, want))          # the same bits on every run
+    graph = torch.cuda.CUDAGraph()
+    with capture(graph):
+        both()
+    for _ in range(4):
+        for o in out:
+            o.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(out, want))
