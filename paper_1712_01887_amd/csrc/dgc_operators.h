@@ -57,7 +57,9 @@ struct ScanArgs {
 
 hipError_t launch_top_logits(const TopArgs& a, int32_t dtype, hipStream_t stream);
 hipError_t launch_distill(const DistillArgs& a, int32_t dtype, hipStream_t stream);
-hipError_t launch_scan(const ScanArgs& a, int32_t dtype, bool free_input, bool backward, hipStream_t stream);
+hipError_t launch_scan(const ScanArgs& a, void* workspace, int32_t dtype, bool free_input, bool backward, hipStream_t stream);
+size_t scan_workspace_bytes(const ScanArgs& a);  // of the shape alone
+int64_t scan_workgroups(const ScanArgs& a);      // tiles or workgroups, whichever a launch counts
 
 // ---- element types ---------------------------------------------------------------
 // An element as it lies in memory, and what it stands for.  To 16 bits: once, to the nearest, ties to even.

@@ -10,6 +10,7 @@ using namespace dgc;
 namespace {
 
 constexpr int64_t kIntLimit = (int64_t)1 << 31;
+constexpr int64_t kWidthLimit = (int64_t)1 << 26;  // channels and row strides of a scan: offsets inside a tile take 32 bits
 
 bool aligned_to(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
@@ -34,20 +35,29 @@ dgc_status check_workspace(const void* workspace, size_t have, size_t need) {
   return have < need ? DGC_ERR_CAPACITY : DGC_OK;
 }
 
+ScanArgs scan_args(const dgc_scan* s) {
+  ScanArgs a{};
+  a.row_offsets = s->row_offsets;
+  a.rows = s->rows;
+  a.max_length = s->max_length;
+  a.channels = s->channels;
+  a.sequences = s->sequences;
+  return a;
+}
+
 dgc_status check_scan(const dgc_scan* s) {
   if (!s || !type_known(s->dtype) || (s->flags & ~(uint32_t)DGC_SCAN_FREE_INPUT) != 0) return DGC_ERR_INVALID_ARG;
   if (s->rows < 0 || s->sequences < 0 || s->max_length < 0 || s->channels < 1) return DGC_ERR_INVALID_ARG;
-  if (s->rows >= (int64_t)1 << 40 || s->channels >= kIntLimit || s->sequences >= kIntLimit || s->max_length >= kIntLimit)
+  if (s->rows >= (int64_t)1 << 40 || s->channels >= kWidthLimit || s->sequences >= kIntLimit || s->max_length >= kIntLimit)
     return DGC_ERR_CAPACITY;
   if (!s->row_offsets && s->sequences * s->max_length != s->rows) return DGC_ERR_INVALID_ARG;
   if (s->row_offsets && !aligned_to(s->row_offsets, 8)) return DGC_ERR_ALIGNMENT;
-  return DGC_OK;
+  return scan_workgroups(scan_args(s)) < kIntLimit ? DGC_OK : DGC_ERR_CAPACITY;
 }
 
 int64_t state_rows(const dgc_scan* s) { return s->rows / DGC_SCAN_STATE_ROWS + s->sequences; }
 
 size_t logits_workspace(const dgc_logits*) { return 0; }
-size_t scan_workspace(const dgc_scan*) { return 0; }
 
 }  // namespace
 
@@ -134,7 +144,7 @@ dgc_status dgc_gated_scan_workspace_bytes(const dgc_scan* shape, size_t* bytes) 
   const dgc_status st = check_scan(shape);
   if (st != DGC_OK) return st;
   if (!bytes) return DGC_ERR_INVALID_ARG;
-  *bytes = scan_workspace(shape);
+  *bytes = scan_workspace_bytes(scan_args(shape));
   return DGC_OK;
 }
 
@@ -153,9 +163,7 @@ dgc_status dgc_gated_scan_forward(const dgc_scan* shape, const void* gate, int64
   if (st != DGC_OK) return st;
   if (gate_stride < shape->channels || x_stride < shape->channels || h_stride < shape->channels)
     return DGC_ERR_INVALID_ARG;
-  if (!addressable(shape->rows, gate_stride) || !addressable(shape->rows, x_stride) ||
-      !addressable(shape->rows, h_stride))
-    return DGC_ERR_CAPACITY;
+  if (gate_stride >= kWidthLimit || x_stride >= kWidthLimit || h_stride >= kWidthLimit) return DGC_ERR_CAPACITY;
   if (shape->sequences == 0) return DGC_OK;
   if (shape->rows > 0 && (!gate || !x || !h)) return DGC_ERR_INVALID_ARG;
   if ((h == gate && h && h_stride != gate_stride) || (h == x && h && h_stride != x_stride)) return DGC_ERR_INVALID_ARG;
@@ -163,8 +171,8 @@ dgc_status dgc_gated_scan_forward(const dgc_scan* shape, const void* gate, int64
   if (!aligned_to(gate, e) || !aligned_to(x, e) || !aligned_to(h, e) || !aligned_to(h0, 4) || !aligned_to(h_last, 4) ||
       !aligned_to(states, 4))
     return DGC_ERR_ALIGNMENT;
-  if ((st = check_workspace(workspace, workspace_bytes, scan_workspace(shape))) != DGC_OK) return st;
-  ScanArgs a{};
+  ScanArgs a = scan_args(shape);
+  if ((st = check_workspace(workspace, workspace_bytes, scan_workspace_bytes(a))) != DGC_OK) return st;
   a.gate = gate;
   a.x = x;
   a.gate_stride = gate_stride;
@@ -174,12 +182,7 @@ dgc_status dgc_gated_scan_forward(const dgc_scan* shape, const void* gate, int64
   a.states = states;
   a.h = h;
   a.h_stride = h_stride;
-  a.row_offsets = shape->row_offsets;
-  a.rows = shape->rows;
-  a.max_length = shape->max_length;
-  a.channels = shape->channels;
-  a.sequences = shape->sequences;
-  if (!hip_ok(launch_scan(a, shape->dtype, (shape->flags & DGC_SCAN_FREE_INPUT) != 0, false,
+  if (!hip_ok(launch_scan(a, workspace, shape->dtype, (shape->flags & DGC_SCAN_FREE_INPUT) != 0, false,
                           static_cast<hipStream_t>(stream_)),
               "launch scan kernels"))
     return DGC_ERR_HIP;
@@ -195,7 +198,7 @@ dgc_status dgc_gated_scan_backward(const dgc_scan* shape, const void* gate, int6
   if (st != DGC_OK) return st;
   for (int64_t stride : {gate_stride, x_stride, dh_stride, dgate_stride, dx_stride}) {
     if (stride < shape->channels) return DGC_ERR_INVALID_ARG;
-    if (!addressable(shape->rows, stride)) return DGC_ERR_CAPACITY;
+    if (stride >= kWidthLimit) return DGC_ERR_CAPACITY;
   }
   if (shape->sequences == 0) return DGC_OK;
   if (shape->rows > 0 && (!gate || !x || !states || !dh || !dgate || !dx)) return DGC_ERR_INVALID_ARG;
@@ -209,8 +212,8 @@ dgc_status dgc_gated_scan_backward(const dgc_scan* shape, const void* gate, int6
     if ((dgate == in[i] && dgate_stride != in_stride[i]) || (dx == in[i] && dx_stride != in_stride[i]))
       return DGC_ERR_INVALID_ARG;
   if (shape->rows > 0 && dgate == dx) return DGC_ERR_INVALID_ARG;
-  if ((st = check_workspace(workspace, workspace_bytes, scan_workspace(shape))) != DGC_OK) return st;
-  ScanArgs a{};
+  ScanArgs a = scan_args(shape);
+  if ((st = check_workspace(workspace, workspace_bytes, scan_workspace_bytes(a))) != DGC_OK) return st;
   a.gate = gate;
   a.x = x;
   a.gate_stride = gate_stride;
@@ -224,12 +227,7 @@ dgc_status dgc_gated_scan_backward(const dgc_scan* shape, const void* gate, int6
   a.dh_stride = dh_stride;
   a.dgate_stride = dgate_stride;
   a.dx_stride = dx_stride;
-  a.row_offsets = shape->row_offsets;
-  a.rows = shape->rows;
-  a.max_length = shape->max_length;
-  a.channels = shape->channels;
-  a.sequences = shape->sequences;
-  if (!hip_ok(launch_scan(a, shape->dtype, (shape->flags & DGC_SCAN_FREE_INPUT) != 0, true,
+  if (!hip_ok(launch_scan(a, workspace, shape->dtype, (shape->flags & DGC_SCAN_FREE_INPUT) != 0, true,
                           static_cast<hipStream_t>(stream_)),
               "launch scan kernels"))
     return DGC_ERR_HIP;
