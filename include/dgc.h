@@ -533,7 +533,7 @@ dgc_status dgc_gated_scan_state_rows(const dgc_scan* shape, int64_t* state_rows)
  *               be h0 itself: a serving loop calls this with max_length = 1 and one state array
  *   states      device, float[state_rows * channels], or NULL: what dgc_gated_scan_backward needs
  * h must not overlap gate or x unless it is one of them, address and stride.
- * Errors: INVALID_ARG, ALIGNMENT, CAPACITY (workspace; channels or strides of 2^26 and more), HIP.
+ * Errors: INVALID_ARG, ALIGNMENT, CAPACITY (workspace; channels or strides of 2^24 and more), HIP.
  */
 dgc_status dgc_gated_scan_forward(const dgc_scan* shape, const void* gate, int64_t gate_stride, const void* x,
                                   int64_t x_stride, const float* h0, void* h, int64_t h_stride, float* h_last,

@@ -62,20 +62,59 @@ size_t scan_workspace_bytes(const ScanArgs& a);  // of the shape alone
 int64_t scan_workgroups(const ScanArgs& a);      // tiles or workgroups, whichever a launch counts
 
 // ---- element types ---------------------------------------------------------------
-// An element as it lies in memory, and what it stands for.  To 16 bits: once, to the nearest, ties to even.
 template <typename T>
 __device__ __forceinline__ float to_float(T x) {
   return static_cast<float>(x);
 }
+// To 16 bits: once, to the nearest, ties to even.
 template <typename T>
 __device__ __forceinline__ T from_float(float x) {
   return static_cast<T>(x);
 }
 
-// N elements that lie behind each other, aligned to the whole of them.
+template <int BYTES>
+struct WordOf {
+  using type = uint32_t;
+};
+template <>
+struct WordOf<2> {
+  using type = uint16_t;
+};
+
+// N elements that lie behind each other, aligned to the whole of them, as the words they are loaded in: elements of 16
+// bits would take a register each.
 template <typename T, int N>
 struct alignas(sizeof(T) * N) Pack {
-  T e[N];
+  using Word = typename WordOf<sizeof(T) * N>::type;
+  static constexpr int kWords = (int)(sizeof(T) * N / sizeof(Word));
+  static constexpr int kPerWord = N / kWords;
+  Word w[kWords];
+  __device__ __forceinline__ float get(int j) const {
+    if constexpr (sizeof(T) == 4) {
+      return __uint_as_float(w[j]);
+    } else {
+      const uint32_t word = w[j / kPerWord];
+      if constexpr (__is_same(T, __bf16)) return __uint_as_float(j % kPerWord ? word & 0xffff0000u : word << 16);
+      return static_cast<float>(__builtin_bit_cast(T, (uint16_t)(j % kPerWord ? word >> 16 : word)));
+    }
+  }
+  __device__ __forceinline__ void set(const float (&v)[N]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) w[j] = __float_as_uint(v[j]);
+    } else if constexpr (N == 1) {
+      w[0] = __builtin_bit_cast(uint16_t, from_float<T>(v[0]));
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; j += 2)
+        w[j / 2] = (uint32_t)__builtin_bit_cast(uint16_t, from_float<T>(v[j])) | (uint32_t)__builtin_bit_cast(uint16_t, from_float<T>(v[j + 1])) << 16;
+    }
+  }
+  // From here on the compiler takes the words for new ones: it will not keep what it has made of them.
+  __device__ __forceinline__ void renew() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) asm volatile("" : "+v"(w[i]));
+  }
 };
 
 }  // namespace dgc

@@ -39,143 +39,116 @@ constexpr int kStateRows = DGC_SCAN_STATE_ROWS;
 __device__ __forceinline__ int64_t state_row(int64_t s, int64_t begin, int64_t c) { return begin / kStateRows + s + c; }
 
 // ---- tiles -------------------------------------------------------------------------------------
-// A wavefront takes kWaveRows steps of kBlock channels: VEC channels to a lane, 64 / VEC lanes to a row and so VEC groups
-// of lanes that take kWaveRows / VEC steps each, one after the other in registers.  A group's steps together are
-// h_out = A h_in + H; groups are joined by shuffles, the W wavefronts of a tile through LDS.
-constexpr int kWaveRows = 32;
-constexpr int kBlock = 64;
-static_assert(kStateRows % kWaveRows == 0, "a kept state lies in front of a wavefront's first step");
-
-// Tiles of one sequence and one block of channels follow each other.  What a tile does to a state is left in a word of its
-// own (A with its sign bit set, H), which is read by the tiles behind it in its group of kGroup tiles; the last tile of a
-// group leaves the state behind it instead (1.0 with the sign bit set, state).  A tile joins, in order, the state in front
-// of its group and the words of the group's tiles before its own: always the same sums, whoever comes first.
-// A word is stored and loaded whole, so that it needs no fence; zero says that it is not there yet.
-constexpr int kGroup = 32;
-
-struct Chain {
-  unsigned long long* words;  // [tile rows][channels]; null: a workgroup walks all tiles of a sequence and block
-  uint32_t* ticket;
-  uint32_t tickets;           // (tile row, block) in all
-  int64_t tile_rows;          // without row_offsets: tiles of a sequence
+// How a wavefront takes its share of a tile: VEC channels to a lane, GROUPS groups of lanes that take S steps each, one
+// after the other in registers.  A row's piece is 64 / GROUPS lanes wide (256 bytes where the rows' alignment allows it).
+// A group's steps together are h_out = A h_in + H; groups are joined by shuffles, wavefronts through LDS.
+template <typename T_, int VEC, int GROUPS, int S>
+struct Shape {
+  using T = T_;
+  static constexpr int kVec = VEC, kGroups = GROUPS, kSteps = S;
+  static constexpr int kLanes = 64 / GROUPS;
+  static constexpr int kBlock = kLanes * VEC;                   // channels
+  static constexpr int kRows = GROUPS * S;                      // of a wavefront
+  static constexpr int kStateWaves = kStateRows / kRows;        // wavefronts to a kept state
+  static_assert(kStateRows % kRows == 0, "a kept state lies in front of a wavefront's first step");
 };
 
-__device__ __forceinline__ unsigned long long chain_word(float a, float h) {
-  // a NaN leaves no finite state, whatever comes in
-  if (!(a <= 1.0f)) h = __builtin_nanf(""), a = 1.0f;
-  return (unsigned long long)(__float_as_uint(a) | 0x80000000u) << 32 | __float_as_uint(h);
-}
-
-__device__ __forceinline__ unsigned long long wait_for(const unsigned long long* p) {
-  unsigned long long w;
-  while (!((w = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) >> 63)) __builtin_amdgcn_s_sleep(1);
-  return w;
-}
-
-// The state in front of the tile at `position` of its chain (in the direction of travel), whose words lie `step` behind
-// those of the one before it (`first`: in front of the first group).  The rows of words waited for belong to lower tickets, and every ticket's workgroup leaves
-// its row, whatever the offsets hold: they run, or have run, and none of them waits for this one, so every wait ends.
-__device__ __forceinline__ float chain_state(const unsigned long long* word, int64_t step, int64_t position, float first) {
-  const int before = (int)(position % kGroup);
-  const unsigned long long* p = word - before * step;
-  float state = first;
-  if (position > before) state = __uint_as_float((uint32_t)wait_for(p - step));
-  for (int i = 0; i < before; ++i, p += step) {
-    const unsigned long long w = wait_for(p);
-    state = fmaf(__uint_as_float((uint32_t)(w >> 32) & 0x7fffffffu), state, __uint_as_float((uint32_t)w));
-  }
-  return state;
-}
-
-struct Tile {
-  int64_t sequence, begin, length;
-  int64_t index, count;  // in its sequence
-  int64_t word_row;      // of its words
-  int32_t block;
-  bool there;
+// Where a tile lies, for the wavefronts that work on it.
+struct Place {
+  int64_t row;    // of the arrays, its first
+  int64_t left;   // steps of the sequence from there on
+  int64_t state;  // row of the kept state in front of it
+  int64_t sequence;
+  int64_t word_row;  // of its words
+  int64_t position;  // in its sequence, in the direction of travel
+  int32_t block;     // of channels
+  int32_t last;      // no tile follows
+  int32_t there;
 };
 
-// Tile `ticket`.  Equal sequences: all first tiles, then all second ones.  With offsets: tile row
-// begin / rows + sequence + index, as for the kept states; rows of that numbering between two sequences stay empty.
-template <int ROWS, bool REVERSE>
-__device__ __forceinline__ Tile tile_of(const ScanArgs& a, const Chain& chain, uint32_t ticket) {
-  const uint32_t blocks = (uint32_t)((a.channels + kBlock - 1) / kBlock);
-  Tile t;
-  uint32_t row = ticket / blocks;
-  t.block = (int32_t)(ticket - row * blocks);
-  if (!a.row_offsets) {
-    const uint32_t sequences = (uint32_t)a.sequences;
-    const uint32_t c = row / sequences;
-    t.sequence = row - c * sequences;
-    sequence_rows(a, t.sequence, t.begin, t.length);
-    t.count = chain.tile_rows;
-    t.index = REVERSE ? t.count - 1 - c : c;
-    t.word_row = t.sequence * t.count + t.index;
-    t.there = true;
-    return t;
-  }
-  if (REVERSE) row = chain.tickets / blocks - 1 - row;
-  // the last sequence whose first tile row is not behind this one
-  const int lane = threadIdx.x & 63;
-  int64_t lo = 0, hi = a.sequences;
-  while (hi - lo > 1) {
-    const int64_t stride = (hi - lo + 63) / 64;
-    const int64_t at = lo + lane * stride;
-    int64_t begin = 0, length = 0;
-    if (at < hi) sequence_rows(a, at, begin, length);
-    const bool before = at < hi && begin / ROWS + at <= row;
-    const int passed = __popcll(__ballot(before));
-    const int64_t next = lo + passed * stride;
-    lo = passed ? next - stride : lo;
-    hi = next < hi && passed ? next : passed ? hi : lo + 1;
-  }
-  t.sequence = __builtin_amdgcn_readfirstlane((int)lo);
-  sequence_rows(a, t.sequence, t.begin, t.length);
-  t.count = (t.length + ROWS - 1) / ROWS;
-  t.count = t.count < 1 ? 1 : t.count;
-  t.index = (int64_t)row - (t.begin / ROWS + t.sequence);
-  t.word_row = row;
-  t.there = t.index >= 0 && t.index < t.count;
-  return t;
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)v >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ Place uniform(const Place& p) {
+  return Place{uniform(p.row), uniform(p.left), uniform(p.state), uniform(p.sequence), uniform(p.word_row), uniform(p.position),
+               __builtin_amdgcn_readfirstlane(p.block), __builtin_amdgcn_readfirstlane(p.last), __builtin_amdgcn_readfirstlane(p.there)};
 }
 
-// A tile row that belongs to no sequence leaves a word all the same: with offsets that do not ascend, some tile may look
-// for it.
-__device__ __forceinline__ void skip_tile(const ScanArgs& a, const Chain& chain, const Tile& t, int64_t channel) {
-  if (threadIdx.x < 64 && channel < a.channels)
-    __hip_atomic_store(chain.words + t.word_row * a.channels + channel, chain_word(1.0f, 0.0f), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// What of a place one lane works on.
+struct Share {
+  int64_t at;  // row of the arrays, the wavefront's first
+  int64_t d;   // channel, the lane's first
+  int group;   // of lanes
+  int steps;   // of the lane
+  int rows;    // of the wavefront
+  bool full;   // no lane of the wavefront has fewer steps than all
+};
+
+template <typename SHAPE>
+__device__ __forceinline__ Share share_of(const ScanArgs& a, const Place& p, int w, int lane) {
+  constexpr int S = SHAPE::kSteps, kRows = SHAPE::kRows;
+  Share h;
+  h.group = lane / SHAPE::kLanes;
+  h.d = (int64_t)p.block * SHAPE::kBlock + (lane % SHAPE::kLanes) * SHAPE::kVec;
+  h.at = p.row + w * kRows;
+  const int64_t left = p.left - w * kRows;
+  h.rows = (int)(left < 0 ? 0 : left > kRows ? kRows : left);
+  const int mine = h.rows - h.group * S;
+  h.steps = h.d < a.channels ? (mine < 0 ? 0 : mine > S ? S : mine) : 0;
+  h.full = __all(h.steps == S);
+  return h;
 }
 
-// VEC elements of every step of a lane; steps behind the last one are not read.
-template <typename T, int VEC, int S>
-__device__ __forceinline__ void load_steps(const T* p, int64_t stride, uint32_t lane_offset, int steps, bool full, Pack<T, VEC> (&out)[S]) {
-  if (full) {
-#pragma unroll
-    for (int i = 0; i < S; ++i) out[i] = *reinterpret_cast<const Pack<T, VEC>*>(p + i * stride + lane_offset);
-  } else {
-#pragma unroll
-    for (int i = 0; i < S; ++i) {
-      out[i] = Pack<T, VEC>{};
-      if (i < steps) out[i] = *reinterpret_cast<const Pack<T, VEC>*>(p + i * stride + lane_offset);
-    }
-  }
-}
+// The wavefront's rows of an array as a buffer resource: an offset behind the last of them reads zeros and stores nothing,
+// and one register to a lane is all that addresses take.  (Data format 32 in word 3, no swizzle, offsets in bytes.)
+constexpr int kBufferFormat = 0x00020000;
+constexpr uint32_t kNowhere = 0xf0000000u;  // behind the end of every such buffer: up to 32 rows of less than 2^24 elements
 
 template <typename T, int VEC, int S>
-__device__ __forceinline__ void store_steps(T* p, int64_t stride, uint32_t lane_offset, int steps, int i, const Pack<T, VEC>& v) {
-  if (i < steps) *reinterpret_cast<Pack<T, VEC>*>(p + i * stride + lane_offset) = v;
+struct Steps {
+  __amdgpu_buffer_rsrc_t rsrc;
+  uint32_t first, stride;  // bytes
+  __device__ __forceinline__ Steps(const void* array, int64_t stride_, const Share& h)
+      : rsrc(__builtin_amdgcn_make_buffer_rsrc((void*)(static_cast<const T*>(array) + h.at * stride_), 0,
+                                               (int)((uint32_t)h.rows * (uint32_t)stride_ * (uint32_t)sizeof(T)), kBufferFormat)),
+        stride((uint32_t)stride_ * (uint32_t)sizeof(T)) {
+    first = h.steps > 0 ? (uint32_t)(h.group * S) * stride + (uint32_t)h.d * (uint32_t)sizeof(T) : kNowhere;
+  }
+  __device__ __forceinline__ Pack<T, VEC> load(int i) const {
+    const uint32_t at = first + (uint32_t)i * stride;
+    if constexpr (sizeof(T) * VEC == 8) return __builtin_bit_cast(Pack<T, VEC>, __builtin_amdgcn_raw_buffer_load_b64(rsrc, at, 0, 0));
+    else if constexpr (sizeof(T) * VEC == 4) return __builtin_bit_cast(Pack<T, VEC>, __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, 0, 0));
+    else return __builtin_bit_cast(Pack<T, VEC>, __builtin_amdgcn_raw_buffer_load_b16(rsrc, at, 0, 0));
+  }
+  __device__ __forceinline__ void store(int i, const Pack<T, VEC>& v) const {
+    const uint32_t at = first + (uint32_t)i * stride;
+    typedef uint32_t two __attribute__((ext_vector_type(2)));
+    if constexpr (sizeof(T) * VEC == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(two, v), rsrc, at, 0, 0);
+    else if constexpr (sizeof(T) * VEC == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), rsrc, at, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), rsrc, at, 0, 0);
+  }
+};
+
+// VEC elements of every step of a lane, zeros behind the last one.
+template <typename T, int VEC, int S>
+__device__ __forceinline__ void load_steps(const void* array, int64_t stride, const Share& h, Pack<T, VEC> (&out)[S]) {
+  const Steps<T, VEC, S> steps(array, stride, h);
+#pragma unroll
+  for (int i = 0; i < S; ++i) out[i] = steps.load(i);
 }
 
-// (A, H) of the lane groups in front of this one; A, H become those up to and with this one.
-template <int VEC, bool DOWN>
+// (A0, H0) of the lane groups in front of this one (DOWN: behind it); A, H become those up to and with this one.
+template <int GROUPS, bool DOWN, int VEC>
 __device__ __forceinline__ void join_groups(float (&A)[VEC], float (&H)[VEC], float (&A0)[VEC], float (&H0)[VEC], int group) {
-  constexpr int kLanes = 64 / VEC;
+  constexpr int kLanes = 64 / GROUPS;
+  auto other = [](float x, int lanes) { return DOWN ? __shfl_down(x, lanes) : __shfl_up(x, lanes); };
 #pragma unroll
-  for (int o = kLanes; o < 64; o *= 2) {
-    const bool has = DOWN ? group < VEC - o / kLanes : group >= o / kLanes;
+  for (int o = 1; o < GROUPS; o *= 2) {
+    const bool has = DOWN ? group < GROUPS - o : group >= o;
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
-      const float pa = DOWN ? __shfl_down(A[j], o) : __shfl_up(A[j], o), ph = DOWN ? __shfl_down(H[j], o) : __shfl_up(H[j], o);
+      const float pa = other(A[j], o * kLanes), ph = other(H[j], o * kLanes);
       if (has) {
         H[j] = fmaf(A[j], ph, H[j]);
         A[j] *= pa;
@@ -186,9 +159,9 @@ __device__ __forceinline__ void join_groups(float (&A)[VEC], float (&H)[VEC], fl
   for (int j = 0; j < VEC; ++j) {
     A0[j] = 1.0f;
     H0[j] = 0.0f;
-    if (VEC > 1) {
-      const float pa = DOWN ? __shfl_down(A[j], kLanes) : __shfl_up(A[j], kLanes), ph = DOWN ? __shfl_down(H[j], kLanes) : __shfl_up(H[j], kLanes);
-      if (DOWN ? group < VEC - 1 : group > 0) {
+    if (GROUPS > 1) {
+      const float pa = other(A[j], kLanes), ph = other(H[j], kLanes);
+      if (DOWN ? group < GROUPS - 1 : group > 0) {
         A0[j] = pa;
         H0[j] = ph;
       }
@@ -196,147 +169,98 @@ __device__ __forceinline__ void join_groups(float (&A)[VEC], float (&H)[VEC], fl
   }
 }
 
-template <typename T, int VEC, int W, bool FREE, bool CHAIN>
-__global__ __launch_bounds__(W * 64) void scan_forward_kernel(ScanArgs a, Chain chain) {
-  constexpr int S = kWaveRows / VEC, kLanes = 64 / VEC, kRows = W * kWaveRows;
-  __shared__ float2 part[W][kBlock];
-  __shared__ float start[W][kBlock];
-  __shared__ uint32_t next;
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int group = lane / kLanes, col = (lane % kLanes) * VEC;
-  uint32_t ticket = blockIdx.x;
-  if (CHAIN) {
-    if (threadIdx.x == 0) next = atomicAdd(chain.ticket, 1u);
-    __syncthreads();
-    ticket = next;
-    if (ticket >= chain.tickets) return;
+// ---- one wavefront's share of a tile, forward ------------------------------------------------------
+template <typename SHAPE>
+struct ForwardInput {
+  using T = typename SHAPE::T;
+  static constexpr int VEC = SHAPE::kVec, S = SHAPE::kSteps;
+  Pack<T, VEC> gate[S], x[S];
+  __device__ __forceinline__ void load(const ScanArgs& a, const Place&, int, const Share& h) {
+    load_steps<T, VEC, S>(a.gate, a.gate_stride, h, gate);
+    load_steps<T, VEC, S>(a.x, a.x_stride, h, x);
   }
-  Tile t{};
-  if (!CHAIN) {
-    const uint32_t blocks = (uint32_t)((a.channels + kBlock - 1) / kBlock);
-    t.sequence = ticket / blocks;
-    t.block = (int32_t)(ticket - (uint32_t)t.sequence * blocks);
-    sequence_rows(a, t.sequence, t.begin, t.length);
-    t.count = (t.length + kRows - 1) / kRows;
-    t.count = t.count < 1 ? 1 : t.count;
-    t.there = true;
-  }
-  float carried = 0.0f;  // wavefront 0, lane by channel: the state in front of the tile
-  for (;;) {
-    uint32_t taken = 0;
-    if (CHAIN) {
-      if (threadIdx.x == 0) taken = atomicAdd(chain.ticket, 1u);
-      t = tile_of<kRows, false>(a, chain, ticket);
-    }
-    const int64_t channel = (int64_t)t.block * kBlock + lane;
-    const int64_t d = (int64_t)t.block * kBlock + col;
-    if (t.there) {
-      const int64_t row = t.index * kRows + w * kWaveRows;  // of the sequence, the wavefront's first
-      const int64_t left = t.length - row - group * S;
-      const int steps = d < a.channels ? (int)(left < 0 ? 0 : left > S ? S : left) : 0;
-      const bool full = __all(steps == S);
-      const int64_t at = t.begin + row;
-      Pack<T, VEC> rf[S], rx[S];
-      load_steps<T, VEC, S>(static_cast<const T*>(a.gate) + at * a.gate_stride, a.gate_stride, (uint32_t)(group * S * a.gate_stride + d), steps, full, rf);
-      load_steps<T, VEC, S>(static_cast<const T*>(a.x) + at * a.x_stride, a.x_stride, (uint32_t)(group * S * a.x_stride + d), steps, full, rx);
-      float ca[S][VEC], cu[S][VEC];
-      float A[VEC], H[VEC], A0[VEC], H0[VEC];
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) A[j] = 1.0f, H[j] = 0.0f;
-#pragma unroll
-      for (int i = 0; i < S; ++i) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const Gates g = gates_of(to_float(rf[i].e[j]));
-          const float xt = to_float(rx[i].e[j]);
-          ca[i][j] = g.a;
-          cu[i][j] = FREE ? xt : g.b * xt;
-        }
-        if (!full && i >= steps) {
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) ca[i][j] = 1.0f, cu[i][j] = 0.0f;
-        }
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          H[j] = fmaf(ca[i][j], H[j], cu[i][j]);
-          A[j] *= ca[i][j];
-        }
-      }
-      join_groups<VEC, false>(A, H, A0, H0, group);
-      if (group == VEC - 1) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) part[w][col + j] = float2{A[j], H[j]};
-      }
-      __syncthreads();
-      if (w == 0) {
-        if (channel < a.channels) {
-          const int64_t carry_at = t.sequence * a.channels + channel;
-          float state = carried;
-          if (CHAIN ? t.index < kGroup : t.index == 0) state = a.first ? a.first[carry_at] : 0.0f;
-          if (CHAIN) {
-            unsigned long long* word = chain.words + t.word_row * a.channels + channel;
-            const bool closes = t.index % kGroup == kGroup - 1;
-            if (!closes) {
-              float ta = 1.0f, th = 0.0f;
-#pragma unroll
-              for (int v = 0; v < W; ++v) {
-                th = fmaf(part[v][lane].x, th, part[v][lane].y);
-                ta *= part[v][lane].x;
-              }
-              __hip_atomic_store(word, chain_word(ta, th), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
-            state = chain_state(word, a.channels, t.index, state);
-          }
-#pragma unroll
-          for (int v = 0; v < W; ++v) {
-            start[v][lane] = state;
-            state = fmaf(part[v][lane].x, state, part[v][lane].y);
-          }
-          carried = state;
-          if (CHAIN && t.index % kGroup == kGroup - 1)
-            __hip_atomic_store(chain.words + t.word_row * a.channels + channel, chain_word(1.0f, state), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          if (t.index + 1 == t.count && a.last) a.last[carry_at] = state;
-        }
-        if (CHAIN && threadIdx.x == 0) next = taken;
-      }
-      __syncthreads();
-      float state[VEC];
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) state[j] = start[w][col + j];
-      if (a.states && group == 0 && steps > 0 && w % (kStateRows / kWaveRows) == 0) {
-        float* kept = a.states + state_row(t.sequence, t.begin, row / kStateRows) * a.channels + d;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) kept[j] = state[j];
-      }
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) state[j] = fmaf(A0[j], state[j], H0[j]);
-      T* h = static_cast<T*>(a.h) + at * a.h_stride;
-      const uint32_t lane_offset = (uint32_t)(group * S * a.h_stride + d);
-#pragma unroll
-      for (int i = 0; i < S; ++i) {
-        Pack<T, VEC> out;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          state[j] = fmaf(ca[i][j], state[j], cu[i][j]);
-          out.e[j] = from_float<T>(state[j]);
-        }
-        store_steps<T, VEC, S>(h, a.h_stride, lane_offset, steps, i, out);
-      }
-    } else if (CHAIN) {
-      skip_tile(a, chain, t, channel);
-      __syncthreads();
-      if (threadIdx.x == 0) next = taken;
-      __syncthreads();
-    }
-    if (CHAIN) {
-      ticket = next;
-      if (ticket >= chain.tickets) return;
-    } else if (++t.index == t.count) {
-      return;
-    }
-  }
-}
+};
 
+template <typename SHAPE_, int W, bool FREE>
+struct ForwardTile {
+  using SHAPE = SHAPE_;
+  using T = typename SHAPE::T;
+  static constexpr int VEC = SHAPE::kVec, S = SHAPE::kSteps, kBlock = SHAPE::kBlock, kStateWaves = SHAPE::kStateWaves;
+  static constexpr bool kReverse = false;
+  using Input = ForwardInput<SHAPE>;
+  struct Parts {  // what a tile's wavefronts leave in LDS
+    float2 of[W][kBlock];
+  };
+  float ca[S][VEC], cu[S][VEC], A0[VEC], H0[VEC];
+
+  // Gates and inputs of every step, and what the wavefront does to a state.
+  __device__ __forceinline__ void fold(const Input& in, const Share& h, int w, int col, Parts& parts) {
+    float A[VEC], H[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) A[j] = 1.0f, H[j] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const Gates g = gates_of(in.gate[i].get(j));
+        const float xt = in.x[i].get(j);
+        ca[i][j] = g.a;
+        cu[i][j] = FREE ? xt : g.b * xt;
+      }
+    }
+    if (!h.full) {  // steps behind the last one leave the state alone
+#pragma unroll
+      for (int i = 0; i < S; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) ca[i][j] = i < h.steps ? ca[i][j] : 1.0f, cu[i][j] = i < h.steps ? cu[i][j] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        H[j] = fmaf(ca[i][j], H[j], cu[i][j]);
+        A[j] *= ca[i][j];
+      }
+    }
+    join_groups<SHAPE::kGroups, false>(A, H, A0, H0, h.group);
+    if (h.group == SHAPE::kGroups - 1) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) parts.of[w][col + j] = float2{A[j], H[j]};
+    }
+  }
+
+  __device__ __forceinline__ void between(const Parts&, int, int) {}
+
+  // One lane by channel: (A, H) of the tile's wavefronts in the direction of travel, the i-th.
+  static __device__ __forceinline__ float2 part(const Parts& parts, int i, int channel) { return parts.of[i][channel]; }
+
+  // The states, from the one in front of the tile.
+  __device__ __forceinline__ void apply(const ScanArgs& a, const Place& p, const Share& h, int w, int col, const Parts& parts,
+                                        float (&state)[VEC]) {
+    for (int v = 0; v < w; ++v) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) state[j] = fmaf(parts.of[v][col + j].x, state[j], parts.of[v][col + j].y);
+    }
+    if (a.states && h.group == 0 && h.steps > 0 && w % kStateWaves == 0) {
+      float* kept = a.states + (p.state + w / kStateWaves) * a.channels + h.d;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) kept[j] = state[j];
+    }
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) state[j] = fmaf(A0[j], state[j], H0[j]);
+    const Steps<T, VEC, S> out(a.h, a.h_stride, h);
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) state[j] = fmaf(ca[i][j], state[j], cu[i][j]);
+      Pack<T, VEC> v;
+      v.set(state);
+      out.store(i, v);
+    }
+  }
+};
+
+// ---- the same backward ---------------------------------------------------------------------------------
 // The smaller of sigmoid(f) and sigmoid(-f), its sign bit set where it is the first: one register that gives both back,
 // the larger as one minus the smaller, which keeps the relative accuracy of each.
 __device__ __forceinline__ float fold_gates(float f) {
@@ -349,210 +273,406 @@ __device__ __forceinline__ Gates unfold_gates(float v) {
   return (__float_as_uint(v) >> 31) ? Gates{m, o} : Gates{o, m};
 }
 
-// The same tiles from the last to the first.  A wavefront forms its states again from the kept one in front of it (an odd
-// one by way of its neighbour's steps), and the gradient runs through the tiles as the state does in the forward pass.
-template <typename T, int VEC, int W, bool FREE, bool CHAIN>
-__global__ __launch_bounds__(W * 64, 3) void scan_backward_kernel(ScanArgs a, Chain chain) {
-  constexpr int S = kWaveRows / VEC, kLanes = 64 / VEC, kRows = W * kWaveRows;
-  static_assert(kStateRows == 2 * kWaveRows && W % 2 == 0, "two wavefronts to a kept state");
-  __shared__ float2 part[W][kBlock];
-  __shared__ float back[W][kBlock];
-  __shared__ float start[W][kBlock];
-  __shared__ uint32_t next;
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int group = lane / kLanes, col = (lane % kLanes) * VEC;
-  uint32_t ticket = blockIdx.x;
-  if (CHAIN) {
-    if (threadIdx.x == 0) next = atomicAdd(chain.ticket, 1u);
-    __syncthreads();
-    ticket = next;
-    if (ticket >= chain.tickets) return;
-  }
-  Tile t{};
-  if (!CHAIN) {
-    const uint32_t blocks = (uint32_t)((a.channels + kBlock - 1) / kBlock);
-    t.sequence = ticket / blocks;
-    t.block = (int32_t)(ticket - (uint32_t)t.sequence * blocks);
-    sequence_rows(a, t.sequence, t.begin, t.length);
-    t.count = (t.length + kRows - 1) / kRows;
-    t.count = t.count < 1 ? 1 : t.count;
-    t.index = t.count - 1;
-    t.there = true;
-  }
-  float carried = 0.0f;
-  for (;;) {
-    uint32_t taken = 0;
-    if (CHAIN) {
-      if (threadIdx.x == 0) taken = atomicAdd(chain.ticket, 1u);
-      t = tile_of<kRows, true>(a, chain, ticket);
+template <typename SHAPE>
+struct BackwardInput {
+  using T = typename SHAPE::T;
+  static constexpr int VEC = SHAPE::kVec, S = SHAPE::kSteps;
+  Pack<T, VEC> gate[S], x[S], dh[S];
+  float state[VEC];  // the kept one in front of the wavefront, or of one of the few before it
+  __device__ __forceinline__ void load(const ScanArgs& a, const Place& p, int w, const Share& h) {
+    load_steps<T, VEC, S>(a.gate, a.gate_stride, h, gate);
+    load_steps<T, VEC, S>(a.x, a.x_stride, h, x);
+    load_steps<T, VEC, S>(a.dh, a.dh_stride, h, dh);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) state[j] = 0.0f;
+    if (h.d < a.channels && w / SHAPE::kStateWaves * kStateRows < p.left) {
+      const float* kept = a.states + (p.state + w / SHAPE::kStateWaves) * a.channels + h.d;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) state[j] = kept[j];
     }
-    const int64_t channel = (int64_t)t.block * kBlock + lane;
-    const int64_t d = (int64_t)t.block * kBlock + col;
-    if (t.there) {
-      const int64_t row = t.index * kRows + w * kWaveRows;
-      const int64_t left = t.length - row - group * S;
-      const int steps = d < a.channels ? (int)(left < 0 ? 0 : left > S ? S : left) : 0;
-      const bool full = __all(steps == S);
-      const int64_t at = t.begin + row;
-      Pack<T, VEC> rf[S], rx[S], rd[S];
-      load_steps<T, VEC, S>(static_cast<const T*>(a.gate) + at * a.gate_stride, a.gate_stride, (uint32_t)(group * S * a.gate_stride + d), steps, full, rf);
-      load_steps<T, VEC, S>(static_cast<const T*>(a.x) + at * a.x_stride, a.x_stride, (uint32_t)(group * S * a.x_stride + d), steps, full, rx);
-      load_steps<T, VEC, S>(static_cast<const T*>(a.dh) + at * a.dh_stride, a.dh_stride, (uint32_t)(group * S * a.dh_stride + d), steps, full, rd);
-      float state[VEC];  // the kept state in front of the pair of wavefronts
-      {
-        const int64_t pair_row = row - (w & 1) * kWaveRows;
+  }
+};
+
+// A wavefront forms its states again from the kept one in front of it (an odd one by way of its neighbour's steps); the
+// gradient runs through the tiles, from the last to the first, as the state does in the forward pass.
+template <typename SHAPE_, int W, bool FREE>
+struct BackwardTile {
+  using SHAPE = SHAPE_;
+  using T = typename SHAPE::T;
+  static constexpr int VEC = SHAPE::kVec, S = SHAPE::kSteps, kBlock = SHAPE::kBlock, kStateWaves = SHAPE::kStateWaves;
+  static constexpr bool kReverse = true;
+  static_assert(W % kStateWaves == 0, "tiles start at kept states");
+  using Input = BackwardInput<SHAPE>;
+  struct Parts {
+    float2 of[W][kBlock];  // forward
+    float back[W][kBlock];
+  };
+  float cm[S][VEC], before[S][VEC], A0[VEC], H0[VEC], B0[VEC], G0[VEC], state[VEC];
+  Pack<T, VEC> x[S], dh[S];
+
+  __device__ __forceinline__ void fold(const Input& in, const Share& h, int w, int col, Parts& parts) {
+    float A[VEC], H[VEC], B[VEC], G[VEC];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) state[j] = 0.0f;
-        if (d < a.channels && pair_row < t.length) {
-          const float* kept = a.states + state_row(t.sequence, t.begin, pair_row / kStateRows) * a.channels + d;
+    for (int j = 0; j < VEC; ++j) A[j] = 1.0f, H[j] = 0.0f, G[j] = 0.0f, state[j] = in.state[j];
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) state[j] = kept[j];
-        }
-      }
-      float cm[S][VEC];
-      float A[VEC], H[VEC], A0[VEC], H0[VEC], B[VEC], G[VEC], B0[VEC], G0[VEC];
+    for (int i = 0; i < S; ++i) {
+      x[i] = in.x[i];
+      dh[i] = in.dh[i];  // zero behind the last step
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) A[j] = 1.0f, H[j] = 0.0f, G[j] = 0.0f;
-#pragma unroll
-      for (int i = 0; i < S; ++i) {
-        if (!full && i >= steps) {
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) rx[i].e[j] = rd[i].e[j] = from_float<T>(0.0f), cm[i][j] = 0.0f;  // a = 1, b = 0
-        } else {
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) cm[i][j] = fold_gates(to_float(rf[i].e[j]));
-        }
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const Gates g = unfold_gates(cm[i][j]);
-          const float xt = to_float(rx[i].e[j]);
-          H[j] = fmaf(g.a, H[j], FREE ? xt : g.b * xt);
-          A[j] *= g.a;
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) B[j] = A[j];
-#pragma unroll
-      for (int i = S - 1; i >= 0; --i)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) G[j] = unfold_gates(cm[i][j]).a * (to_float(rd[i].e[j]) + G[j]);
-      join_groups<VEC, false>(A, H, A0, H0, group);
-      join_groups<VEC, true>(B, G, B0, G0, group);
-      if (group == VEC - 1) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) part[w][col + j] = float2{A[j], H[j]};
-      }
-      if (group == 0) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) back[w][col + j] = G[j];
-      }
-      __syncthreads();
-      if (w == 0) {
-        if (channel < a.channels) {
-          const int64_t carry_at = t.sequence * a.channels + channel;
-          const int64_t position = t.count - 1 - t.index;
-          float flow = carried;
-          if (CHAIN ? position < kGroup : position == 0) flow = a.first ? a.first[carry_at] : 0.0f;
-          if (CHAIN) {
-            unsigned long long* word = chain.words + t.word_row * a.channels + channel;
-            const bool closes = position % kGroup == kGroup - 1;
-            if (!closes) {
-              float ta = 1.0f, th = 0.0f;
-#pragma unroll
-              for (int v = W - 1; v >= 0; --v) {
-                th = fmaf(part[v][lane].x, th, back[v][lane]);
-                ta *= part[v][lane].x;
-              }
-              __hip_atomic_store(word, chain_word(ta, th), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
-            flow = chain_state(word, -a.channels, position, flow);
-          }
-#pragma unroll
-          for (int v = W - 1; v >= 0; --v) {
-            start[v][lane] = flow;
-            flow = fmaf(part[v][lane].x, flow, back[v][lane]);
-          }
-          carried = flow;
-          if (CHAIN && position % kGroup == kGroup - 1)
-            __hip_atomic_store(chain.words + t.word_row * a.channels + channel, chain_word(1.0f, flow), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          if (t.index == 0 && a.last) a.last[carry_at] = flow;
-        }
-        if (CHAIN && threadIdx.x == 0) next = taken;
-      }
-      if (w & 1) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) state[j] = fmaf(part[w - 1][col + j].x, state[j], part[w - 1][col + j].y);
-      }
-      float before[S][VEC];
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) state[j] = fmaf(A0[j], state[j], H0[j]);
+      for (int j = 0; j < VEC; ++j) cm[i][j] = fold_gates(in.gate[i].get(j));
+    }
+    if (!h.full) {  // a = 1, b = 0 there
 #pragma unroll
       for (int i = 0; i < S; ++i)
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const Gates g = unfold_gates(cm[i][j]);
-          const float xt = to_float(rx[i].e[j]);
-          before[i][j] = FREE ? state[j] : state[j] - xt;
-          state[j] = fmaf(g.a, state[j], FREE ? xt : g.b * xt);
-        }
-      __syncthreads();
-      float flow[VEC];
+        for (int j = 0; j < VEC; ++j) cm[i][j] = i < h.steps ? cm[i][j] : 0.0f;
+    }
+    keep_folded();
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) flow[j] = fmaf(B0[j], start[w][col + j], G0[j]);
-      T* dgate = static_cast<T*>(a.dgate) + at * a.dgate_stride;
-      T* dx = static_cast<T*>(a.dx) + at * a.dx_stride;
-      const uint32_t gate_offset = (uint32_t)(group * S * a.dgate_stride + d), x_offset = (uint32_t)(group * S * a.dx_stride + d);
+    for (int i = 0; i < S; ++i) {
 #pragma unroll
-      for (int i = S - 1; i >= 0; --i) {
-        Pack<T, VEC> og, ox;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const Gates g = unfold_gates(cm[i][j]);
-          const float gt = to_float(rd[i].e[j]) + flow[j];
-          ox.e[j] = from_float<T>(FREE ? gt : g.b * gt);
-          og.e[j] = from_float<T>(gt * before[i][j] * (g.a * g.b));
-          flow[j] = g.a * gt;
-        }
-        store_steps<T, VEC, S>(dx, a.dx_stride, x_offset, steps, i, ox);
-        store_steps<T, VEC, S>(dgate, a.dgate_stride, gate_offset, steps, i, og);
+      for (int j = 0; j < VEC; ++j) {
+        const Gates g = unfold_gates(cm[i][j]);
+        const float xt = x[i].get(j);
+        H[j] = fmaf(g.a, H[j], FREE ? xt : g.b * xt);
+        A[j] *= g.a;
+        G[j] = fmaf(A[j], dh[i].get(j), G[j]);  // what dh of this step leaves in front of the first one
       }
-    } else if (CHAIN) {
-      skip_tile(a, chain, t, channel);
-      __syncthreads();
-      if (threadIdx.x == 0) next = taken;
-      __syncthreads();
     }
-    if (CHAIN) {
-      ticket = next;
-      if (ticket >= chain.tickets) return;
-    } else if (--t.index < 0) {
-      return;
+    keep_folded();
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) B[j] = A[j];
+    join_groups<SHAPE::kGroups, false>(A, H, A0, H0, h.group);
+    join_groups<SHAPE::kGroups, true>(B, G, B0, G0, h.group);
+    if (h.group == SHAPE::kGroups - 1) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) parts.of[w][col + j] = float2{A[j], H[j]};
     }
+    if (h.group == 0) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) parts.back[w][col + j] = G[j];
+    }
+  }
+
+  // The compiler would rather keep both factors of all steps, in twice the registers, than form them again.
+  __device__ __forceinline__ void keep_folded() {
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) asm volatile("" : "+v"(cm[i][j]));
+      x[i].renew();
+      dh[i].renew();
+    }
+  }
+
+  static __device__ __forceinline__ float2 part(const Parts& parts, int i, int channel) {
+    return float2{parts.of[W - 1 - i][channel].x, parts.back[W - 1 - i][channel]};
+  }
+
+  // While the gradient is on its way: the states once more, h_{t-1} - x_t of every step.
+  __device__ __forceinline__ void between(const Parts& parts, int w, int col) {
+    for (int v = w / kStateWaves * kStateWaves; v < w; ++v) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) state[j] = fmaf(parts.of[v][col + j].x, state[j], parts.of[v][col + j].y);
+    }
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) state[j] = fmaf(A0[j], state[j], H0[j]);
+#pragma unroll
+    for (int i = 0; i < S; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const Gates g = unfold_gates(cm[i][j]);
+        const float xt = x[i].get(j);
+        before[i][j] = FREE ? state[j] : state[j] - xt;
+        state[j] = fmaf(g.a, state[j], FREE ? xt : g.b * xt);
+      }
+    keep_folded();
+  }
+
+  __device__ __forceinline__ void apply(const ScanArgs& a, const Place&, const Share& h, int w, int col, const Parts& parts,
+                                        float (&flow)[VEC]) {
+    for (int v = W - 1; v > w; --v) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) flow[j] = fmaf(parts.of[v][col + j].x, flow[j], parts.back[v][col + j]);
+    }
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) flow[j] = fmaf(B0[j], flow[j], G0[j]);
+    const Steps<T, VEC, S> out_gate(a.dgate, a.dgate_stride, h), out_x(a.dx, a.dx_stride, h);
+#pragma unroll
+    for (int i = S - 1; i >= 0; --i) {
+      float vg[VEC], vx[VEC];
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const Gates g = unfold_gates(cm[i][j]);
+        const float gt = dh[i].get(j) + flow[j];
+        vx[j] = FREE ? gt : g.b * gt;
+        vg[j] = gt * before[i][j] * (g.a * g.b);
+        flow[j] = g.a * gt;
+      }
+      Pack<T, VEC> og, ox;
+      og.set(vg);
+      ox.set(vx);
+      out_x.store(i, ox);
+      out_gate.store(i, og);
+    }
+  }
+};
+
+// ---- short sequences: a workgroup walks the tiles of one sequence and block ---------------------------------
+template <typename TILE, int W>
+__global__ __launch_bounds__(W * 64) void scan_walk_kernel(ScanArgs a) {
+  using SHAPE = typename TILE::SHAPE;
+  constexpr int VEC = SHAPE::kVec, kBlock = SHAPE::kBlock, kRows = W * SHAPE::kRows;
+  __shared__ typename TILE::Parts parts[2];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane % SHAPE::kLanes * VEC;
+  const uint32_t blocks = (uint32_t)((a.channels + kBlock - 1) / kBlock);
+  const uint32_t s = blockIdx.x / blocks;
+  int64_t begin, length;
+  sequence_rows(a, s, begin, length);
+  const int64_t count = length > 0 ? (length + kRows - 1) / kRows : 1;
+  const int64_t d = (int64_t)(blockIdx.x - s * blocks) * kBlock + col;
+  float carry[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) carry[j] = a.first && d + j < a.channels ? a.first[s * a.channels + d + j] : 0.0f;
+  for (int64_t i = 0; i < count; ++i) {
+    const int64_t index = TILE::kReverse ? count - 1 - i : i;
+    const Place p{begin + index * kRows, length - index * kRows, state_row(s, begin, index * (kRows / kStateRows)), s, 0, i,
+                  (int32_t)(blockIdx.x - s * blocks), 0, 1};
+    const Share h = share_of<SHAPE>(a, p, w, lane);
+    typename TILE::Input in;
+    TILE tile;
+    in.load(a, p, w, h);
+    tile.fold(in, h, w, col, parts[i & 1]);
+    __syncthreads();
+    tile.between(parts[i & 1], w, col);
+    float state[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) state[j] = carry[j];
+#pragma unroll
+    for (int v = 0; v < W; ++v)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float2 part = TILE::part(parts[i & 1], v, col + j);
+        carry[j] = fmaf(part.x, carry[j], part.y);
+      }
+    tile.apply(a, p, h, w, col, parts[i & 1], state);
+  }
+  if (a.last && w == 0 && lane < SHAPE::kLanes && d < a.channels) {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) a.last[s * a.channels + d + j] = carry[j];
   }
 }
 
-template <typename T, int VEC, int W, bool CHAIN>
-hipError_t launch_tiles(const ScanArgs& a, const Chain& chain, uint32_t groups, bool free_input, bool backward, hipStream_t stream) {
-  auto kernel = backward ? (free_input ? scan_backward_kernel<T, VEC, W, true, CHAIN> : scan_backward_kernel<T, VEC, W, false, CHAIN>)
-                         : (free_input ? scan_forward_kernel<T, VEC, W, true, CHAIN> : scan_forward_kernel<T, VEC, W, false, CHAIN>);
-  kernel<<<dim3(groups), W * 64, 0, stream>>>(a, chain);
-  return hipGetLastError();
+// ---- long sequences: tiles side by side ---------------------------------------------------------------------
+// Tiles of one sequence and block of channels follow each other.  What a tile does to a state is left in a word of its own
+// (A with its sign bit set, H), which is read by the tiles behind it in its group of kGroup tiles; the last tile of a group,
+// and the first of a sequence, leave the state behind them instead (0 with the sign bit set, state).  A tile joins, in order,
+// the state in front of its group and the words of the group's tiles before its own: always the same sums, whoever comes
+// first.  A word is stored and loaded whole, so that it needs no fence; zero says that it is not there yet.
+constexpr int kGroup = 16;
+
+struct Chain {
+  unsigned long long* words;  // [tile rows][channels]
+  uint32_t* ticket;
+  uint32_t tickets;   // (tile row, block) in all
+  int64_t tile_rows;  // without row_offsets: tiles of a sequence
+};
+
+__device__ __forceinline__ unsigned long long chain_word(float a, float h) {
+  // a NaN leaves no finite state, whatever comes in
+  if (!(a <= 1.0f)) h = __builtin_nanf(""), a = 1.0f;
+  return (unsigned long long)(__float_as_uint(a) | 0x80000000u) << 32 | __float_as_uint(h);
 }
 
-// Sequences of up to so many steps are walked by one workgroup each (and block of channels).
-constexpr int kTileWaves = 4;
-constexpr int kTileRows = kTileWaves * kWaveRows;
+// The state in front of the tile at `position` > 0 of its chain (in the direction of travel), whose words lie `step` behind
+// those of the one before it.  The rows of words waited for belong to lower tickets, and every ticket's workgroup leaves
+// its row, whatever the offsets hold: they run, or have run, and none of them waits for this one, so every wait ends.  All
+// words are asked for at once.
+__device__ __forceinline__ float chain_state(const unsigned long long* word, int64_t step, int64_t position) {
+  const int before = (int)(position % kGroup);
+  const int n = before + (position > before ? 1 : 0);
+  unsigned long long v[kGroup];
+  for (;;) {
+    unsigned long long all = ~0ull;
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i)
+      v[i] = __hip_atomic_load(word - (n - (i < n ? i : n - 1)) * step, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) all &= v[i];
+    if (all >> 63) break;
+    __builtin_amdgcn_s_sleep(1);
+  }
+  float state = 0.0f;  // the first word is a state
+#pragma unroll
+  for (int i = 0; i < kGroup; ++i)
+    if (i < n) state = fmaf(__uint_as_float((uint32_t)(v[i] >> 32) & 0x7fffffffu), state, __uint_as_float((uint32_t)v[i]));
+  return state;
+}
+
+// Tile `ticket`.  Equal sequences: all first tiles, then all second ones.  With offsets: tile row
+// begin / ROWS + sequence + index, as for the kept states; rows of that numbering between two sequences stay empty.
+template <int ROWS, int BLOCK, bool REVERSE>
+__device__ __forceinline__ Place tile_of(const ScanArgs& a, const Chain& chain, uint32_t ticket) {
+  const uint32_t blocks = (uint32_t)((a.channels + BLOCK - 1) / BLOCK);
+  uint32_t row = ticket / blocks;
+  Place p;
+  p.block = (int32_t)(ticket - row * blocks);
+  int64_t begin, length, index, count;
+  if (!a.row_offsets) {
+    const uint32_t sequences = (uint32_t)a.sequences;
+    p.position = row / sequences;
+    p.sequence = row - (uint32_t)p.position * sequences;
+    sequence_rows(a, p.sequence, begin, length);
+    count = chain.tile_rows;
+    index = REVERSE ? count - 1 - p.position : p.position;
+    p.word_row = p.sequence * count + index;
+    p.there = 1;
+  } else {
+    if (REVERSE) row = chain.tickets / blocks - 1 - row;
+    // the last sequence whose first tile row is not behind this one
+    const int lane = threadIdx.x & 63;
+    int64_t lo = 0, hi = a.sequences;
+    while (hi - lo > 1) {
+      const int64_t stride = (hi - lo + 63) / 64;
+      const int64_t at = lo + lane * stride;
+      if (at < hi) sequence_rows(a, at, begin, length);
+      const bool before = at < hi && begin / ROWS + at <= row;
+      const int passed = __popcll(__ballot(before));
+      const int64_t next = lo + passed * stride;
+      if (passed) {
+        lo = next - stride;
+        hi = next < hi ? next : hi;
+      } else {
+        hi = lo + 1;
+      }
+    }
+    p.sequence = __builtin_amdgcn_readfirstlane((int)lo);
+    sequence_rows(a, p.sequence, begin, length);
+    count = length > 0 ? (length + ROWS - 1) / ROWS : 1;
+    index = (int64_t)row - (begin / ROWS + p.sequence);
+    p.position = REVERSE ? count - 1 - index : index;
+    p.word_row = row;
+    p.there = index >= 0 && index < count;
+  }
+  p.row = begin + index * ROWS;
+  p.left = length - index * ROWS;
+  p.state = state_row(p.sequence, begin, index * (ROWS / kStateRows));
+  p.last = p.position + 1 == count;
+  return p;
+}
+
+// The next tile that is there; `there` is zero behind the last one.  A tile row that belongs to no sequence leaves words
+// all the same: with offsets that do not ascend, some tile may look for them.
+template <int ROWS, int BLOCK, bool REVERSE>
+__device__ __forceinline__ Place next_tile(const ScanArgs& a, const Chain& chain, int lane) {
+  for (;;) {
+    uint32_t ticket = 0;
+    if (lane == 0) ticket = atomicAdd(chain.ticket, 1u);
+    ticket = __builtin_amdgcn_readfirstlane(ticket);
+    if (ticket >= chain.tickets) return Place{};
+    const Place p = tile_of<ROWS, BLOCK, REVERSE>(a, chain, ticket);
+    if (p.there) return p;
+    for (int64_t channel = (int64_t)p.block * BLOCK + lane; channel < (int64_t)(p.block + 1) * BLOCK && channel < a.channels; channel += 64)
+      __hip_atomic_store(chain.words + p.word_row * a.channels + channel, chain_word(1.0f, 0.0f), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+}
+
+// A barrier for what lies in LDS: loads that are on their way stay on their way.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// W wavefronts work on tiles; those behind them, one to 64 channels, see to the chain: the first of them takes tickets, all
+// leave words, and wait for those of other tiles.
+template <typename TILE, int W, int RESIDENT>
+__global__ __launch_bounds__(W * 64 + TILE::kBlock, RESIDENT) void scan_chain_kernel(ScanArgs a, Chain chain) {
+  using SHAPE = typename TILE::SHAPE;
+  constexpr int VEC = SHAPE::kVec, kBlock = SHAPE::kBlock, kRows = W * SHAPE::kRows;
+  __shared__ typename TILE::Parts parts[2];
+  __shared__ Place places[2];
+  __shared__ float carry[kBlock];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (w >= W) {
+    if (w == W) {
+      const Place p = next_tile<kRows, kBlock, TILE::kReverse>(a, chain, lane);
+      if (lane == 0) places[0] = p;
+    }
+    lds_barrier();
+    for (int turn = 0;; turn ^= 1) {
+      const Place p = uniform(places[turn]);
+      if (!p.there) return;
+      if (w == W) {
+        const Place next = next_tile<kRows, kBlock, TILE::kReverse>(a, chain, lane);
+        if (lane == 0) places[turn ^ 1] = next;
+      }
+      lds_barrier();
+      const int mine = (w - W) * 64 + lane;
+      const int64_t channel = (int64_t)p.block * kBlock + mine;
+      if (channel < a.channels) {
+        const bool closes = p.position == 0 || p.position % kGroup == kGroup - 1;
+        unsigned long long* word = chain.words + p.word_row * a.channels + channel;
+        float A = 1.0f, H = 0.0f;
+#pragma unroll
+        for (int v = 0; v < W; ++v) {
+          const float2 part = TILE::part(parts[turn], v, mine);
+          H = fmaf(part.x, H, part.y);
+          A *= part.x;
+        }
+        if (!closes) __hip_atomic_store(word, chain_word(A, H), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const int64_t carried = p.sequence * a.channels + channel;
+        float state;
+        if (p.position == 0)
+          state = a.first ? a.first[carried] : 0.0f;
+        else
+          state = chain_state(word, TILE::kReverse ? -a.channels : a.channels, p.position);
+        carry[mine] = state;
+        state = fmaf(A, state, H);
+        if (closes) __hip_atomic_store(word, chain_word(0.0f, state), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (p.last && a.last) a.last[carried] = state;
+      }
+      lds_barrier();
+    }
+  }
+  const int col = lane % SHAPE::kLanes * VEC;
+  lds_barrier();
+  for (int turn = 0;; turn ^= 1) {
+    const Place p = uniform(places[turn]);
+    if (!p.there) return;
+    const Share h = share_of<SHAPE>(a, p, w, lane);
+    typename TILE::Input in;
+    in.load(a, p, w, h);
+    TILE tile;
+    tile.fold(in, h, w, col, parts[turn]);
+    lds_barrier();
+    tile.between(parts[turn], w, col);
+    lds_barrier();
+    float state[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) state[j] = carry[col + j];
+    tile.apply(a, p, h, w, col, parts[turn], state);
+  }
+}
+
+// Sequences of more steps than a tile holds are cut into tiles.
+constexpr int kTileRows = 128;
 constexpr int kChainGroups = 4 * 256;
 
-template <typename T, int VEC>
-hipError_t launch_vec(const ScanArgs& a, void* workspace, bool free_input, bool backward, hipStream_t stream) {
-  const int64_t blocks = ceil_div(a.channels, kBlock);
-  Chain chain{};
+template <template <typename, int, bool> class TILE, typename SHAPE, bool FREE>
+hipError_t launch_tiles(const ScanArgs& a, void* workspace, hipStream_t stream) {
+  const int64_t blocks = ceil_div(a.channels, SHAPE::kBlock);
+  constexpr int kWaves = kTileRows / SHAPE::kRows;
   if (!scan_chained(a)) {
-    const uint32_t groups = (uint32_t)(a.sequences * blocks);
-    if (a.max_length <= 2 * kWaveRows) return launch_tiles<T, VEC, 2, false>(a, chain, groups, free_input, backward, stream);
-    return launch_tiles<T, VEC, kTileWaves, false>(a, chain, groups, free_input, backward, stream);
+    const dim3 groups((uint32_t)(a.sequences * blocks));
+    if (a.max_length <= kStateRows)
+      scan_walk_kernel<TILE<SHAPE, SHAPE::kStateWaves, FREE>, SHAPE::kStateWaves><<<groups, SHAPE::kStateWaves * 64, 0, stream>>>(a);
+    else
+      scan_walk_kernel<TILE<SHAPE, kWaves, FREE>, kWaves><<<groups, kWaves * 64, 0, stream>>>(a);
+    return hipGetLastError();
   }
+  Chain chain{};
   chain.ticket = static_cast<uint32_t*>(workspace);
   chain.words = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace) + 256);
   chain.tile_rows = ceil_div(a.max_length, kTileRows);
@@ -560,7 +680,17 @@ hipError_t launch_vec(const ScanArgs& a, void* workspace, bool free_input, bool 
   const hipError_t e = launch_clear_words(static_cast<uint32_t*>(workspace), scan_workspace_bytes(a) / 4, stream);
   if (e != hipSuccess) return e;
   const uint32_t groups = chain.tickets < (uint32_t)kChainGroups ? chain.tickets : (uint32_t)kChainGroups;
-  return launch_tiles<T, VEC, kTileWaves, true>(a, chain, groups, free_input, backward, stream);
+  using Kernel = TILE<SHAPE, kWaves, FREE>;
+  constexpr int kResident = Kernel::kReverse ? 3 : 4;
+  scan_chain_kernel<Kernel, kWaves, kResident><<<groups, kWaves * 64 + SHAPE::kBlock, 0, stream>>>(a, chain);
+  return hipGetLastError();
+}
+
+template <typename SHAPE>
+hipError_t launch_shape(const ScanArgs& a, void* workspace, bool free_input, bool backward, hipStream_t stream) {
+  if (backward)
+    return free_input ? launch_tiles<BackwardTile, SHAPE, true>(a, workspace, stream) : launch_tiles<BackwardTile, SHAPE, false>(a, workspace, stream);
+  return free_input ? launch_tiles<ForwardTile, SHAPE, true>(a, workspace, stream) : launch_tiles<ForwardTile, SHAPE, false>(a, workspace, stream);
 }
 
 // Channels to a lane: as many as all rows are aligned for, eight bytes of them at most.
@@ -571,9 +701,13 @@ hipError_t launch(const ScanArgs& a, void* workspace, bool free_input, bool back
     bits |= reinterpret_cast<uintptr_t>(p);
   for (int64_t stride : {a.gate_stride, a.x_stride, a.h_stride, a.dh_stride, a.dgate_stride, a.dx_stride})
     bits |= (uint64_t)stride * sizeof(T);
-  if (sizeof(T) == 2 && bits % 8 == 0) return launch_vec<T, sizeof(T) == 2 ? 4 : 2>(a, workspace, free_input, backward, stream);
-  if (bits % (2 * sizeof(T)) == 0) return launch_vec<T, 2>(a, workspace, free_input, backward, stream);
-  return launch_vec<T, 1>(a, workspace, free_input, backward, stream);
+  if constexpr (sizeof(T) == 2) {
+    if (bits % 8 == 0) return launch_shape<Shape<T, 4, 2, 8>>(a, workspace, free_input, backward, stream);
+    if (bits % 4 == 0) return launch_shape<Shape<T, 2, 1, 16>>(a, workspace, free_input, backward, stream);
+  } else {
+    if (bits % 8 == 0) return launch_shape<Shape<T, 2, 2, 8>>(a, workspace, free_input, backward, stream);
+  }
+  return launch_shape<Shape<T, 1, 1, 16>>(a, workspace, free_input, backward, stream);
 }
 
 }  // namespace
@@ -585,7 +719,7 @@ int64_t scan_word_rows(const ScanArgs& a) {
 bool scan_chained(const ScanArgs& a) { return a.max_length > kTileRows; }
 
 int64_t scan_workgroups(const ScanArgs& a) {
-  return (scan_chained(a) ? scan_word_rows(a) : a.sequences) * ceil_div(a.channels, kBlock);
+  return (scan_chained(a) ? scan_word_rows(a) : a.sequences) * ceil_div(a.channels, 64);
 }
 
 size_t scan_workspace_bytes(const ScanArgs& a) {
