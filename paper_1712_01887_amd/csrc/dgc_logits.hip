@@ -1,189 +1,588 @@
 // Operators on rows of logits: a teacher's largest ones as pairs, and the loss of a student against such pairs
 // with its gradient.
 
+#include "dgc_device.h"
 #include "dgc_operators.h"
 
 namespace dgc {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
 constexpr float kLog2E = 1.44269504088896341f;
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kInf = __builtin_inff();
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Sum or maximum over the wavefront, the same in every lane.
 __device__ __forceinline__ float wave_sum_f(float x) {
+#pragma unroll
   for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
   return x;
 }
 __device__ __forceinline__ float wave_max_f(float x) {
+#pragma unroll
   for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
   return x;
 }
 
-// The workgroup's sum or maximum, the same in every thread.  `words`: kWaves floats of LDS.
-__device__ __forceinline__ float block_sum(float x, float* words) {
-  x = wave_sum_f(x);
-  __syncthreads();
-  if (threadIdx.x % 64 == 0) words[threadIdx.x / 64] = x;
-  __syncthreads();
-  float s = 0.0f;
-  for (int i = 0; i < kWaves; ++i) s += words[i];
-  return s;
-}
-__device__ __forceinline__ float block_max(float x, float* words) {
-  x = wave_max_f(x);
-  __syncthreads();
-  if (threadIdx.x % 64 == 0) words[threadIdx.x / 64] = x;
-  __syncthreads();
-  float m = words[0];
-  for (int i = 1; i < kWaves; ++i) m = fmaxf(m, words[i]);
-  return m;
-}
+// ---- a row ------------------------------------------------------------------------------------------------
+// A workgroup of NT threads takes a row in vectors of 16 bytes, vector v by thread v mod NT: CH of them to a thread, which
+// keeps them in registers from the row's only read on, or, with CH = 0 (rows longer than the registers hold), reads them
+// again in every pass.  The few elements behind the last whole vector go to one thread each.  Places behind the row's end
+// hold -inf.
+template <typename T, int NT, int CH>
+struct Row {
+  static constexpr int E = 16 / (int)sizeof(T);
+  using Vector = Pack<T, E>;
+  struct __attribute__((packed, aligned(sizeof(T)))) Loose {  // a row starts where any element may
+    Vector v;
+  };
+  Vector held[CH > 0 ? CH : 1];
+  float rest;
 
+  static __device__ __forceinline__ Vector nothing() {
+    constexpr uint32_t word = sizeof(T) == 4 ? 0xff800000u : __is_same(T, __bf16) ? 0xff80ff80u : 0xfc00fc00u;
+    Vector p;
+#pragma unroll
+    for (int i = 0; i < Vector::kWords; ++i) p.w[i] = word;
+    return p;
+  }
+  static __device__ __forceinline__ Vector load(const T* z, int v) { return reinterpret_cast<const Loose*>(z + (uint32_t)v * (uint32_t)E)->v; }
+  // Vector i of this thread: the loads of all of them are under way before the first is looked at.
+  __device__ __forceinline__ void read(const T* z, int vocab, int i) {
+    const int whole = vocab / E, v = i * NT + (int)threadIdx.x;
+    if (whole > 0) held[i] = load(z, v < whole ? v : whole - 1);
+  }
+  __device__ __forceinline__ void read_rest(const T* z, int vocab) {
+    const int at = vocab / E * E + (int)threadIdx.x;
+    rest = at < vocab ? to_float(z[at]) : -kInf;
+  }
+  __device__ __forceinline__ void read(const T* z, int vocab) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) read(z, vocab, i);
+    read_rest(z, vocab);
+  }
+  // Before a row that was read is used: its end.
+  __device__ __forceinline__ void cut(int vocab) {
+    const int whole = vocab / E;
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+      if ((i + 1) * NT > whole) {
+        const Vector none = nothing();
+#pragma unroll
+        for (int j = 0; j < Vector::kWords; ++j) held[i].w[j] = i * NT + (int)threadIdx.x < whole ? held[i].w[j] : none.w[j];
+      }
+  }
+  // Between two passes: what the first has made of the elements is not kept, it would take several times the registers.
+  __device__ __forceinline__ void renew() {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) held[i].renew();
+  }
+  // f(vector, its number) for every vector of this thread
+  template <typename F>
+  __device__ __forceinline__ void each(const T* z, int vocab, F f) const {
+    if constexpr (CH > 0) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i) f(held[i], i * NT + (int)threadIdx.x);
+    } else {
+      const int whole = vocab / E;
+#pragma unroll 4
+      for (int v = threadIdx.x; v < whole; v += NT) f(load(z, v), v);
+    }
+  }
+  __device__ __forceinline__ float largest(const T* z, int vocab) const {
+    float m = rest;
+    each(z, vocab, [&](const Vector& p, int) {
+#pragma unroll
+      for (int j = 0; j < E; ++j) m = fmaxf(m, p.get(j));
+    });
+    return m;
+  }
+};
+
+// What the wavefronts of a workgroup leave for each other.
+template <int NT>
+struct Between {
+  float largest[NT / 64];
+  float2 sums[NT / 64];
+  __device__ __forceinline__ float max_of() const {
+    float m = largest[0];
+#pragma unroll
+    for (int i = 1; i < NT / 64; ++i) m = fmaxf(m, largest[i]);
+    return m;
+  }
+  __device__ __forceinline__ float2 sum_of() const {
+    float2 s = sums[0];
+#pragma unroll
+    for (int i = 1; i < NT / 64; ++i) s.x += sums[i].x, s.y += sums[i].y;
+    return s;
+  }
+};
+
+// ---- top logits ---------------------------------------------------------------------------------------------
 // A whole number that orders as the logits do, zero for those that are never chosen (NaN, -inf); both zeros are one.
 __device__ __forceinline__ uint32_t order_key(float z) {
   if (!(z > -kInf)) return 0u;
   const uint32_t b = __float_as_uint(z + 0.0f);
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ float key_value(uint32_t key) {
+  return __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key);
+}
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void top_logits_kernel(TopArgs a) {
-  __shared__ unsigned long long best[kWaves];
-  __shared__ float words[kWaves];
-  const int64_t r = blockIdx.x;
-  const T* z = static_cast<const T*>(a.logits) + r * a.row_stride;
-  unsigned long long last = ~0ull;  // the pair chosen before: value, then index from the highest
-  for (int p = 0; p < a.k; ++p) {
-    unsigned long long mine = 0;
-    if (last != 0)
-      for (int j = threadIdx.x; j < a.vocab; j += kThreads) {
-        const uint32_t key = order_key(to_float(z[j]));
-        const unsigned long long word = key ? (unsigned long long)key << 32 | (uint32_t)~j : 0ull;
-        if (word < last && word > mine) mine = word;
+template <int NT>
+struct TopShared {
+  static constexpr int kCandidates = NT < 256 ? 512 : 1024, kVectors = NT < 256 ? NT : 1024;
+  Between<NT> between;
+  uint4 vectors[kVectors];                     // those with an element that reaches the floor
+  int32_t numbers[kVectors];
+  unsigned long long candidates[kCandidates];  // key, then index from the highest
+  uint32_t rank[kCandidates];
+  uint32_t keys[NT];                           // the threads' largest
+  uint32_t histogram[256];
+  uint32_t totals[NT / 64];
+  uint32_t floor, count, hits, prefix, wanted;
+};
+
+// A key that at least k of the `n` keys in LDS reach, its low 16 bits zero; 1 if fewer than k are not zero.  One wavefront.
+template <int N>
+__device__ __forceinline__ uint32_t floor_of(const uint32_t* keys, int k, int lane) {
+  constexpr int kEach = (N + 63) / 64;
+  uint32_t mine[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) mine[i] = i * 64 + lane < N ? keys[i * 64 + lane] : 0u;
+  uint32_t found = 0;
+  for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
+    const uint32_t probe = found | bit;
+    int passed = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) passed += __popcll(__ballot(mine[i] >= probe));
+    if (passed >= k) found = probe;
+  }
+  return found ? found : 1u;
+}
+
+// The exact way, for rows in which too many logits reach the floor (ties above all): the k-th largest key by its bytes from
+// the highest, then all logits above it and the first few, by index, of those that equal it.  The row is read again in every
+// pass.
+template <typename T, int NT>
+__device__ __forceinline__ void select_exactly(const T* z, int vocab, int k, TopShared<NT>& s) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  uint32_t prefix = 0, wanted = (uint32_t)k;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    for (int i = threadIdx.x; i < 256; i += NT) s.histogram[i] = 0;
+    __syncthreads();
+    for (int first = 0; first < vocab; first += NT) {
+      const int j = first + (int)threadIdx.x;
+      const uint32_t key = j < vocab ? order_key(to_float(z[j])) : 0u;
+      const bool counts = key != 0 && (shift == 24 || key >> (shift + 8) == prefix);
+      const uint32_t bin = (key >> shift) & 255u;
+      const unsigned long long all = __ballot(counts);
+      if (all) {  // the bin that one of the lanes names, once for all that name it
+        const int leader = __ffsll(all) - 1;
+        const uint32_t one = __builtin_amdgcn_readlane(bin, leader);
+        const unsigned long long same = __ballot(counts && bin == one);
+        if (lane == leader) atomicAdd(&s.histogram[one], (uint32_t)__popcll(same));
+        if (counts && bin != one) atomicAdd(&s.histogram[bin], 1u);
       }
-    for (int o = 32; o > 0; o >>= 1) {
-      const unsigned long long other = __shfl_xor(mine, o);
-      if (other > mine) mine = other;
     }
     __syncthreads();
-    if (threadIdx.x % 64 == 0) best[threadIdx.x / 64] = mine;
-    __syncthreads();
-    last = best[0];
-    for (int i = 1; i < kWaves; ++i) last = best[i] > last ? best[i] : last;
-    if (threadIdx.x == 0) {
-      const int j = (int)~(uint32_t)last;
-      a.out_idx[r * a.k + p] = last ? j : -1;
-      a.out_val[r * a.k + p] = last ? to_float(z[j]) : -kInf;
+    if (w == 0) {  // lane l: bins 255 - 4 l and the three below
+      uint32_t c[4], sum = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[i] = s.histogram[255 - 4 * lane - i], sum += c[i];
+      uint32_t above = wave_inclusive_sum(sum) - sum;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (above < wanted && above + c[i] >= wanted) s.prefix = prefix << 8 | (uint32_t)(255 - 4 * lane - i), s.wanted = wanted - above;
+        above += c[i];
+      }
     }
+    __syncthreads();
+    prefix = s.prefix;
+    wanted = s.wanted;
   }
-  if (!a.out_lse) return;
-  float m = -kInf;
-  for (int j = threadIdx.x; j < a.vocab; j += kThreads) m = fmaxf(m, to_float(z[j]));
-  m = block_max(m, words);
-  const float shift = m == -kInf ? 0.0f : m;
-  float sum = 0.0f;
-  const float c = a.inv_temperature * kLog2E;
-  for (int j = threadIdx.x; j < a.vocab; j += kThreads) sum += exp2_fast((to_float(z[j]) - shift) * c);
-  sum = block_sum(sum, words);
-  if (threadIdx.x == 0) a.out_lse[r] = shift * a.inv_temperature + kLn2 * __log2f(sum);
+  if (threadIdx.x == 0) s.count = 0;
+  __syncthreads();
+  uint32_t seen = 0;  // equal ones before this turn, in ascending order
+  for (int first = 0; first < vocab; first += NT) {
+    const int j = first + (int)threadIdx.x;
+    const uint32_t key = j < vocab ? order_key(to_float(z[j])) : 0u;
+    const unsigned long long equal = __ballot(key == prefix);
+    bool taken = key > prefix;
+    if (seen < wanted) {
+      if (lane == 0) s.totals[w] = (uint32_t)__popcll(equal);
+      __syncthreads();
+      uint32_t at = seen + (uint32_t)__popcll(equal & ((1ull << lane) - 1));
+      for (int i = 0; i < NT / 64; ++i) {
+        if (i < w) at += s.totals[i];
+        seen += s.totals[i];
+      }
+      taken |= key == prefix && at < wanted;
+      __syncthreads();
+    }
+    if (taken) s.candidates[atomicAdd(&s.count, 1u)] = (unsigned long long)key << 32 | (uint32_t)~j;
+  }
+  __syncthreads();
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a) {
-  __shared__ float words[kWaves];
-  __shared__ int taken;
-  const int64_t r = blockIdx.x;
-  const T* z = static_cast<const T*>(a.logits) + r * a.row_stride;
-  T* grad = a.grad ? static_cast<T*>(a.grad) + r * a.grad_stride : nullptr;
-  const float w = a.row_weight ? a.row_weight[r] : 1.0f;
-  int y = a.labels ? a.labels[r] : -1;
-  int at = threadIdx.x < a.k ? a.top_idx[r * a.k + threadIdx.x] : -1;
-  if ((y >= a.vocab || at >= a.vocab) && a.diag_flags) atomicOr(a.diag_flags, (uint32_t)DGC_DIAG_BAD_INDEX);
-  if (y >= a.vocab) y = -1;
-  if (at >= a.vocab) at = -1;
-  float m = -kInf;
-  if (w != 0.0f)
-    for (int j = threadIdx.x; j < a.vocab; j += kThreads) m = fmaxf(m, to_float(z[j]));
-  m = block_max(m, words);
-  const float shift = m == -kInf ? 0.0f : m;
-  const float tau = a.temperature, inv_tau = 1.0f / tau, c = inv_tau * kLog2E;
-  const bool second = y >= 0 && tau != 1.0f;
-  float sum = 0.0f, sum1 = 0.0f;
-  if (w != 0.0f)
-    for (int j = threadIdx.x; j < a.vocab; j += kThreads) {
-      const float zj = to_float(z[j]) - shift;
-      sum += exp2_fast(zj * c);
-      if (second) sum1 += exp2_fast(zj * kLog2E);
+// A floor that at least k logits reach is the k-th largest of the threads' largest; hardly more reach it, unless ties or
+// neighbours crowd there.  Those are listed in LDS and ranked by counting.
+template <typename T, int NT, int CH>
+__global__ __launch_bounds__(NT) void top_logits_kernel(TopArgs a) {
+  constexpr int E = Row<T, NT, CH>::E;
+  constexpr uint32_t kCandidates = TopShared<NT>::kCandidates, kVectors = TopShared<NT>::kVectors;
+  __shared__ TopShared<NT> s;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  Row<T, NT, CH> row;
+  int64_t r = blockIdx.x;
+  row.read(static_cast<const T*>(a.logits) + r * a.row_stride, a.vocab);
+  for (;;) {
+    asm volatile("" : "+s"(a.vocab));  // places of vectors are counted anew for every row, not kept in registers
+    const T* z = static_cast<const T*>(a.logits) + r * a.row_stride;
+    row.cut(a.vocab);
+    const float mine = row.largest(z, a.vocab);
+    row.renew();
+    s.keys[threadIdx.x] = order_key(mine);
+    const float wave = wave_max_f(mine);
+    if (lane == 0) s.between.largest[w] = wave;
+    if (threadIdx.x == 0) s.count = s.hits = 0;
+    __syncthreads();
+    if (w == 0) {
+      const uint32_t floor = floor_of<NT>(s.keys, a.k, lane);
+      if (lane == 0) s.floor = floor;
     }
-  sum = block_sum(sum, words);
-  sum1 = second ? block_sum(sum1, words) : sum;
-  if (w == 0.0f || sum == 0.0f) {
-    if (a.loss && threadIdx.x == 0) a.loss[r] = 0.0f;
-    if (grad)
-      for (int j = threadIdx.x; j < a.vocab; j += kThreads) grad[j] = from_float<T>(0.0f);
-    return;
+    float2 sums{0.0f, 0.0f};
+    const float m = s.between.max_of(), shift = m == -kInf ? 0.0f : m;
+    if (a.out_lse) {
+      const float c = a.inv_temperature * kLog2E;
+      row.each(z, a.vocab, [&](const Pack<T, E>& p, int) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) sums.x += exp2_fast((p.get(j) - shift) * c);
+      });
+      sums.x = wave_sum_f(sums.x + exp2_fast((row.rest - shift) * c));
+      if (lane == 0) s.between.sums[w] = sums;
+      row.renew();
+    }
+    __syncthreads();
+    const uint32_t floor = s.floor;
+    const float least = floor > 1u ? key_value(floor) : -3.402823466e38f;  // whatever can be chosen
+    auto list = [&](float value, int j) {
+      const uint32_t at = atomicAdd(&s.count, 1u);
+      if (at < kCandidates) s.candidates[at] = (unsigned long long)order_key(value) << 32 | (uint32_t)~j;
+    };
+    row.each(z, a.vocab, [&](const Pack<T, E>& p, int v) {
+      float m = p.get(0);
+#pragma unroll
+      for (int j = 1; j < E; ++j) m = fmaxf(m, p.get(j));
+      if (m >= least) {
+        const uint32_t at = atomicAdd(&s.hits, 1u);
+        if (at < kVectors) s.vectors[at] = __builtin_bit_cast(uint4, p), s.numbers[at] = v;
+      }
+    });
+    if (row.rest >= least) list(row.rest, a.vocab / E * E + (int)threadIdx.x);
+    if (threadIdx.x == 0 && a.out_lse) a.out_lse[r] = shift * a.inv_temperature + kLn2 * __log2f(s.between.sum_of().x);
+    __syncthreads();
+    const uint32_t hits = s.hits;
+    for (uint32_t i = threadIdx.x; i < hits * E && hits <= kVectors; i += NT) {
+      const float value = to_float(reinterpret_cast<const T*>(s.vectors)[i]);
+      if (value >= least) list(value, s.numbers[i / E] * E + (int)(i % E));
+    }
+    __syncthreads();
+    uint32_t n = s.count;
+    if (hits > kVectors || n > kCandidates) {
+      __syncthreads();
+      select_exactly<T, NT>(z, a.vocab, a.k, s);
+      n = s.count;
+    }
+    const int64_t next = r + gridDim.x;
+    if (next < a.rows) row.read(static_cast<const T*>(a.logits) + next * a.row_stride, a.vocab);
+    // rank: 2^b >= n candidates, NT / 2^b threads to each
+    int b = 6;
+    while (b < 10 && (1u << b) < n) ++b;
+    for (uint32_t i = threadIdx.x; i < (1u << b) && i < kCandidates; i += NT) s.rank[i] = 0;
+    __syncthreads();
+    for (uint32_t t = threadIdx.x; t < (1u << b) || t < NT; t += NT) {
+      const uint32_t c = t & ((1u << b) - 1), part = t >> b, parts = (1u << b) >= NT ? 1u : NT >> b;
+      if (c < n) {
+        const unsigned long long key = s.candidates[c];
+        uint32_t better = 0;
+        for (uint32_t i = part; i < n; i += parts) better += s.candidates[i] > key;
+        if (better) atomicAdd(&s.rank[c], better);
+      }
+    }
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < n; c += NT) {
+      const uint32_t rank = s.rank[c];
+      if (rank < (uint32_t)a.k) {
+        a.out_idx[r * a.k + rank] = (int)~(uint32_t)s.candidates[c];
+        a.out_val[r * a.k + rank] = key_value((uint32_t)(s.candidates[c] >> 32));
+      }
+    }
+    for (int c = (int)n + (int)threadIdx.x; c < a.k; c += NT) {
+      a.out_idx[r * a.k + c] = -1;
+      a.out_val[r * a.k + c] = -kInf;
+    }
+    if (next >= a.rows) return;
+    r = next;
+    __syncthreads();
   }
-  // the pairs, one to a thread
-  const float t = at >= 0 ? a.top_val[r * a.k + threadIdx.x] * inv_tau : -kInf;
-  const float z_at = at >= 0 ? to_float(z[at]) - shift : 0.0f;
-  const float z_y = y >= 0 ? to_float(z[y]) - shift : 0.0f;
-  float log_p;
-  if (a.top_lse) {
-    log_p = t - a.top_lse[r];
-  } else {
-    float tm = block_max(t, words);
-    tm = tm == -kInf ? 0.0f : tm;
-    const float total = block_sum(at >= 0 ? __expf(t - tm) : 0.0f, words);
-    log_p = t - tm - (total > 0.0f ? __logf(total) : 0.0f);
-  }
-  const float p = at >= 0 ? __expf(log_p) : 0.0f;
-  const float mass = block_sum(p, words);
-  const float kl = block_sum(p != 0.0f ? p * (log_p - z_at * inv_tau + __logf(sum)) : 0.0f, words);
-  if (a.loss && threadIdx.x == 0)
-    a.loss[r] = w * ((1.0f - a.hard_weight) * tau * tau * kl + (y >= 0 ? a.hard_weight * (__logf(sum1) - z_y) : 0.0f));
-  if (!grad) return;
-  const float soft = w * (1.0f - a.hard_weight) * tau, hard = y >= 0 ? w * a.hard_weight : 0.0f;
-  const float cs = soft * mass / sum, ch = hard / sum1;
-  if (threadIdx.x == 0) taken = 0;
-  __syncthreads();
-  if (at >= 0 && at == y) taken = 1;
-  for (int j = threadIdx.x; j < a.vocab; j += kThreads) {
-    const float zj = to_float(z[j]) - shift;
-    float g = cs * exp2_fast(zj * c);
-    if (hard != 0.0f) g += ch * exp2_fast(zj * kLog2E);
-    grad[j] = from_float<T>(g);
-  }
-  __syncthreads();
-  // the few elements that a pair or the label names, once more
-  if (at >= 0) {
-    float g = cs * exp2_fast(z_at * c) - soft * p;
-    if (hard != 0.0f) g += ch * exp2_fast(z_at * kLog2E) - (at == y ? hard : 0.0f);
-    grad[at] = from_float<T>(g);
-  }
-  if (threadIdx.x == 0 && y >= 0 && !taken)
-    grad[y] = from_float<T>(cs * exp2_fast(z_y * c) + ch * exp2_fast(z_y * kLog2E) - hard);
 }
+
+// ---- distillation ---------------------------------------------------------------------------------------------
+constexpr int kPairs = DGC_TOP_MAX / 64;  // of a lane of the first wavefront
+
+template <int NT>
+struct DistillShared {
+  Between<NT> between;
+  float mass, kl;
+  int32_t at[DGC_TOP_MAX];  // the pairs' elements, what they hold, and the teacher's share
+  float z_at[DGC_TOP_MAX], p[DGC_TOP_MAX];
+};
+
+// The exponentials of an element at the temperature and without one: not needed or the same, the square of the first (a
+// temperature of two), or one of its own.
+enum { kOnce, kSquare, kTwice };
+template <int MODE>
+__device__ __forceinline__ float2 powers(float z, float c) {
+  const float e = exp2_fast(z * c);
+  return float2{e, MODE == kOnce ? 0.0f : MODE == kSquare ? e * e : exp2_fast(z * kLog2E)};
+}
+template <int MODE>
+struct Mode {
+  static constexpr int value = MODE;
+};
+template <typename F>
+__device__ __forceinline__ void in_mode(int mode, F f) {
+  if (mode == kOnce) f(Mode<kOnce>{});
+  else if (mode == kSquare) f(Mode<kSquare>{});
+  else f(Mode<kTwice>{});
+}
+
+template <typename T, int NT, int CH>
+__global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
+  constexpr int E = Row<T, NT, CH>::E;
+  __shared__ DistillShared<NT> s;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const float tau = a.temperature, inv_tau = 1.0f / tau, c = inv_tau * kLog2E;
+  Row<T, NT, CH> row;
+  int64_t r = blockIdx.x;
+  float weight = a.row_weight ? a.row_weight[r] : 1.0f;
+  if (weight != 0.0f) row.read(static_cast<const T*>(a.logits) + r * a.row_stride, a.vocab);
+  for (;;) {
+    asm volatile("" : "+s"(a.vocab));  // places of vectors are counted anew for every row, not kept in registers
+    const T* z = static_cast<const T*>(a.logits) + r * a.row_stride;
+    T* grad = a.grad ? static_cast<T*>(a.grad) + r * a.grad_stride : nullptr;
+    const int64_t next = r + gridDim.x;
+    const float next_weight = next < a.rows ? (a.row_weight ? a.row_weight[next] : 1.0f) : 0.0f;
+    int y = a.labels ? a.labels[r] : -1;
+    // the pairs, and the logits they and the label name: the first wavefront's
+    int at[kPairs];
+    float t[kPairs], z_at[kPairs], z_y = 0.0f;
+    bool named = false;  // the label is one of the pairs
+    if (w == 0) {
+      bool bad = y >= a.vocab;
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        const int p = i * 64 + lane;
+        at[i] = p < a.k ? a.top_idx[r * a.k + p] : -1;
+        bad |= at[i] >= a.vocab;
+        if (at[i] >= a.vocab) at[i] = -1;
+        t[i] = at[i] >= 0 ? a.top_val[r * a.k + p] * inv_tau : -kInf;
+        z_at[i] = at[i] >= 0 ? to_float(z[at[i]]) : 0.0f;
+        named |= at[i] >= 0 && at[i] == y;
+      }
+      if (bad && a.diag_flags) atomicOr(a.diag_flags, (uint32_t)DGC_DIAG_BAD_INDEX);
+      if (y >= 0 && y < a.vocab) z_y = to_float(z[y]);
+      named = __any(named);
+    }
+    if (y >= a.vocab) y = -1;
+    bool live = weight != 0.0f;
+    float shift = 0.0f, cs = 0.0f, ch = 0.0f, soft = 0.0f, hard = 0.0f;
+    const int mode = y < 0 || tau == 1.0f ? kOnce : tau == 2.0f ? kSquare : kTwice;
+    const bool second = mode != kOnce;
+    if (live) {
+      row.cut(a.vocab);
+      const float wave = wave_max_f(row.largest(z, a.vocab));
+      row.renew();
+      if (lane == 0) s.between.largest[w] = wave;
+      __syncthreads();
+      const float m = s.between.max_of();
+      shift = m == -kInf ? 0.0f : m;
+      float2 sums{0.0f, 0.0f};
+      auto add = [&](auto mode) {
+        auto one = [&](float zj) {
+          const float2 e = powers<decltype(mode)::value>(zj - shift, c);
+          sums.x += e.x;
+          if (decltype(mode)::value != kOnce) sums.y += e.y;
+        };
+        row.each(z, a.vocab, [&](const Pack<T, E>& v, int) {
+#pragma unroll
+          for (int j = 0; j < E; ++j) one(v.get(j));
+        });
+        one(row.rest);
+      };
+      in_mode(mode, add);
+      row.renew();
+      sums.x = wave_sum_f(sums.x);
+      if (second) sums.y = wave_sum_f(sums.y);
+      if (lane == 0) s.between.sums[w] = sums;
+      if (w == 0) {
+        float log_p[kPairs], from;
+        if (a.top_lse) {
+          from = a.top_lse[r];
+        } else {
+          float tm = t[0];
+#pragma unroll
+          for (int i = 1; i < kPairs; ++i) tm = fmaxf(tm, t[i]);
+          tm = wave_max_f(tm);
+          tm = tm == -kInf ? 0.0f : tm;
+          float total = 0.0f;
+#pragma unroll
+          for (int i = 0; i < kPairs; ++i) total += at[i] >= 0 ? __expf(t[i] - tm) : 0.0f;
+          total = wave_sum_f(total);
+          from = tm + (total > 0.0f ? __logf(total) : 0.0f);
+        }
+        float mass = 0.0f, kl = 0.0f;  // of the divergence, what does not need the row's sum
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+          log_p[i] = t[i] - from;
+          const float p = at[i] >= 0 ? __expf(log_p[i]) : 0.0f;
+          z_at[i] -= shift;
+          mass += p;
+          kl += p != 0.0f ? p * (log_p[i] - z_at[i] * inv_tau) : 0.0f;
+          s.at[i * 64 + lane] = at[i];
+          s.z_at[i * 64 + lane] = z_at[i];
+          s.p[i * 64 + lane] = p;
+        }
+        mass = wave_sum_f(mass);
+        kl = wave_sum_f(kl);
+        z_y -= shift;
+        if (lane == 0) s.mass = mass, s.kl = kl;
+      }
+      __syncthreads();
+      sums = s.between.sum_of();
+      const float mass = s.mass;
+      live = sums.x != 0.0f;  // zero: nothing but -inf
+      if (!second) sums.y = sums.x;
+      if (live) {
+        soft = weight * (1.0f - a.hard_weight) * tau;
+        hard = y >= 0 ? weight * a.hard_weight : 0.0f;
+        cs = soft * mass / sums.x;
+        ch = hard / sums.y;
+        if (a.loss && threadIdx.x == 0)
+          a.loss[r] = weight * ((1.0f - a.hard_weight) * tau * tau * (s.kl + mass * __logf(sums.x)) + (y >= 0 ? a.hard_weight * (__logf(sums.y) - z_y) : 0.0f));
+      }
+    }
+    if (!live && a.loss && threadIdx.x == 0) a.loss[r] = 0.0f;
+    if (!second) cs += ch;  // one exponential stands for both
+    const T* z_next = static_cast<const T*>(a.logits) + next * a.row_stride;
+    const int whole = a.vocab / E;
+    auto value = [&](auto mode, float zj) {
+      const float2 e = powers<decltype(mode)::value>(zj, c);
+      return decltype(mode)::value == kOnce ? cs * e.x : fmaf(ch, e.y, cs * e.x);
+    };
+    auto store = [&](const Pack<T, E>& out, int number) {
+      if (number < whole) reinterpret_cast<typename Row<T, NT, CH>::Loose*>(grad + (uint32_t)number * (uint32_t)E)->v = out;
+    };
+    const int behind = whole * E + (int)threadIdx.x;
+    // The next row comes in where this one goes out.
+    if (grad && live) {
+      in_mode(mode, [&](auto mode) {
+        auto put = [&](const Pack<T, E>& v, int number) {
+          float g[E];
+#pragma unroll
+          for (int j = 0; j < E; ++j) g[j] = value(mode, v.get(j) - shift);
+          Pack<T, E> out;
+          out.set(g);
+          store(out, number);
+        };
+        if constexpr (CH > 0) {
+#pragma unroll
+          for (int i = 0; i < CH; ++i) {
+            put(row.held[i], i * NT + (int)threadIdx.x);
+            if (next_weight != 0.0f) row.read(z_next, a.vocab, i);
+          }
+        } else {
+          row.each(z, a.vocab, put);
+        }
+        if (behind < a.vocab) grad[behind] = from_float<T>(value(mode, row.rest - shift));
+      });
+    } else {
+      if (grad) {
+        for (int v = threadIdx.x; v < whole; v += NT) store(Pack<T, E>{}, v);
+        if (behind < a.vocab) grad[behind] = from_float<T>(0.0f);
+      }
+      if (next_weight != 0.0f) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) row.read(z_next, a.vocab, i);
+      }
+    }
+    if (next_weight != 0.0f) row.read_rest(z_next, a.vocab);
+    if (grad && live) {
+      __syncthreads();
+      if (w == 0)  // the few elements that a pair or the label names, once more
+        in_mode(mode, [&](auto mode) {
+          for (int i = lane; i < a.k; i += 64) {
+            const int j = s.at[i];
+            if (j >= 0) grad[j] = from_float<T>(value(mode, s.z_at[i]) - soft * s.p[i] - (j == y ? hard : 0.0f));
+          }
+          if (lane == 0 && y >= 0 && !named) grad[y] = from_float<T>(value(mode, z_y) - hard);
+        });
+    }
+    if (next >= a.rows) return;
+    r = next;
+    weight = next_weight;
+  }
+}
+
+// ---- launches ----------------------------------------------------------------------------------------------------
+// Workgroups that walk all rows, as many as the device holds at a time.
+template <typename T, int NT, int CH, typename ARGS>
+hipError_t launch_rows(const ARGS& a, void (*kernel)(ARGS), hipStream_t stream) {
+  int per_unit = 0;
+  const hipError_t e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_unit, kernel, NT, 0);
+  if (e != hipSuccess) return e;
+  const int64_t most = (int64_t)(per_unit < 1 ? 1 : per_unit) * compute_units();
+  kernel<<<dim3((unsigned)(a.rows < most ? a.rows : most)), NT, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, typename ARGS, typename PICK>
+hipError_t launch_vocab(const ARGS& a, PICK pick, hipStream_t stream) {
+  const int64_t vectors = ceil_div(a.vocab, 16 / (int64_t)sizeof(T));
+#define DGC_ROW(NT, CH) return launch_rows<T, NT, CH>(a, pick.template operator()<T, NT, CH>(), stream)
+  if (vectors <= 64) DGC_ROW(64, 1);
+  if (vectors <= 256) DGC_ROW(256, 1);
+  if (vectors <= 1024) DGC_ROW(256, 4);
+  if (vectors <= 4096) DGC_ROW(1024, 4);
+  if (vectors <= 8192) DGC_ROW(1024, 8);
+  if (vectors <= 16384) DGC_ROW(1024, 16);
+  DGC_ROW(1024, 0);
+#undef DGC_ROW
+}
+
+template <typename ARGS, typename PICK>
+hipError_t launch_type(const ARGS& a, int32_t dtype, PICK pick, hipStream_t stream) {
+  switch (dtype) {
+    case DGC_F32: return launch_vocab<float>(a, pick, stream);
+    case DGC_F16: return launch_vocab<_Float16>(a, pick, stream);
+    default: return launch_vocab<__bf16>(a, pick, stream);
+  }
+}
+
+struct PickTop {
+  template <typename T, int NT, int CH>
+  auto operator()() const { return &top_logits_kernel<T, NT, CH>; }
+};
+struct PickDistill {
+  template <typename T, int NT, int CH>
+  auto operator()() const { return &distill_kernel<T, NT, CH>; }
+};
 
 }  // namespace
 
-hipError_t launch_top_logits(const TopArgs& a, int32_t dtype, hipStream_t stream) {
-  const dim3 grid((unsigned)a.rows);
-  auto kernel = dtype == DGC_F32   ? top_logits_kernel<float>
-                : dtype == DGC_F16 ? top_logits_kernel<_Float16>
-                                   : top_logits_kernel<__bf16>;
-  kernel<<<grid, kThreads, 0, stream>>>(a);
-  return hipGetLastError();
-}
-
-hipError_t launch_distill(const DistillArgs& a, int32_t dtype, hipStream_t stream) {
-  const dim3 grid((unsigned)a.rows);
-  auto kernel = dtype == DGC_F32 ? distill_kernel<float> : dtype == DGC_F16 ? distill_kernel<_Float16> : distill_kernel<__bf16>;
-  kernel<<<grid, kThreads, 0, stream>>>(a);
-  return hipGetLastError();
-}
+hipError_t launch_top_logits(const TopArgs& a, int32_t dtype, hipStream_t stream) { return launch_type(a, dtype, PickTop{}, stream); }
+hipError_t launch_distill(const DistillArgs& a, int32_t dtype, hipStream_t stream) { return launch_type(a, dtype, PickDistill{}, stream); }
 
 }  // namespace dgc
