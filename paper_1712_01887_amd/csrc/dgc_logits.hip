@@ -11,6 +11,9 @@ constexpr float kLog2E = 1.44269504088896341f;
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kInf = __builtin_inff();
 
+// A value that is the same in every lane, in a register of the wavefront's.
+__device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Sum or maximum over the wavefront, the same in every lane.
@@ -48,18 +51,28 @@ struct Row {
     return p;
   }
   static __device__ __forceinline__ Vector load(const T* z, int v) { return reinterpret_cast<const Loose*>(z + (uint32_t)v * (uint32_t)E)->v; }
-  // Vector i of this thread: the loads of all of them are under way before the first is looked at.
-  __device__ __forceinline__ void read(const T* z, int vocab, int i) {
-    const int whole = vocab / E, v = i * NT + (int)threadIdx.x;
-    if (whole > 0) held[i] = load(z, v < whole ? v : whole - 1);
+  // The whole vectors of a row as a buffer resource (data format 32, offsets in bytes): behind its end nothing is read or
+  // stored, and so nowhere in the row of a null pointer.
+  static __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const T* z, int vocab) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)z, 0, z ? (int)((uint32_t)(vocab / E) * 16u) : 0, 0x00020000);
+  }
+  static __device__ __forceinline__ uint32_t offset(uint32_t thread, int i) { return (thread + (uint32_t)(i * NT)) * 16u; }
+  // Vector i of this thread.
+  __device__ __forceinline__ void read(__amdgpu_buffer_rsrc_t z, uint32_t thread, int i) {
+    held[i] = __builtin_bit_cast(Vector, __builtin_amdgcn_raw_buffer_load_b128(z, offset(thread, i), 0, 0));
+  }
+  static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t g, uint32_t thread, int i, const Vector& v) {
+    typedef uint32_t four __attribute__((ext_vector_type(4)));
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(four, v), g, offset(thread, i), 0, 0);
   }
   __device__ __forceinline__ void read_rest(const T* z, int vocab) {
     const int at = vocab / E * E + (int)threadIdx.x;
-    rest = at < vocab ? to_float(z[at]) : -kInf;
+    rest = z && at < vocab ? to_float(z[at]) : -kInf;
   }
   __device__ __forceinline__ void read(const T* z, int vocab) {
+    const __amdgpu_buffer_rsrc_t from = buffer(z, vocab);
 #pragma unroll
-    for (int i = 0; i < CH; ++i) read(z, vocab, i);
+    for (int i = 0; i < CH; ++i) read(from, threadIdx.x, i);
     read_rest(z, vocab);
   }
   // Before a row that was read is used: its end.
@@ -109,13 +122,13 @@ struct Between {
     float m = largest[0];
 #pragma unroll
     for (int i = 1; i < NT / 64; ++i) m = fmaxf(m, largest[i]);
-    return m;
+    return uniform(m);
   }
   __device__ __forceinline__ float2 sum_of() const {
     float2 s = sums[0];
 #pragma unroll
     for (int i = 1; i < NT / 64; ++i) s.x += sums[i].x, s.y += sums[i].y;
-    return s;
+    return float2{uniform(s.x), uniform(s.y)};
   }
 };
 
@@ -233,7 +246,7 @@ __global__ __launch_bounds__(NT) void top_logits_kernel(TopArgs a) {
   constexpr int E = Row<T, NT, CH>::E;
   constexpr uint32_t kCandidates = TopShared<NT>::kCandidates, kVectors = TopShared<NT>::kVectors;
   __shared__ TopShared<NT> s;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Row<T, NT, CH> row;
   int64_t r = blockIdx.x;
   row.read(static_cast<const T*>(a.logits) + r * a.row_stride, a.vocab);
@@ -265,7 +278,7 @@ __global__ __launch_bounds__(NT) void top_logits_kernel(TopArgs a) {
       row.renew();
     }
     __syncthreads();
-    const uint32_t floor = s.floor;
+    const uint32_t floor = __builtin_amdgcn_readfirstlane(s.floor);
     const float least = floor > 1u ? key_value(floor) : -3.402823466e38f;  // whatever can be chosen
     auto list = [&](float value, int j) {
       const uint32_t at = atomicAdd(&s.count, 1u);
@@ -283,17 +296,17 @@ __global__ __launch_bounds__(NT) void top_logits_kernel(TopArgs a) {
     if (row.rest >= least) list(row.rest, a.vocab / E * E + (int)threadIdx.x);
     if (threadIdx.x == 0 && a.out_lse) a.out_lse[r] = shift * a.inv_temperature + kLn2 * __log2f(s.between.sum_of().x);
     __syncthreads();
-    const uint32_t hits = s.hits;
+    const uint32_t hits = __builtin_amdgcn_readfirstlane(s.hits);
     for (uint32_t i = threadIdx.x; i < hits * E && hits <= kVectors; i += NT) {
       const float value = to_float(reinterpret_cast<const T*>(s.vectors)[i]);
       if (value >= least) list(value, s.numbers[i / E] * E + (int)(i % E));
     }
     __syncthreads();
-    uint32_t n = s.count;
+    uint32_t n = __builtin_amdgcn_readfirstlane(s.count);
     if (hits > kVectors || n > kCandidates) {
       __syncthreads();
       select_exactly<T, NT>(z, a.vocab, a.k, s);
-      n = s.count;
+      n = __builtin_amdgcn_readfirstlane(s.count);
     }
     const int64_t next = r + gridDim.x;
     if (next < a.rows) row.read(static_cast<const T*>(a.logits) + next * a.row_stride, a.vocab);
@@ -363,19 +376,19 @@ template <typename T, int NT, int CH>
 __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
   constexpr int E = Row<T, NT, CH>::E;
   __shared__ DistillShared<NT> s;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float tau = a.temperature, inv_tau = 1.0f / tau, c = inv_tau * kLog2E;
   Row<T, NT, CH> row;
   int64_t r = blockIdx.x;
-  float weight = a.row_weight ? a.row_weight[r] : 1.0f;
-  if (weight != 0.0f) row.read(static_cast<const T*>(a.logits) + r * a.row_stride, a.vocab);
+  float weight = a.row_weight ? uniform(a.row_weight[r]) : 1.0f;
+  row.read(weight != 0.0f ? static_cast<const T*>(a.logits) + r * a.row_stride : nullptr, a.vocab);
   for (;;) {
     asm volatile("" : "+s"(a.vocab));  // places of vectors are counted anew for every row, not kept in registers
     const T* z = static_cast<const T*>(a.logits) + r * a.row_stride;
     T* grad = a.grad ? static_cast<T*>(a.grad) + r * a.grad_stride : nullptr;
     const int64_t next = r + gridDim.x;
-    const float next_weight = next < a.rows ? (a.row_weight ? a.row_weight[next] : 1.0f) : 0.0f;
-    int y = a.labels ? a.labels[r] : -1;
+    const float next_weight = next < a.rows ? (a.row_weight ? uniform(a.row_weight[next]) : 1.0f) : 0.0f;
+    int y = a.labels ? __builtin_amdgcn_readfirstlane(a.labels[r]) : -1;
     // the pairs, and the logits they and the label name: the first wavefront's
     int at[kPairs];
     float t[kPairs], z_at[kPairs], z_y = 0.0f;
@@ -462,7 +475,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
       }
       __syncthreads();
       sums = s.between.sum_of();
-      const float mass = s.mass;
+      const float mass = uniform(s.mass);
       live = sums.x != 0.0f;  // zero: nothing but -inf
       if (!second) sums.y = sums.x;
       if (live) {
@@ -476,49 +489,50 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
     }
     if (!live && a.loss && threadIdx.x == 0) a.loss[r] = 0.0f;
     if (!second) cs += ch;  // one exponential stands for both
-    const T* z_next = static_cast<const T*>(a.logits) + next * a.row_stride;
-    const int whole = a.vocab / E;
+    const T* z_next = next_weight != 0.0f ? static_cast<const T*>(a.logits) + next * a.row_stride : nullptr;
+    const __amdgpu_buffer_rsrc_t from = Row<T, NT, CH>::buffer(z_next, a.vocab);
+    const int whole = a.vocab / E, behind = whole * E + (int)threadIdx.x;
+    uint32_t thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));  // offsets of vectors are counted anew for every row, not kept in registers
     auto value = [&](auto mode, float zj) {
       const float2 e = powers<decltype(mode)::value>(zj, c);
       return decltype(mode)::value == kOnce ? cs * e.x : fmaf(ch, e.y, cs * e.x);
     };
-    auto store = [&](const Pack<T, E>& out, int number) {
-      if (number < whole) reinterpret_cast<typename Row<T, NT, CH>::Loose*>(grad + (uint32_t)number * (uint32_t)E)->v = out;
-    };
-    const int behind = whole * E + (int)threadIdx.x;
     // The next row comes in where this one goes out.
     if (grad && live) {
       in_mode(mode, [&](auto mode) {
-        auto put = [&](const Pack<T, E>& v, int number) {
+        auto of = [&](const Pack<T, E>& v) {
           float g[E];
 #pragma unroll
           for (int j = 0; j < E; ++j) g[j] = value(mode, v.get(j) - shift);
           Pack<T, E> out;
           out.set(g);
-          store(out, number);
+          return out;
         };
         if constexpr (CH > 0) {
+          const __amdgpu_buffer_rsrc_t to = Row<T, NT, CH>::buffer(grad, a.vocab);
 #pragma unroll
           for (int i = 0; i < CH; ++i) {
-            put(row.held[i], i * NT + (int)threadIdx.x);
-            if (next_weight != 0.0f) row.read(z_next, a.vocab, i);
+            Row<T, NT, CH>::store(to, thread, i, of(row.held[i]));
+            row.read(from, thread, i);
           }
         } else {
-          row.each(z, a.vocab, put);
+          row.each(z, a.vocab, [&](const Pack<T, E>& v, int number) {
+            reinterpret_cast<typename Row<T, NT, CH>::Loose*>(grad + (uint32_t)number * (uint32_t)E)->v = of(v);
+          });
         }
         if (behind < a.vocab) grad[behind] = from_float<T>(value(mode, row.rest - shift));
       });
     } else {
       if (grad) {
-        for (int v = threadIdx.x; v < whole; v += NT) store(Pack<T, E>{}, v);
+        for (int v = threadIdx.x; v < whole; v += NT)
+          reinterpret_cast<typename Row<T, NT, CH>::Loose*>(grad + (uint32_t)v * (uint32_t)E)->v = Pack<T, E>{};
         if (behind < a.vocab) grad[behind] = from_float<T>(0.0f);
       }
-      if (next_weight != 0.0f) {
 #pragma unroll
-        for (int i = 0; i < CH; ++i) row.read(z_next, a.vocab, i);
-      }
+      for (int i = 0; i < CH; ++i) row.read(from, thread, i);
     }
-    if (next_weight != 0.0f) row.read_rest(z_next, a.vocab);
+    row.read_rest(z_next, a.vocab);
     if (grad && live) {
       __syncthreads();
       if (w == 0)  // the few elements that a pair or the label names, once more
