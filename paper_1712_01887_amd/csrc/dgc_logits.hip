@@ -361,18 +361,7 @@ __device__ __forceinline__ float2 powers(float z, float c) {
   const float e = exp2_fast(z * c);
   return float2{e, MODE == kOnce ? 0.0f : MODE == kSquare ? e * e : exp2_fast(z * kLog2E)};
 }
-template <int MODE>
-struct Mode {
-  static constexpr int value = MODE;
-};
-template <typename F>
-__device__ __forceinline__ void in_mode(int mode, F f) {
-  if (mode == kOnce) f(Mode<kOnce>{});
-  else if (mode == kSquare) f(Mode<kSquare>{});
-  else f(Mode<kTwice>{});
-}
-
-template <typename T, int NT, int CH>
+template <typename T, int NT, int CH, int MODE, bool GRAD>
 __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
   constexpr int E = Row<T, NT, CH>::E;
   __shared__ DistillShared<NT> s;
@@ -385,7 +374,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
   for (;;) {
     asm volatile("" : "+s"(a.vocab));  // places of vectors are counted anew for every row, not kept in registers
     const T* z = static_cast<const T*>(a.logits) + r * a.row_stride;
-    T* grad = a.grad ? static_cast<T*>(a.grad) + r * a.grad_stride : nullptr;
+    T* grad = GRAD ? static_cast<T*>(a.grad) + r * a.grad_stride : nullptr;
     const int64_t next = r + gridDim.x;
     const float next_weight = next < a.rows ? (a.row_weight ? uniform(a.row_weight[next]) : 1.0f) : 0.0f;
     int y = a.labels ? __builtin_amdgcn_readfirstlane(a.labels[r]) : -1;
@@ -412,8 +401,6 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
     if (y >= a.vocab) y = -1;
     bool live = weight != 0.0f;
     float shift = 0.0f, cs = 0.0f, ch = 0.0f, soft = 0.0f, hard = 0.0f;
-    const int mode = y < 0 || tau == 1.0f ? kOnce : tau == 2.0f ? kSquare : kTwice;
-    const bool second = mode != kOnce;
     if (live) {
       row.cut(a.vocab);
       const float wave = wave_max_f(row.largest(z, a.vocab));
@@ -423,22 +410,19 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
       const float m = s.between.max_of();
       shift = m == -kInf ? 0.0f : m;
       float2 sums{0.0f, 0.0f};
-      auto add = [&](auto mode) {
-        auto one = [&](float zj) {
-          const float2 e = powers<decltype(mode)::value>(zj - shift, c);
-          sums.x += e.x;
-          if (decltype(mode)::value != kOnce) sums.y += e.y;
-        };
-        row.each(z, a.vocab, [&](const Pack<T, E>& v, int) {
-#pragma unroll
-          for (int j = 0; j < E; ++j) one(v.get(j));
-        });
-        one(row.rest);
+      auto add = [&](float zj) {
+        const float2 e = powers<MODE>(zj - shift, c);
+        sums.x += e.x;
+        if (MODE != kOnce) sums.y += e.y;
       };
-      in_mode(mode, add);
+      row.each(z, a.vocab, [&](const Pack<T, E>& v, int) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) add(v.get(j));
+      });
+      add(row.rest);
       row.renew();
       sums.x = wave_sum_f(sums.x);
-      if (second) sums.y = wave_sum_f(sums.y);
+      if (MODE != kOnce) sums.y = wave_sum_f(sums.y);
       if (lane == 0) s.between.sums[w] = sums;
       if (w == 0) {
         float log_p[kPairs], from;
@@ -477,7 +461,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
       sums = s.between.sum_of();
       const float mass = uniform(s.mass);
       live = sums.x != 0.0f;  // zero: nothing but -inf
-      if (!second) sums.y = sums.x;
+      if (MODE == kOnce) sums.y = sums.x;
       if (live) {
         soft = weight * (1.0f - a.hard_weight) * tau;
         hard = y >= 0 ? weight * a.hard_weight : 0.0f;
@@ -488,61 +472,55 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
       }
     }
     if (!live && a.loss && threadIdx.x == 0) a.loss[r] = 0.0f;
-    if (!second) cs += ch;  // one exponential stands for both
+    if (MODE == kOnce) cs += ch;  // one exponential stands for both
     const T* z_next = next_weight != 0.0f ? static_cast<const T*>(a.logits) + next * a.row_stride : nullptr;
     const __amdgpu_buffer_rsrc_t from = Row<T, NT, CH>::buffer(z_next, a.vocab);
     const int whole = a.vocab / E, behind = whole * E + (int)threadIdx.x;
     uint32_t thread = threadIdx.x;
     asm volatile("" : "+v"(thread));  // offsets of vectors are counted anew for every row, not kept in registers
-    auto value = [&](auto mode, float zj) {
-      const float2 e = powers<decltype(mode)::value>(zj, c);
-      return decltype(mode)::value == kOnce ? cs * e.x : fmaf(ch, e.y, cs * e.x);
+    auto value = [&](float zj) {
+      const float2 e = powers<MODE>(zj, c);
+      return MODE == kOnce ? cs * e.x : fmaf(ch, e.y, cs * e.x);
     };
-    // The next row comes in where this one goes out.
-    if (grad && live) {
-      in_mode(mode, [&](auto mode) {
-        auto of = [&](const Pack<T, E>& v) {
-          float g[E];
+    if constexpr (GRAD) {
+      auto of = [&](const Pack<T, E>& v) {
+        float g[E];
 #pragma unroll
-          for (int j = 0; j < E; ++j) g[j] = value(mode, v.get(j) - shift);
-          Pack<T, E> out;
-          out.set(g);
-          return out;
-        };
-        if constexpr (CH > 0) {
-          const __amdgpu_buffer_rsrc_t to = Row<T, NT, CH>::buffer(grad, a.vocab);
+        for (int j = 0; j < E; ++j) g[j] = value(v.get(j) - shift);
+        Pack<T, E> out;
+        out.set(g);
+        return out;
+      };
+      if (!live)  // (what the sweep below forms of such a row is not stored)
+        for (int j = threadIdx.x; j < a.vocab; j += NT) grad[j] = from_float<T>(0.0f);
+      if constexpr (CH > 0) {  // the next row comes in where this one goes out
+        const __amdgpu_buffer_rsrc_t to = Row<T, NT, CH>::buffer(live ? grad : nullptr, a.vocab);
 #pragma unroll
-          for (int i = 0; i < CH; ++i) {
-            Row<T, NT, CH>::store(to, thread, i, of(row.held[i]));
-            row.read(from, thread, i);
-          }
-        } else {
-          row.each(z, a.vocab, [&](const Pack<T, E>& v, int number) {
-            reinterpret_cast<typename Row<T, NT, CH>::Loose*>(grad + (uint32_t)number * (uint32_t)E)->v = of(v);
-          });
+        for (int i = 0; i < CH; ++i) {
+          Row<T, NT, CH>::store(to, thread, i, of(row.held[i]));
+          row.read(from, thread, i);
+          __builtin_amdgcn_sched_barrier(1);  // no load before the registers it fills are free
         }
-        if (behind < a.vocab) grad[behind] = from_float<T>(value(mode, row.rest - shift));
-      });
-    } else {
-      if (grad) {
-        for (int v = threadIdx.x; v < whole; v += NT)
-          reinterpret_cast<typename Row<T, NT, CH>::Loose*>(grad + (uint32_t)v * (uint32_t)E)->v = Pack<T, E>{};
-        if (behind < a.vocab) grad[behind] = from_float<T>(0.0f);
+      } else if (live) {
+        row.each(z, a.vocab, [&](const Pack<T, E>& v, int number) {
+          reinterpret_cast<typename Row<T, NT, CH>::Loose*>(grad + (uint32_t)number * (uint32_t)E)->v = of(v);
+        });
       }
+      if (live && behind < a.vocab) grad[behind] = from_float<T>(value(row.rest - shift));
+    } else {
 #pragma unroll
       for (int i = 0; i < CH; ++i) row.read(from, thread, i);
     }
     row.read_rest(z_next, a.vocab);
-    if (grad && live) {
+    if (GRAD && live) {
       __syncthreads();
-      if (w == 0)  // the few elements that a pair or the label names, once more
-        in_mode(mode, [&](auto mode) {
-          for (int i = lane; i < a.k; i += 64) {
-            const int j = s.at[i];
-            if (j >= 0) grad[j] = from_float<T>(value(mode, s.z_at[i]) - soft * s.p[i] - (j == y ? hard : 0.0f));
-          }
-          if (lane == 0 && y >= 0 && !named) grad[y] = from_float<T>(value(mode, z_y) - hard);
-        });
+      if (w == 0) {  // the few elements that a pair or the label names, once more
+        for (int i = lane; i < a.k; i += 64) {
+          const int j = s.at[i];
+          if (j >= 0) grad[j] = from_float<T>(value(s.z_at[i]) - soft * s.p[i] - (j == y ? hard : 0.0f));
+        }
+        if (lane == 0 && y >= 0 && !named) grad[y] = from_float<T>(value(z_y) - hard);
+      }
     }
     if (next >= a.rows) return;
     r = next;
@@ -569,9 +547,9 @@ hipError_t launch_vocab(const ARGS& a, PICK pick, hipStream_t stream) {
   if (vectors <= 64) DGC_ROW(64, 1);
   if (vectors <= 256) DGC_ROW(256, 1);
   if (vectors <= 1024) DGC_ROW(256, 4);
-  if (vectors <= 4096) DGC_ROW(1024, 4);
-  if (vectors <= 8192) DGC_ROW(1024, 8);
-  if (vectors <= 16384) DGC_ROW(1024, 16);
+  if (vectors <= 4096) DGC_ROW(512, 8);
+  if (vectors <= 8192) DGC_ROW(512, 16);
+  if (vectors <= 16384) DGC_ROW(512, 32);
   DGC_ROW(1024, 0);
 #undef DGC_ROW
 }
@@ -589,14 +567,23 @@ struct PickTop {
   template <typename T, int NT, int CH>
   auto operator()() const { return &top_logits_kernel<T, NT, CH>; }
 };
+template <int MODE, bool GRAD>
 struct PickDistill {
   template <typename T, int NT, int CH>
-  auto operator()() const { return &distill_kernel<T, NT, CH>; }
+  auto operator()() const { return &distill_kernel<T, NT, CH, MODE, GRAD>; }
 };
+template <int MODE>
+hipError_t launch_mode(const DistillArgs& a, int32_t dtype, hipStream_t stream) {
+  return a.grad ? launch_type(a, dtype, PickDistill<MODE, true>{}, stream) : launch_type(a, dtype, PickDistill<MODE, false>{}, stream);
+}
 
 }  // namespace
 
 hipError_t launch_top_logits(const TopArgs& a, int32_t dtype, hipStream_t stream) { return launch_type(a, dtype, PickTop{}, stream); }
-hipError_t launch_distill(const DistillArgs& a, int32_t dtype, hipStream_t stream) { return launch_type(a, dtype, PickDistill{}, stream); }
+hipError_t launch_distill(const DistillArgs& a, int32_t dtype, hipStream_t stream) {
+  if (!a.labels || a.temperature == 1.0f) return launch_mode<kOnce>(a, dtype, stream);
+  if (a.temperature == 2.0f) return launch_mode<kSquare>(a, dtype, stream);
+  return launch_mode<kTwice>(a, dtype, stream);
+}
 
 }  // namespace dgc
