@@ -69,12 +69,20 @@ struct Row {
     const int at = vocab / E * E + (int)threadIdx.x;
     rest = z && at < vocab ? to_float(z[at]) : -kInf;
   }
-  __device__ __forceinline__ void read(const T* z, int vocab) {
-    const __amdgpu_buffer_rsrc_t from = buffer(z, vocab);
+  __device__ __forceinline__ void read(__amdgpu_buffer_rsrc_t from) {
 #pragma unroll
     for (int i = 0; i < CH; ++i) read(from, threadIdx.x, i);
+  }
+  __device__ __forceinline__ void read(const T* z, int vocab) {
+    read(buffer(z, vocab));
     read_rest(z, vocab);
   }
+  // Piece k of NT x CH vectors of a longer row.
+  __device__ __forceinline__ void read_piece(const T* z, int whole, int k) {
+    const int first = k * NT * CH;
+    read(buffer(z ? z + (int64_t)first * E : nullptr, (whole - first) * E));
+  }
+  __device__ __forceinline__ void cut_piece(int whole, int k) { cut((whole - k * NT * CH) * E); }
   // Before a row that was read is used: its end.
   __device__ __forceinline__ void cut(int vocab) {
     const int whole = vocab / E;
@@ -143,15 +151,17 @@ __device__ __forceinline__ float key_value(uint32_t key) {
   return __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key);
 }
 
+// LDS of a workgroup.  Two keys to a thread where there are few threads: with no more keys than k, the floor would be the
+// least of them.
 template <int NT>
 struct TopShared {
-  static constexpr int kCandidates = NT < 256 ? 512 : 1024, kVectors = NT < 256 ? NT : 1024;
-  Between<NT> between;
+  static constexpr int kCandidates = NT < 256 ? 512 : 1024, kVectors = NT < 256 ? 128 : 1024, kKeys = NT <= 256 ? 2 * NT : NT;
+  float2 sums[NT / 64];                        // largest and sum of the wavefronts
   uint4 vectors[kVectors];                     // those with an element that reaches the floor
   int32_t numbers[kVectors];
   unsigned long long candidates[kCandidates];  // key, then index from the highest
   uint32_t rank[kCandidates];
-  uint32_t keys[NT];                           // the threads' largest
+  uint32_t keys[kKeys];
   uint32_t histogram[256];
   uint32_t totals[NT / 64];
   uint32_t floor, count, hits, prefix, wanted;
@@ -173,6 +183,42 @@ __device__ __forceinline__ uint32_t floor_of(const uint32_t* keys, int k, int la
     if (passed >= k) found = probe;
   }
   return found ? found : 1u;
+}
+
+// The largest of four neighbouring lanes' values.
+__device__ __forceinline__ float quad_max(float x) {
+  x = fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0xb1, 0xf, 0xf, false)));  // quad_perm 1 0 3 2
+  return fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x4e, 0xf, 0xf, false)));  // 2 3 0 1
+}
+
+// Of the vectors listed, those that still reach the floor.
+template <typename T, int NT>
+__device__ __forceinline__ void thin_out(TopShared<NT>& s, uint32_t listed, float least) {
+  constexpr int kVectors = TopShared<NT>::kVectors, kEach = kVectors / NT > 0 ? kVectors / NT : 1, E = 16 / (int)sizeof(T);
+  uint4 mine[kEach];
+  int32_t number[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const uint32_t at = (uint32_t)(i * NT) + threadIdx.x;
+    if (at < listed) mine[i] = s.vectors[at], number[i] = s.numbers[at];
+  }
+  if (threadIdx.x == 0) s.hits = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    if ((uint32_t)(i * NT) + threadIdx.x < listed) {
+      const Pack<T, E> p = __builtin_bit_cast(Pack<T, E>, mine[i]);
+      float m = p.get(0);
+#pragma unroll
+      for (int j = 1; j < E; ++j) m = fmaxf(m, p.get(j));
+      if (m >= least) {
+        const uint32_t at = atomicAdd(&s.hits, 1u);
+        s.vectors[at] = mine[i];
+        s.numbers[at] = number[i];
+      }
+    }
+  }
+  __syncthreads();
 }
 
 // The exact way, for rows in which too many logits reach the floor (ties above all): the k-th largest key by its bytes from
@@ -240,66 +286,116 @@ __device__ __forceinline__ void select_exactly(const T* z, int vocab, int k, Top
 }
 
 // A floor that at least k logits reach is the k-th largest of the threads' largest; hardly more reach it, unless ties or
-// neighbours crowd there.  Those are listed in LDS and ranked by counting.
+// neighbours crowd there.  A row goes by in pieces of NT x CH vectors, the next one on its way while one is looked at: the
+// vectors that reach the floor of what has gone by are listed in LDS, in the end their elements that reach the last floor,
+// and these are ranked by counting.
 template <typename T, int NT, int CH>
 __global__ __launch_bounds__(NT) void top_logits_kernel(TopArgs a) {
-  constexpr int E = Row<T, NT, CH>::E;
+  using Piece = Row<T, NT, CH>;
+  constexpr int E = Piece::E;
   constexpr uint32_t kCandidates = TopShared<NT>::kCandidates, kVectors = TopShared<NT>::kVectors;
+  constexpr int kKeys = TopShared<NT>::kKeys;
   __shared__ TopShared<NT> s;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  Row<T, NT, CH> row;
+  const float c = a.inv_temperature * kLog2E;
+  const int whole = a.vocab / E, pieces = whole > 0 ? (whole + NT * CH - 1) / (NT * CH) : 1;
+  Piece piece;
   int64_t r = blockIdx.x;
-  row.read(static_cast<const T*>(a.logits) + r * a.row_stride, a.vocab);
+  const T* z = static_cast<const T*>(a.logits) + r * a.row_stride;
+  piece.read_piece(z, whole, 0);
+  piece.read_rest(z, a.vocab);
   for (;;) {
-    asm volatile("" : "+s"(a.vocab));  // places of vectors are counted anew for every row, not kept in registers
-    const T* z = static_cast<const T*>(a.logits) + r * a.row_stride;
-    row.cut(a.vocab);
-    const float mine = row.largest(z, a.vocab);
-    row.renew();
-    s.keys[threadIdx.x] = order_key(mine);
-    const float wave = wave_max_f(mine);
-    if (lane == 0) s.between.largest[w] = wave;
     if (threadIdx.x == 0) s.count = s.hits = 0;
-    __syncthreads();
-    if (w == 0) {
-      const uint32_t floor = floor_of<NT>(s.keys, a.k, lane);
-      if (lane == 0) s.floor = floor;
-    }
-    float2 sums{0.0f, 0.0f};
-    const float m = s.between.max_of(), shift = m == -kInf ? 0.0f : m;
-    if (a.out_lse) {
-      const float c = a.inv_temperature * kLog2E;
-      row.each(z, a.vocab, [&](const Pack<T, E>& p, int) {
+    const float rest = piece.rest;
+    const int64_t next = r + gridDim.x;
+    const T* z_next = next < a.rows ? static_cast<const T*>(a.logits) + next * a.row_stride : nullptr;
+    float largest[2] = {rest, -kInf};           // of even and odd vectors or halves of them
+    float m = -kInf, sum = 0.0f;                // of this thread: sum of exp((z - m) / T)
+    float least = 0.0f;
+    for (int k = 0; k < pieces; ++k) {
+      asm volatile("" : "+s"(a.vocab));
+      Piece now = piece;
+      now.cut_piece(whole, k);
+      const bool more = k + 1 < pieces;
+      piece.read_piece(more ? z : z_next, whole, more ? k + 1 : 0);
+      float top[CH];
 #pragma unroll
-        for (int j = 0; j < E; ++j) sums.x += exp2_fast((p.get(j) - shift) * c);
-      });
-      sums.x = wave_sum_f(sums.x + exp2_fast((row.rest - shift) * c));
-      if (lane == 0) s.between.sums[w] = sums;
-      row.renew();
+      for (int i = 0; i < CH; ++i) {
+        float low = now.held[i].get(0), high = now.held[i].get(E / 2);
+#pragma unroll
+        for (int j = 1; j < E / 2; ++j) low = fmaxf(low, now.held[i].get(j)), high = fmaxf(high, now.held[i].get(E / 2 + j));
+        largest[0] = fmaxf(largest[0], low);
+        largest[1] = fmaxf(largest[1], high);
+        top[i] = fmaxf(low, high);
+      }
+      const float seen = fmaxf(largest[0], largest[1]);
+      now.renew();
+      if (a.out_lse) {
+        const float shift = seen == -kInf ? 0.0f : seen;
+        sum *= exp2_fast((m - shift) * c);
+        m = seen;
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+          for (int j = 0; j < E; ++j) sum += exp2_fast((now.held[i].get(j) - shift) * c);
+        if (k == 0) sum += exp2_fast((rest - shift) * c);
+        now.renew();
+      }
+      if ((k & (k - 1)) == 0 || k + 1 == pieces) {  // the floor of what has gone by, when that has doubled
+        const bool few = a.k * 8 <= kKeys;            // a quarter of the keys do
+        float keyed[2] = {kKeys == NT ? seen : largest[0], largest[1]};
+        if (few) {
+#pragma unroll
+          for (int i = 0; i < kKeys / NT; ++i) keyed[i] = quad_max(keyed[i]);
+          if (lane % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < kKeys / NT; ++i) s.keys[(i * NT + (int)threadIdx.x) / 4] = order_key(keyed[i]);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kKeys / NT; ++i) s.keys[i * NT + threadIdx.x] = order_key(keyed[i]);
+        }
+        __syncthreads();
+        if (w == 0) {
+          const uint32_t floor = few ? floor_of<kKeys / 4>(s.keys, a.k, lane) : floor_of<kKeys>(s.keys, a.k, lane);
+          if (lane == 0) s.floor = floor;
+        }
+        const uint32_t listed = __builtin_amdgcn_readfirstlane(s.hits);
+        __syncthreads();
+        const uint32_t floor = __builtin_amdgcn_readfirstlane(s.floor);
+        least = floor > 1u ? key_value(floor) : -3.402823466e38f;  // whatever can be chosen
+        if (listed > kVectors / 2 && listed <= kVectors) thin_out<T, NT>(s, listed, least);
+      }
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+        if (top[i] >= least) {
+          const uint32_t at = atomicAdd(&s.hits, 1u);
+          if (at < kVectors) s.vectors[at] = __builtin_bit_cast(uint4, now.held[i]), s.numbers[at] = (k * CH + i) * NT + (int)threadIdx.x;
+        }
     }
-    __syncthreads();
-    const uint32_t floor = __builtin_amdgcn_readfirstlane(s.floor);
-    const float least = floor > 1u ? key_value(floor) : -3.402823466e38f;  // whatever can be chosen
+    piece.read_rest(z_next, a.vocab);
     auto list = [&](float value, int j) {
       const uint32_t at = atomicAdd(&s.count, 1u);
       if (at < kCandidates) s.candidates[at] = (unsigned long long)order_key(value) << 32 | (uint32_t)~j;
     };
-    row.each(z, a.vocab, [&](const Pack<T, E>& p, int v) {
-      float m = p.get(0);
-#pragma unroll
-      for (int j = 1; j < E; ++j) m = fmaxf(m, p.get(j));
-      if (m >= least) {
-        const uint32_t at = atomicAdd(&s.hits, 1u);
-        if (at < kVectors) s.vectors[at] = __builtin_bit_cast(uint4, p), s.numbers[at] = v;
-      }
-    });
-    if (row.rest >= least) list(row.rest, a.vocab / E * E + (int)threadIdx.x);
-    if (threadIdx.x == 0 && a.out_lse) a.out_lse[r] = shift * a.inv_temperature + kLn2 * __log2f(s.between.sum_of().x);
+    if (rest >= least) list(rest, whole * E + (int)threadIdx.x);
+    if (a.out_lse) {
+      const float all = wave_max_f(m);
+      const float total = wave_sum_f(sum * exp2_fast((m - (all == -kInf ? 0.0f : all)) * c));
+      if (lane == 0) s.sums[w] = float2{all, total};
+    }
     __syncthreads();
     const uint32_t hits = __builtin_amdgcn_readfirstlane(s.hits);
     for (uint32_t i = threadIdx.x; i < hits * E && hits <= kVectors; i += NT) {
       const float value = to_float(reinterpret_cast<const T*>(s.vectors)[i]);
       if (value >= least) list(value, s.numbers[i / E] * E + (int)(i % E));
+    }
+    if (a.out_lse && threadIdx.x == 0) {
+      float all = s.sums[0].x, total = 0.0f;
+      for (int i = 1; i < NT / 64; ++i) all = fmaxf(all, s.sums[i].x);
+      all = all == -kInf ? 0.0f : all;
+      for (int i = 0; i < NT / 64; ++i) total += s.sums[i].y * exp2_fast((s.sums[i].x - all) * c);
+      a.out_lse[r] = all * a.inv_temperature + kLn2 * __log2f(total);
     }
     __syncthreads();
     uint32_t n = __builtin_amdgcn_readfirstlane(s.count);
@@ -308,8 +404,6 @@ __global__ __launch_bounds__(NT) void top_logits_kernel(TopArgs a) {
       select_exactly<T, NT>(z, a.vocab, a.k, s);
       n = __builtin_amdgcn_readfirstlane(s.count);
     }
-    const int64_t next = r + gridDim.x;
-    if (next < a.rows) row.read(static_cast<const T*>(a.logits) + next * a.row_stride, a.vocab);
     // rank: 2^b >= n candidates, NT / 2^b threads to each
     int b = 6;
     while (b < 10 && (1u << b) < n) ++b;
@@ -336,8 +430,9 @@ __global__ __launch_bounds__(NT) void top_logits_kernel(TopArgs a) {
       a.out_idx[r * a.k + c] = -1;
       a.out_val[r * a.k + c] = -kInf;
     }
-    if (next >= a.rows) return;
+    if (!z_next) return;
     r = next;
+    z = z_next;
     __syncthreads();
   }
 }
@@ -540,46 +635,54 @@ hipError_t launch_rows(const ARGS& a, void (*kernel)(ARGS), hipStream_t stream) 
   return hipGetLastError();
 }
 
-template <typename T, typename ARGS, typename PICK>
-hipError_t launch_vocab(const ARGS& a, PICK pick, hipStream_t stream) {
-  const int64_t vectors = ceil_div(a.vocab, 16 / (int64_t)sizeof(T));
-#define DGC_ROW(NT, CH) return launch_rows<T, NT, CH>(a, pick.template operator()<T, NT, CH>(), stream)
-  if (vectors <= 64) DGC_ROW(64, 1);
-  if (vectors <= 256) DGC_ROW(256, 1);
-  if (vectors <= 1024) DGC_ROW(256, 4);
-  if (vectors <= 4096) DGC_ROW(512, 8);
-  if (vectors <= 8192) DGC_ROW(512, 16);
-  if (vectors <= 16384) DGC_ROW(512, 32);
-  DGC_ROW(1024, 0);
-#undef DGC_ROW
-}
-
-template <typename ARGS, typename PICK>
-hipError_t launch_type(const ARGS& a, int32_t dtype, PICK pick, hipStream_t stream) {
-  switch (dtype) {
-    case DGC_F32: return launch_vocab<float>(a, pick, stream);
-    case DGC_F16: return launch_vocab<_Float16>(a, pick, stream);
-    default: return launch_vocab<__bf16>(a, pick, stream);
-  }
-}
-
 struct PickTop {
-  template <typename T, int NT, int CH>
-  auto operator()() const { return &top_logits_kernel<T, NT, CH>; }
+  template <typename T, typename ARGS>
+  static hipError_t launch(const ARGS& a, hipStream_t stream) {
+    const int64_t vectors = ceil_div(a.vocab, 16 / (int64_t)sizeof(T));
+#define DGC_ROW(NT, CH) return launch_rows<T, NT, CH>(a, &top_logits_kernel<T, NT, CH>, stream)
+    if (vectors <= 64) DGC_ROW(64, 1);
+    if (vectors <= 256) DGC_ROW(256, 1);
+    if (vectors <= 1024) DGC_ROW(256, 4);
+    if (a.rows <= 2 * compute_units()) DGC_ROW(512, 8);  // few rows: what a row takes is what counts
+    DGC_ROW(256, 8);
+#undef DGC_ROW
+  }
 };
 template <int MODE, bool GRAD>
 struct PickDistill {
-  template <typename T, int NT, int CH>
-  auto operator()() const { return &distill_kernel<T, NT, CH, MODE, GRAD>; }
+  template <typename T, typename ARGS>
+  static hipError_t launch(const ARGS& a, hipStream_t stream) {
+    const int64_t vectors = ceil_div(a.vocab, 16 / (int64_t)sizeof(T));
+#define DGC_ROW(NT, CH) return launch_rows<T, NT, CH>(a, &distill_kernel<T, NT, CH, MODE, GRAD>, stream)
+    if (vectors <= 64) DGC_ROW(64, 1);
+    if (vectors <= 256) DGC_ROW(256, 1);
+    if (vectors <= 1024) DGC_ROW(256, 4);
+    if (vectors <= 3072) DGC_ROW(512, 6);
+    if (vectors <= 5120) DGC_ROW(512, 10);
+    if (vectors <= 7168) DGC_ROW(512, 14);
+    if (vectors <= 16384) DGC_ROW(1024, 16);
+    DGC_ROW(1024, 0);
+#undef DGC_ROW
+  }
 };
+
+template <typename PICK, typename ARGS>
+hipError_t launch_type(const ARGS& a, int32_t dtype, hipStream_t stream) {
+  switch (dtype) {
+    case DGC_F32: return PICK::template launch<float>(a, stream);
+    case DGC_F16: return PICK::template launch<_Float16>(a, stream);
+    default: return PICK::template launch<__bf16>(a, stream);
+  }
+}
+
 template <int MODE>
 hipError_t launch_mode(const DistillArgs& a, int32_t dtype, hipStream_t stream) {
-  return a.grad ? launch_type(a, dtype, PickDistill<MODE, true>{}, stream) : launch_type(a, dtype, PickDistill<MODE, false>{}, stream);
+  return a.grad ? launch_type<PickDistill<MODE, true>>(a, dtype, stream) : launch_type<PickDistill<MODE, false>>(a, dtype, stream);
 }
 
 }  // namespace
 
-hipError_t launch_top_logits(const TopArgs& a, int32_t dtype, hipStream_t stream) { return launch_type(a, dtype, PickTop{}, stream); }
+hipError_t launch_top_logits(const TopArgs& a, int32_t dtype, hipStream_t stream) { return launch_type<PickTop>(a, dtype, stream); }
 hipError_t launch_distill(const DistillArgs& a, int32_t dtype, hipStream_t stream) {
   if (!a.labels || a.temperature == 1.0f) return launch_mode<kOnce>(a, dtype, stream);
   if (a.temperature == 2.0f) return launch_mode<kSquare>(a, dtype, stream);
