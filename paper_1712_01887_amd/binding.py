@@ -454,48 +454,63 @@ def _dtype_code(dtype) -> int:
     return codes[dtype]
 
 
-def _rows_of(t, name: str, dtype, rows: int, columns: int, device) -> int:
-    """The row stride of a rows x columns tensor whose rows are contiguous."""
-    if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != columns or t.device != device:
-        raise DgcError(DGC_ERR_INVALID_ARG, f"{name}: {tuple(t.shape)} of {t.dtype} on {t.device} where "
-                                            f"({rows}, {columns}) of {dtype} on {device} is needed")
-    if columns > 1 and t.stride(1) != 1:
-        raise DgcError(DGC_ERR_INVALID_ARG, f"{name}: the elements of a row must be contiguous")
-    stride = t.stride(0) if rows > 1 else columns
-    if stride < columns:
-        raise DgcError(DGC_ERR_INVALID_ARG, f"{name}: rows overlap")
+# The checks below run before every launch of kernels that may take as little as four microseconds: one comparison of
+# shapes and few calls into torch (the text of a refusal is put together when there is one).
+def _refuse(t, name: str, what: str, dtype, shape, index: int):
+    raise DgcError(DGC_ERR_INVALID_ARG, f"{name}: {tuple(t.shape)} of {t.dtype} on {t.device} where {what} "
+                                        f"{tuple(shape)} of {dtype} on device {index} is needed")
+
+
+def _rows_of(t, name: str, dtype, shape, index: int) -> int:
+    """The row stride of a tensor of this shape whose rows are contiguous and do not overlap."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
+        _refuse(t, name, "rows", dtype, shape, index)
+    stride, step = t.stride()
+    rows, columns = shape
+    if rows <= 1:
+        stride = columns
+    if (step != 1 and columns > 1) or stride < columns:
+        raise DgcError(DGC_ERR_INVALID_ARG, f"{name}: strides {t.stride()} (the elements of a row must be contiguous, rows apart)")
     return stride
 
 
-def _dense(t, name: str, dtype, shape, device) -> int:
+def _dense(t, name: str, dtype, shape, index: int) -> int:
     """The address of a contiguous tensor of this type and shape; 0 for None."""
     if t is None:
         return 0
-    if t.dtype is not dtype or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
-        raise DgcError(DGC_ERR_INVALID_ARG, f"{name}: {tuple(t.shape)} of {t.dtype} on {t.device} where a contiguous "
-                                            f"{shape} of {dtype} on {device} is needed")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        _refuse(t, name, "a contiguous", dtype, shape, index)
     return t.data_ptr()
 
 
-class _Workspace:
-    """A device workspace of the caller's size, aligned as the library wants it, for one device's current stream."""
+class _Plan:
+    """What the plans below share: a device, and a workspace on it, aligned as the library wants it."""
 
-    def __init__(self, nbytes: int, device):
+    def _on(self, device) -> None:
         import torch
-        self.tensor = torch.empty(nbytes + 256, dtype=torch.uint8, device=device) if nbytes else None
-        self.ptr = (self.tensor.data_ptr() + 255) // 256 * 256 if nbytes else 0
-        self.nbytes = nbytes
+        device = torch.device(device)
+        if device.type != "cuda":
+            raise DgcError(DGC_ERR_INVALID_ARG, f"device {device}: the kernels run on a GPU")
+        self._index = torch.cuda.current_device() if device.index is None else device.index
+        self.device = torch.device("cuda", self._index)
+        self._f32, self._i32 = torch.float32, torch.int32
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._current = torch.cuda.current_device
+
+    def _allocate(self, nbytes: int) -> None:
+        import torch
+        self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device) if nbytes else None
+        self._ws_ptr = (self.workspace.data_ptr() + 255) // 256 * 256 if nbytes else 0
+        self._ws_bytes = nbytes
+
+    def _stream(self) -> int:
+        """The current stream of the plan's device, which has to be the current one."""
+        if self._current() != self._index:
+            raise DgcError(DGC_ERR_INVALID_ARG, f"a plan for device {self._index} called with device {self._current()} current")
+        return self._raw_stream(self._index) if self._raw_stream is not None else _stream()
 
 
-def _device(device):
-    import torch
-    device = torch.device(device)
-    if device.type != "cuda":
-        raise DgcError(DGC_ERR_INVALID_ARG, f"device {device}: the kernels run on a GPU")
-    return torch.device("cuda", torch.cuda.current_device() if device.index is None else device.index)
-
-
-class Distillation:
+class Distillation(_Plan):
     """Rows of logits over one vocabulary: a teacher's pairs, and a student's loss and gradient against such pairs.
 
     `rows`: of a call at most.  The plan owns a workspace: its calls belong on one stream (or are ordered by events)."""
@@ -504,10 +519,11 @@ class Distillation:
         self.lib = load()
         self.rows, self.vocab, self.dtype = int(rows), int(vocab), dtype
         self._shape = DgcLogits(_dtype_code(dtype), 0, self.rows, self.vocab, self.vocab)
+        self._shape_ref = C.byref(self._shape)
         b = C.c_size_t()
-        _check(self.lib.dgc_logits_workspace_bytes(C.byref(self._shape), C.byref(b)), "dgc_logits_workspace_bytes")
-        self.device = _device(device)
-        self.workspace = _Workspace(int(b.value), self.device)
+        _check(self.lib.dgc_logits_workspace_bytes(self._shape_ref, C.byref(b)), "dgc_logits_workspace_bytes")
+        self._on(device)
+        self._allocate(int(b.value))
 
     def alloc_top_logits(self, k: int):
         """(out_idx, out_val, out_lse) for `rows` rows of k pairs."""
@@ -521,43 +537,41 @@ class Distillation:
         if rows > self.rows:
             raise DgcError(DGC_ERR_CAPACITY, f"{rows} rows in a plan for {self.rows}")
         self._shape.rows = rows
-        self._shape.row_stride = _rows_of(logits, "logits", self.dtype, rows, self.vocab, self.device)
+        self._shape.row_stride = _rows_of(logits, "logits", self.dtype, (rows, self.vocab), self._index)
         return rows
 
     def dgc_top_logits(self, logits, out_idx, out_val, out_lse=None, temperature: float = 1.0) -> None:
         """The k largest logits of every row (k = out_idx.shape[1]) and, if wanted, the rows' log-sum-exp."""
-        import torch
-        rows, k, dev = self._set_shape(logits), out_idx.shape[-1], self.device
-        _check(self.lib.dgc_top_logits(
-            C.byref(self._shape), logits.data_ptr(), temperature, k,
-            _dense(out_idx, "out_idx", torch.int32, (rows, k), dev),
-            _dense(out_val, "out_val", torch.float32, (rows, k), dev),
-            _dense(out_lse, "out_lse", torch.float32, (rows,), dev),
-            self.workspace.ptr, self.workspace.nbytes, _stream()), "dgc_top_logits")
+        rows, k, dev = self._set_shape(logits), out_idx.shape[-1], self._index
+        pairs = (rows, k)
+        status = self.lib.dgc_top_logits(
+            self._shape_ref, logits.data_ptr(), temperature, k, _dense(out_idx, "out_idx", self._i32, pairs, dev),
+            _dense(out_val, "out_val", self._f32, pairs, dev), _dense(out_lse, "out_lse", self._f32, (rows,), dev),
+            self._ws_ptr, self._ws_bytes, self._stream())
+        if status:
+            _check(status, "dgc_top_logits")
 
     def dgc_distill_loss(self, logits, top_idx, top_val, loss, grad=None, top_lse=None, labels=None, row_weight=None,
                          temperature: float = 1.0, hard_weight: float = 0.0, diag_flags=None) -> None:
         """loss (or None) and grad (or None; may be `logits`) of every row; see the header for the formulas.
         top_idx and top_val may both be None: no teacher, hard labels alone."""
-        import torch
-        rows, dev = self._set_shape(logits), self.device
+        rows, dev, f32, i32 = self._set_shape(logits), self._index, self._f32, self._i32
         k = 0 if top_idx is None else top_idx.shape[-1]
         if (top_idx is None) != (top_val is None):
             raise DgcError(DGC_ERR_INVALID_ARG, "top_idx and top_val: one without the other")
-        stride = self.vocab if grad is None else _rows_of(grad, "grad", self.dtype, rows, self.vocab, dev)
-        _check(self.lib.dgc_distill_loss(
-            C.byref(self._shape), logits.data_ptr(), k,
-            _dense(top_idx, "top_idx", torch.int32, (rows, k), dev),
-            _dense(top_val, "top_val", torch.float32, (rows, k), dev),
-            _dense(top_lse, "top_lse", torch.float32, (rows,), dev),
-            _dense(labels, "labels", torch.int32, (rows,), dev),
-            _dense(row_weight, "row_weight", torch.float32, (rows,), dev), temperature, hard_weight,
-            _dense(loss, "loss", torch.float32, (rows,), dev), _ptr(grad), stride,
-            _dense(diag_flags, "diag_flags", torch.int32, (1,), dev),
-            self.workspace.ptr, self.workspace.nbytes, _stream()), "dgc_distill_loss")
+        one, pairs = (rows,), (rows, k)
+        stride = self.vocab if grad is None else _rows_of(grad, "grad", self.dtype, (rows, self.vocab), dev)
+        status = self.lib.dgc_distill_loss(
+            self._shape_ref, logits.data_ptr(), k, _dense(top_idx, "top_idx", i32, pairs, dev),
+            _dense(top_val, "top_val", f32, pairs, dev), _dense(top_lse, "top_lse", f32, one, dev),
+            _dense(labels, "labels", i32, one, dev), _dense(row_weight, "row_weight", f32, one, dev), temperature,
+            hard_weight, _dense(loss, "loss", f32, one, dev), 0 if grad is None else grad.data_ptr(), stride,
+            _dense(diag_flags, "diag_flags", i32, (1,), dev), self._ws_ptr, self._ws_bytes, self._stream())
+        if status:
+            _check(status, "dgc_distill_loss")
 
 
-class GatedScan:
+class GatedScan(_Plan):
     """Sequences of one shape (or, with `row_offsets`, of different lengths behind each other in `rows` rows) under the
     gated linear recurrence.  row_offsets: int64 on the device, sequences + 1 ascending row numbers.  The plan owns a
     workspace: its calls belong on one stream (or are ordered by events)."""
@@ -566,7 +580,7 @@ class GatedScan:
                  row_offsets=None, rows: int = None, device="cuda"):
         import torch
         self.lib = load()
-        self.device = _device(device)
+        self._on(device)
         self.sequences, self.channels, self.dtype = int(sequences), int(channels), dtype
         if row_offsets is None:
             if rows is not None and rows != sequences * max_length:
@@ -579,43 +593,41 @@ class GatedScan:
         self.row_offsets = row_offsets                                # kept alive: its address is in the shape
         self._shape = DgcScan(_dtype_code(dtype), DGC_SCAN_FREE_INPUT if free_input else 0, self.rows, self.sequences,
                               int(max_length), self.channels,
-                              _dense(row_offsets, "row_offsets", torch.int64, (self.sequences + 1,), self.device))
+                              _dense(row_offsets, "row_offsets", torch.int64, (self.sequences + 1,), self._index))
+        self._shape_ref = C.byref(self._shape)
         b, n = C.c_size_t(), C.c_int64()
-        _check(self.lib.dgc_gated_scan_workspace_bytes(C.byref(self._shape), C.byref(b)),
-               "dgc_gated_scan_workspace_bytes")
-        _check(self.lib.dgc_gated_scan_state_rows(C.byref(self._shape), C.byref(n)), "dgc_gated_scan_state_rows")
+        _check(self.lib.dgc_gated_scan_workspace_bytes(self._shape_ref, C.byref(b)), "dgc_gated_scan_workspace_bytes")
+        _check(self.lib.dgc_gated_scan_state_rows(self._shape_ref, C.byref(n)), "dgc_gated_scan_state_rows")
         self.state_rows = int(n.value)
-        self.workspace = _Workspace(int(b.value), self.device)
+        self._steps, self._carried = (self.rows, self.channels), (self.sequences, self.channels)
+        self._kept = (self.state_rows, self.channels)
+        self._allocate(int(b.value))
 
     def alloc_states(self):
         """What a forward call leaves for the backward call of the same inputs."""
         import torch
         return torch.empty(self.state_rows, self.channels, dtype=torch.float32, device=self.device)
 
-    def _rows(self, t, name: str) -> int:
-        return _rows_of(t, name, self.dtype, self.rows, self.channels, self.device)
-
-    def _carried(self, t, name: str) -> int:
-        import torch
-        return _dense(t, name, torch.float32, (self.sequences, self.channels), self.device)
-
-    def _kept(self, t) -> int:
-        import torch
-        return _dense(t, "states", torch.float32, (self.state_rows, self.channels), self.device)
-
     def dgc_gated_scan_forward(self, gate, x, h0, h, h_last=None, states=None) -> None:
         """h, and h_last (may be h0 itself) and states where given; h0 = None: zeros."""
-        _check(self.lib.dgc_gated_scan_forward(
-            C.byref(self._shape), gate.data_ptr(), self._rows(gate, "gate"), x.data_ptr(), self._rows(x, "x"),
-            self._carried(h0, "h0"), h.data_ptr(), self._rows(h, "h"), self._carried(h_last, "h_last"),
-            self._kept(states), self.workspace.ptr, self.workspace.nbytes, _stream()), "dgc_gated_scan_forward")
+        t, steps, dev, f32 = self.dtype, self._steps, self._index, self._f32
+        status = self.lib.dgc_gated_scan_forward(
+            self._shape_ref, gate.data_ptr(), _rows_of(gate, "gate", t, steps, dev), x.data_ptr(),
+            _rows_of(x, "x", t, steps, dev), _dense(h0, "h0", f32, self._carried, dev), h.data_ptr(),
+            _rows_of(h, "h", t, steps, dev), _dense(h_last, "h_last", f32, self._carried, dev),
+            _dense(states, "states", f32, self._kept, dev), self._ws_ptr, self._ws_bytes, self._stream())
+        if status:
+            _check(status, "dgc_gated_scan_forward")
 
     def dgc_gated_scan_backward(self, gate, x, states, dh, dh_last, dgate, dx, dh0=None) -> None:
         """dgate, dx, and dh0 (may be dh_last itself) where given, from the states of the forward call; dh_last = None:
         zeros."""
-        _check(self.lib.dgc_gated_scan_backward(
-            C.byref(self._shape), gate.data_ptr(), self._rows(gate, "gate"), x.data_ptr(), self._rows(x, "x"),
-            self._kept(states), dh.data_ptr(), self._rows(dh, "dh"), self._carried(dh_last, "dh_last"),
-            dgate.data_ptr(), self._rows(dgate, "dgate"), dx.data_ptr(), self._rows(dx, "dx"),
-            self._carried(dh0, "dh0"), self.workspace.ptr, self.workspace.nbytes, _stream()),
-            "dgc_gated_scan_backward")
+        t, steps, dev, f32 = self.dtype, self._steps, self._index, self._f32
+        status = self.lib.dgc_gated_scan_backward(
+            self._shape_ref, gate.data_ptr(), _rows_of(gate, "gate", t, steps, dev), x.data_ptr(),
+            _rows_of(x, "x", t, steps, dev), _dense(states, "states", f32, self._kept, dev), dh.data_ptr(),
+            _rows_of(dh, "dh", t, steps, dev), _dense(dh_last, "dh_last", f32, self._carried, dev), dgate.data_ptr(),
+            _rows_of(dgate, "dgate", t, steps, dev), dx.data_ptr(), _rows_of(dx, "dx", t, steps, dev),
+            _dense(dh0, "dh0", f32, self._carried, dev), self._ws_ptr, self._ws_bytes, self._stream())
+        if status:
+            _check(status, "dgc_gated_scan_backward")

@@ -624,14 +624,15 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------
-// Workgroups that walk all rows, as many as the device holds at a time.
-template <typename T, int NT, int CH, typename ARGS>
-hipError_t launch_rows(const ARGS& a, void (*kernel)(ARGS), hipStream_t stream) {
-  int per_unit = 0;
-  const hipError_t e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_unit, kernel, NT, 0);
-  if (e != hipSuccess) return e;
-  const int64_t most = (int64_t)(per_unit < 1 ? 1 : per_unit) * compute_units();
-  kernel<<<dim3((unsigned)(a.rows < most ? a.rows : most)), NT, 0, stream>>>(a);
+// Workgroups that walk all rows, as many as the device holds at a time (asked for once: it takes longer than a launch).
+template <typename T, int NT, int CH, typename ARGS, void (*KERNEL)(ARGS)>
+hipError_t launch_rows(const ARGS& a, hipStream_t stream) {
+  static const int per_unit = [] {
+    int n = 0;
+    return hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, KERNEL, NT, 0) == hipSuccess && n > 0 ? n : 1;
+  }();
+  const int64_t most = (int64_t)per_unit * compute_units();
+  KERNEL<<<dim3((unsigned)(a.rows < most ? a.rows : most)), NT, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -639,7 +640,7 @@ struct PickTop {
   template <typename T, typename ARGS>
   static hipError_t launch(const ARGS& a, hipStream_t stream) {
     const int64_t vectors = ceil_div(a.vocab, 16 / (int64_t)sizeof(T));
-#define DGC_ROW(NT, CH) return launch_rows<T, NT, CH>(a, &top_logits_kernel<T, NT, CH>, stream)
+#define DGC_ROW(NT, CH) return launch_rows<T, NT, CH, TopArgs, &top_logits_kernel<T, NT, CH>>(a, stream)
     if (vectors <= 64) DGC_ROW(64, 1);
     if (vectors <= 256) DGC_ROW(256, 1);
     if (vectors <= 1024) DGC_ROW(256, 4);
@@ -653,7 +654,7 @@ struct PickDistill {
   template <typename T, typename ARGS>
   static hipError_t launch(const ARGS& a, hipStream_t stream) {
     const int64_t vectors = ceil_div(a.vocab, 16 / (int64_t)sizeof(T));
-#define DGC_ROW(NT, CH) return launch_rows<T, NT, CH>(a, &distill_kernel<T, NT, CH, MODE, GRAD>, stream)
+#define DGC_ROW(NT, CH) return launch_rows<T, NT, CH, DistillArgs, &distill_kernel<T, NT, CH, MODE, GRAD>>(a, stream)
     if (vectors <= 64) DGC_ROW(64, 1);
     if (vectors <= 256) DGC_ROW(256, 1);
     if (vectors <= 1024) DGC_ROW(256, 4);

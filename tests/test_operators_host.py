@@ -138,18 +138,21 @@ def test_binding_refuses_other_tensors():
     with pytest.raises(B.DgcError):
         B._dtype_code(torch.float64)
     t = torch.zeros(4, 10)
-    with pytest.raises(B.DgcError):
-        B._rows_of(t, "t", torch.float32, 4, 9, t.device)
-    with pytest.raises(B.DgcError):
-        B._rows_of(t, "t", torch.bfloat16, 4, 10, t.device)
-    with pytest.raises(B.DgcError):
-        B._rows_of(torch.zeros(10, 4).t(), "t", torch.float32, 4, 10, t.device)
-    with pytest.raises(B.DgcError):
-        B._rows_of(torch.zeros(1, 10).expand(4, 10), "t", torch.float32, 4, 10, t.device)
-    with pytest.raises(B.DgcError):
-        B._dense(torch.zeros(4, 10)[:, :5], "t", torch.float32, (4, 5), t.device)
-    assert B._rows_of(torch.zeros(4, 30)[:, 5:15], "t", torch.float32, 4, 10, t.device) == 30
-    assert B._dense(None, "t", torch.float32, (4,), t.device) == 0
+    here = t.get_device()                                             # -1: not a GPU
+    f32 = torch.float32
+    for tensor, dtype, shape, index in ((t, f32, (4, 9), here), (t, f32, (5, 10), here), (t, torch.bfloat16, (4, 10), here),
+                                        (t, f32, (4, 10), 0), (torch.zeros(10, 4).t(), f32, (4, 10), here),
+                                        (torch.zeros(1, 10).expand(4, 10), f32, (4, 10), here),
+                                        (torch.zeros(40), f32, (4, 10), here)):
+        with pytest.raises(B.DgcError) as err:
+            B._rows_of(tensor, "t", dtype, shape, index)
+        assert err.value.status == B.DGC_ERR_INVALID_ARG
+    for tensor, shape in ((torch.zeros(4, 10)[:, :5], (4, 5)), (t, (40,))):
+        with pytest.raises(B.DgcError):
+            B._dense(tensor, "t", f32, shape, here)
+    assert B._rows_of(torch.zeros(4, 30)[:, 5:15], "t", f32, (4, 10), here) == 30
+    assert B._rows_of(torch.zeros(1, 10).expand(1, 10), "t", f32, (1, 10), here) == 10
+    assert B._dense(None, "t", f32, (4,), here) == 0
 
 
 # --- the definitions themselves ----------------------------------------------------------
