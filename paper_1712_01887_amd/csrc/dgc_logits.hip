@@ -79,8 +79,8 @@ struct Row {
   }
   // Piece k of NT x CH vectors of a longer row.
   __device__ __forceinline__ void read_piece(const T* z, int whole, int k) {
-    const int first = k * NT * CH;
-    read(buffer(z ? z + (int64_t)first * E : nullptr, (whole - first) * E));
+    const int first = k * NT * CH, vectors = whole - first < NT * CH ? whole - first : NT * CH;
+    read(buffer(z ? z + (int64_t)first * E : nullptr, vectors * E));
   }
   __device__ __forceinline__ void cut_piece(int whole, int k) { cut((whole - k * NT * CH) * E); }
   // Before a row that was read is used: its end.

@@ -136,6 +136,20 @@ def test_long_sequences(lengths, channels, dtype):
     check(lengths, channels, dtype, packed=len(set(lengths)) > 1, seed=7)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_more_tiles_than_workgroups(dtype):
+    check([9000, 1, 0, 7003, 4096], 1100, dtype, seed=20)             # each workgroup takes several
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_short_and_a_few_long_sequences(dtype):
+    rng = np.random.default_rng(21)
+    lengths = [int(x) for x in rng.integers(0, 40, 400)]
+    for i in (0, 117, 399):
+        lengths[i] = 1500
+    check(lengths, 300, dtype, seed=21)
+
+
 def test_rows_behind_the_last_sequence_stay():
     check([33, 70], 50, "f32", gap=9, seed=8)
     check([33, 700], 50, "bf16", gap=130, seed=9)
