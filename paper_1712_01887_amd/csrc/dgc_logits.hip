@@ -185,10 +185,10 @@ __device__ __forceinline__ uint32_t floor_of(const uint32_t* keys, int k, int la
   return found ? found : 1u;
 }
 
-// The largest of four neighbouring lanes' values.
-__device__ __forceinline__ float quad_max(float x) {
-  x = fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0xb1, 0xf, 0xf, false)));  // quad_perm 1 0 3 2
-  return fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x4e, 0xf, 0xf, false)));  // 2 3 0 1
+// The value of a lane of the same four: the neighbour's (0xb1) or that of the other two (0x4e).
+template <int PERM>
+__device__ __forceinline__ float neighbour(float x) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), PERM, 0xf, 0xf, false));
 }
 
 // Of the vectors listed, those that still reach the floor.
@@ -290,7 +290,7 @@ __device__ __forceinline__ void select_exactly(const T* z, int vocab, int k, Top
 // vectors that reach the floor of what has gone by are listed in LDS, in the end their elements that reach the last floor,
 // and these are ranked by counting.
 template <typename T, int NT, int CH>
-__global__ __launch_bounds__(NT) void top_logits_kernel(TopArgs a) {
+__global__ __launch_bounds__(NT, NT < 512 || CH > 4 ? 4 : 6) void top_logits_kernel(TopArgs a) {
   using Piece = Row<T, NT, CH>;
   constexpr int E = Piece::E;
   constexpr uint32_t kCandidates = TopShared<NT>::kCandidates, kVectors = TopShared<NT>::kVectors;
@@ -342,22 +342,19 @@ __global__ __launch_bounds__(NT) void top_logits_kernel(TopArgs a) {
         now.renew();
       }
       if ((k & (k - 1)) == 0 || k + 1 == pieces) {  // the floor of what has gone by, when that has doubled
-        const bool few = a.k * 8 <= kKeys;            // a quarter of the keys do
+        const int fold = a.k * 8 <= kKeys ? 4 : a.k * 4 <= kKeys ? 2 : 1;  // fewer keys do where k is small
         float keyed[2] = {kKeys == NT ? seen : largest[0], largest[1]};
-        if (few) {
 #pragma unroll
-          for (int i = 0; i < kKeys / NT; ++i) keyed[i] = quad_max(keyed[i]);
-          if (lane % 4 == 0) {
-#pragma unroll
-            for (int i = 0; i < kKeys / NT; ++i) s.keys[(i * NT + (int)threadIdx.x) / 4] = order_key(keyed[i]);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < kKeys / NT; ++i) s.keys[i * NT + threadIdx.x] = order_key(keyed[i]);
+        for (int i = 0; i < kKeys / NT; ++i) {
+          if (fold > 1) keyed[i] = fmaxf(keyed[i], neighbour<0xb1>(keyed[i]));
+          if (fold > 2) keyed[i] = fmaxf(keyed[i], neighbour<0x4e>(keyed[i]));
+          if (lane % fold == 0) s.keys[(i * NT + (int)threadIdx.x) / fold] = order_key(keyed[i]);
         }
         __syncthreads();
         if (w == 0) {
-          const uint32_t floor = few ? floor_of<kKeys / 4>(s.keys, a.k, lane) : floor_of<kKeys>(s.keys, a.k, lane);
+          const uint32_t floor = fold == 4   ? floor_of<kKeys / 4>(s.keys, a.k, lane)
+                                 : fold == 2 ? floor_of<kKeys / 2>(s.keys, a.k, lane)
+                                             : floor_of<kKeys>(s.keys, a.k, lane);
           if (lane == 0) s.floor = floor;
         }
         const uint32_t listed = __builtin_amdgcn_readfirstlane(s.hits);
@@ -404,19 +401,17 @@ __global__ __launch_bounds__(NT) void top_logits_kernel(TopArgs a) {
       select_exactly<T, NT>(z, a.vocab, a.k, s);
       n = __builtin_amdgcn_readfirstlane(s.count);
     }
-    // rank: 2^b >= n candidates, NT / 2^b threads to each
-    int b = 6;
-    while (b < 10 && (1u << b) < n) ++b;
-    for (uint32_t i = threadIdx.x; i < (1u << b) && i < kCandidates; i += NT) s.rank[i] = 0;
+    // rank: so many threads to a candidate that all have work, each with its share of the others to compare with
+    const uint32_t span = (n + 63u) & ~63u, parts = span >= NT || span == 0 ? 1u : NT / span;
+    for (uint32_t i = threadIdx.x; i < span; i += NT) s.rank[i] = 0;
     __syncthreads();
-    for (uint32_t t = threadIdx.x; t < (1u << b) || t < NT; t += NT) {
-      const uint32_t c = t & ((1u << b) - 1), part = t >> b, parts = (1u << b) >= NT ? 1u : NT >> b;
-      if (c < n) {
-        const unsigned long long key = s.candidates[c];
-        uint32_t better = 0;
-        for (uint32_t i = part; i < n; i += parts) better += s.candidates[i] > key;
-        if (better) atomicAdd(&s.rank[c], better);
-      }
+    for (uint32_t t = threadIdx.x; t < span * parts; t += NT) {
+      const uint32_t part = t / span, c = t - part * span;
+      const unsigned long long key = s.candidates[c < n ? c : 0];
+      uint32_t better = 0;
+#pragma unroll 1
+      for (uint32_t i = part; i < n; i += parts) better += s.candidates[i] > key;
+      if (c < n && better) atomicAdd(&s.rank[c], better);
     }
     __syncthreads();
     for (uint32_t c = threadIdx.x; c < n; c += NT) {
@@ -644,8 +639,11 @@ struct PickTop {
     if (vectors <= 64) DGC_ROW(64, 1);
     if (vectors <= 256) DGC_ROW(256, 1);
     if (vectors <= 1024) DGC_ROW(256, 4);
-    if (a.rows <= 2 * compute_units()) DGC_ROW(512, 8);  // few rows: what a row takes is what counts
-    DGC_ROW(256, 8);
+    // Few rows: what one of them takes is what counts, so fewer pieces (333 rows of 10000 in 32 bits, 64 pairs: 10.6 us in
+    // pieces of 8 vectors a thread, 13.3 in pieces of 4).  Many: workgroups to a compute unit (4096 of 32000 in bfloat16: 84.6
+    // and 79.6; 2048 of 131072, 256 pairs: 218 and 186; pieces of 8 to 256 threads 83.2 and 233).
+    if (a.rows <= 2 * compute_units()) DGC_ROW(512, 8);
+    DGC_ROW(512, 4);
 #undef DGC_ROW
   }
 };
