@@ -418,9 +418,91 @@ struct BackwardTile {
   }
 };
 
+// ---- a few steps: a thread walks VEC channels of one sequence --------------------------------------------------
+// What bounds this is the launch: 256 streams of 1500 channels in 32 bits, one step, took 20 us by tiles, of which a
+// wavefront uses one row then.
+constexpr int kShort = 4;
+constexpr int kShortThreads = 256;
+
+template <typename T, int VEC, bool FREE, bool REVERSE>
+__global__ __launch_bounds__(kShortThreads) void scan_short_kernel(ScanArgs a) {
+  const uint32_t groups = (uint32_t)((a.channels / VEC + kShortThreads - 1) / kShortThreads);  // of a sequence
+  const int64_t s = blockIdx.x / groups;
+  const int64_t d = ((int64_t)(blockIdx.x - (uint32_t)s * groups) * kShortThreads + threadIdx.x) * VEC;
+  if (d >= a.channels) return;
+  int64_t begin, length;
+  sequence_rows(a, s, begin, length);
+  auto at = [&](const void* array, int64_t stride, int t) {
+    return reinterpret_cast<const Pack<T, VEC>*>(static_cast<const T*>(array) + (begin + t) * stride + d);
+  };
+  auto to = [&](void* array, int64_t stride, int t) {
+    return reinterpret_cast<Pack<T, VEC>*>(static_cast<T*>(array) + (begin + t) * stride + d);
+  };
+  Pack<T, VEC> gate[kShort]{}, x[kShort]{}, dh[kShort]{};
+#pragma unroll
+  for (int t = 0; t < kShort; ++t)
+    if (t < length) {
+      gate[t] = *at(a.gate, a.gate_stride, t);
+      x[t] = *at(a.x, a.x_stride, t);
+      if (REVERSE) dh[t] = *at(a.dh, a.dh_stride, t);
+    }
+  float carry[VEC], state[VEC], before[kShort][VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) carry[j] = a.first ? a.first[s * a.channels + d + j] : 0.0f;
+  float* kept = a.states ? a.states + state_row(s, begin, 0) * a.channels + d : nullptr;
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) {
+    state[j] = carry[j];
+    if (REVERSE) state[j] = length > 0 ? kept[j] : 0.0f;
+    if (!REVERSE && kept && length > 0) kept[j] = state[j];
+  }
+#pragma unroll
+  for (int t = 0; t < kShort; ++t)
+    if (t < length) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const Gates g = gates_of(gate[t].get(j));
+        const float xt = x[t].get(j);
+        before[t][j] = state[j];
+        state[j] = fmaf(g.a, state[j], FREE ? xt : g.b * xt);
+      }
+      if (!REVERSE) {
+        Pack<T, VEC> h;
+        h.set(state);
+        *to(a.h, a.h_stride, t) = h;
+      }
+    }
+  if (REVERSE) {
+#pragma unroll
+    for (int t = kShort - 1; t >= 0; --t)
+      if (t < length) {
+        float vg[VEC], vx[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          const Gates g = gates_of(gate[t].get(j));
+          const float gt = dh[t].get(j) + carry[j], inner = FREE ? before[t][j] : before[t][j] - x[t].get(j);
+          vx[j] = FREE ? gt : g.b * gt;
+          vg[j] = gt * inner * (g.a * g.b);
+          carry[j] = g.a * gt;
+        }
+        Pack<T, VEC> og, ox;
+        og.set(vg);
+        ox.set(vx);
+        *to(a.dx, a.dx_stride, t) = ox;
+        *to(a.dgate, a.dgate_stride, t) = og;
+      }
+  }
+  if (a.last) {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) a.last[s * a.channels + d + j] = REVERSE ? carry[j] : state[j];
+  }
+}
+
 // ---- short sequences: a workgroup walks the tiles of one sequence and block ---------------------------------
+// (Two wavefronts of a SIMD at least: left to itself the compiler takes registers for one, and tiles of twice as many steps
+// are no better either: 512 sequences of 128 x 2048 in bfloat16 188 and 430 us so, 152 and 334 as it is.)
 template <typename TILE, int W>
-__global__ __launch_bounds__(W * 64) void scan_walk_kernel(ScanArgs a) {
+__global__ __launch_bounds__(W * 64, 2) void scan_walk_kernel(ScanArgs a) {
   using SHAPE = typename TILE::SHAPE;
   constexpr int VEC = SHAPE::kVec, kBlock = SHAPE::kBlock, kRows = W * SHAPE::kRows;
   __shared__ typename TILE::Parts parts[2];
@@ -664,12 +746,15 @@ template <template <typename, int, bool> class TILE, typename SHAPE, bool FREE>
 hipError_t launch_tiles(const ScanArgs& a, void* workspace, hipStream_t stream) {
   const int64_t blocks = ceil_div(a.channels, SHAPE::kBlock);
   constexpr int kWaves = kTileRows / SHAPE::kRows;
+  if (a.max_length <= kShort) {
+    using T = typename SHAPE::T;
+    const int64_t groups = ceil_div(a.channels / SHAPE::kVec, kShortThreads) * a.sequences;
+    scan_short_kernel<T, SHAPE::kVec, FREE, TILE<SHAPE, kWaves, FREE>::kReverse><<<dim3((uint32_t)groups), kShortThreads, 0, stream>>>(a);
+    return hipGetLastError();
+  }
   if (!scan_chained(a)) {
-    const dim3 groups((uint32_t)(a.sequences * blocks));
-    if (a.max_length <= kStateRows)
-      scan_walk_kernel<TILE<SHAPE, SHAPE::kStateWaves, FREE>, SHAPE::kStateWaves><<<groups, SHAPE::kStateWaves * 64, 0, stream>>>(a);
-    else
-      scan_walk_kernel<TILE<SHAPE, kWaves, FREE>, kWaves><<<groups, kWaves * 64, 0, stream>>>(a);
+    constexpr int W = SHAPE::kStateWaves;
+    scan_walk_kernel<TILE<SHAPE, W, FREE>, W><<<dim3((uint32_t)(a.sequences * blocks)), W * 64, 0, stream>>>(a);
     return hipGetLastError();
   }
   Chain chain{};

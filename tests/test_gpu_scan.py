@@ -137,6 +137,15 @@ def test_long_sequences(lengths, channels, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("channels", [1, 30, 96, 1100, 2052])
+def test_a_few_steps(channels, dtype):
+    for free in (False, True):
+        check([1, 0, 3, 4, 2, 1], channels, dtype, free=free, seed=channels)
+        check([1] * 7, channels, dtype, free=free, packed=False, seed=channels, extremes=True)
+        check([4, 3], channels, dtype, free=free, stride=channels + 5, shift=1, carried=False, seed=channels)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_more_tiles_than_workgroups(dtype):
     check([9000, 1, 0, 7003, 4096], 1100, dtype, seed=20)             # each workgroup takes several
 
