@@ -801,7 +801,16 @@ int64_t scan_word_rows(const ScanArgs& a) {
   return a.row_offsets ? a.rows / kTileRows + a.sequences : a.sequences * ceil_div(a.max_length, kTileRows);
 }
 
-bool scan_chained(const ScanArgs& a) { return a.max_length > kTileRows; }
+// Long sequences are cut into tiles that wait for each other, unless there are so many of them (times blocks of 64
+// channels) that a workgroup to each fills the device, and none is much longer than the mean.  In us, tiles side by side and
+// one behind the other, forward / backward in bfloat16: 12 x 1500 x 1200 47/73 and 61/129, 24 (456 blocks) 80/155 and 70/167,
+// 48 155/277 and 140/243, 64 x 1024 x 2048 190/348 and 173/277, 48 of 187 to 1500 steps 108/188 and 97/168; in 32 bits 20 x
+// 200 x 1500 32/39 and 19/30.
+constexpr int64_t kWalkBlocks = 384;
+bool scan_chained(const ScanArgs& a) {
+  if (a.max_length <= kTileRows) return false;
+  return a.sequences * ceil_div(a.channels, 64) < kWalkBlocks || a.max_length > 4 * (a.rows / a.sequences);
+}
 
 int64_t scan_workgroups(const ScanArgs& a) {
   return (scan_chained(a) ? scan_word_rows(a) : a.sequences) * ceil_div(a.channels, 64);

@@ -150,6 +150,13 @@ def test_more_tiles_than_workgroups(dtype):
     check([9000, 1, 0, 7003, 4096], 1100, dtype, seed=20)             # each workgroup takes several
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_sequences_enough_to_fill_the_device(dtype):
+    rng = np.random.default_rng(22)
+    check([int(x) for x in rng.integers(120, 300, 200)], 130, dtype, seed=22)
+    check([200] * 130, 192, dtype, packed=False, seed=23, carried=False, extremes=True)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_many_short_and_a_few_long_sequences(dtype):
     rng = np.random.default_rng(21)
