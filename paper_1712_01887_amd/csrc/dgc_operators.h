@@ -110,18 +110,6 @@ struct alignas(sizeof(T) * N) Pack {
         w[j / 2] = (uint32_t)__builtin_bit_cast(uint16_t, from_float<T>(v[j])) | (uint32_t)__builtin_bit_cast(uint16_t, from_float<T>(v[j + 1])) << 16;
     }
   }
-  __device__ __forceinline__ T take(int j) const {
-    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, w[j]);
-    else return __builtin_bit_cast(T, (uint16_t)(w[j / kPerWord] >> (j % kPerWord ? 16 : 0)));
-  }
-  __device__ __forceinline__ void put(int j, T v) {
-    if constexpr (sizeof(T) == 4) {
-      w[j] = __builtin_bit_cast(uint32_t, v);
-    } else {
-      const uint32_t bits = __builtin_bit_cast(uint16_t, v);
-      w[j / kPerWord] = j % kPerWord ? (w[j / kPerWord] & 0xffffu) | bits << 16 : (w[j / kPerWord] & 0xffff0000u) | bits;
-    }
-  }
   // From here on the compiler takes the words for new ones: it will not keep what it has made of them.
   __device__ __forceinline__ void renew() {
 #pragma unroll
