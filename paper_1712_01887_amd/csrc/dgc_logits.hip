@@ -221,6 +221,32 @@ __device__ __forceinline__ void thin_out(TopShared<NT>& s, uint32_t listed, floa
   __syncthreads();
 }
 
+// So many threads to a candidate that all have work, each with its share of the others to compare with, four of them at a
+// time; a single wavefront with several candidates to a lane looks at what it has read for HELD of them (4096 rows of 500 in
+// bfloat16 to their 256 largest: one by one 357 us, others in fours 164, HELD = 4 too 100; 2048 x 131072 to 256: 188 and 160).
+template <int NT, uint32_t HELD>
+__device__ __forceinline__ void count_better(TopShared<NT>& s, uint32_t n, uint32_t span) {
+  const uint32_t parts = span >= NT || span == 0 ? 1u : NT / span;  // a power of two
+  for (uint32_t t = threadIdx.x; t < span * parts; t += NT * HELD) {
+    const uint32_t part = t / span, c = t - part * span;
+    unsigned long long key[HELD];
+    uint32_t better[HELD];
+#pragma unroll
+    for (uint32_t m = 0; m < HELD; ++m) key[m] = s.candidates[c + m * NT < span ? c + m * NT : c], better[m] = 0;
+#pragma unroll 1
+    for (uint32_t i = part; i < n; i += 4 * parts) {
+      const unsigned long long others[4] = {s.candidates[i], s.candidates[i + parts], s.candidates[i + 2 * parts], s.candidates[i + 3 * parts]};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (uint32_t m = 0; m < HELD; ++m) better[m] += others[j] > key[m];
+    }
+#pragma unroll
+    for (uint32_t m = 0; m < HELD; ++m)
+      if (c + m * NT < n && better[m]) atomicAdd(&s.rank[c + m * NT], better[m]);
+  }
+}
+
 // The exact way, for rows in which too many logits reach the floor (ties above all): the k-th largest key by its bytes from
 // the highest, then all logits above it and the first few, by index, of those that equal it.  The row is read again in every
 // pass.
@@ -290,7 +316,7 @@ __device__ __forceinline__ void select_exactly(const T* z, int vocab, int k, Top
 // on its way while one is looked at: the vectors that reach the floor of what has gone by are listed in LDS, in the end
 // their elements that reach the last floor, and these are ranked by counting.  Each logit is read once, and takes a maximum
 // and, for the log-sum-exp, an exponential against the thread's own largest so far.
-//   4096 x 131072 in bfloat16, 64 pairs: 222 us, 4.8 TB/s of 6.5 that a bare kernel reaches.  A row held in registers as a
+//   4096 x 131072 in bfloat16, 64 pairs: 218 us, 4.9 TB/s of 6.5 that a bare kernel reaches.  A row held in registers as a
 //   whole took 302: nothing was on its way while it was ranked.  8 x 32768 7.1 us, 700 x 10000 in 32 bits 15.4: a row's chain
 //   of piece, floor, list and rank, about 5 us behind its loads.
 template <typename T, int NT, int CH>
@@ -405,18 +431,14 @@ __global__ __launch_bounds__(NT, NT < 512 || CH > 4 ? 4 : 6) void top_logits_ker
       select_exactly<T, NT>(z, a.vocab, a.k, s);
       n = __builtin_amdgcn_readfirstlane(s.count);
     }
-    // rank: so many threads to a candidate that all have work, each with its share of the others to compare with
-    const uint32_t span = (n + 63u) & ~63u, parts = span >= NT || span == 0 ? 1u : NT / span;
-    for (uint32_t i = threadIdx.x; i < span; i += NT) s.rank[i] = 0;
-    __syncthreads();
-    for (uint32_t t = threadIdx.x; t < span * parts; t += NT) {
-      const uint32_t part = t / span, c = t - part * span;
-      const unsigned long long key = s.candidates[c < n ? c : 0];
-      uint32_t better = 0;
-#pragma unroll 1
-      for (uint32_t i = part; i < n; i += parts) better += s.candidates[i] > key;
-      if (c < n && better) atomicAdd(&s.rank[c], better);
+    const uint32_t span = (n + 63u) & ~63u;
+    for (uint32_t i = threadIdx.x; i < span; i += NT) {
+      s.rank[i] = 0;
+      if (i >= n) s.candidates[i] = 0;  // less than any, so that no four need a look at the end
     }
+    __syncthreads();
+    if (NT == 64 && span > NT) count_better<NT, 4>(s, n, span);
+    else count_better<NT, 1>(s, n, span);
     __syncthreads();
     for (uint32_t c = threadIdx.x; c < n; c += NT) {
       const uint32_t rank = s.rank[c];

@@ -123,6 +123,13 @@ def test_top_many_rows():
     check_top(logits(700, 2000, "f32", 2), 16, "f32")
 
 
+@pytest.mark.parametrize("vocab,k", [(65, 65), (128, 127), (224, 210), (256, 256), (500, 193), (511, 256)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_top_most_of_a_row(vocab, k, dtype):
+    check_top(logits(300, vocab, dtype, vocab), k, dtype)
+    check_top(logits(3, vocab, dtype, k, "ties"), k, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_top_nan_and_infinity(dtype):
     for vocab in (500, 20000):
