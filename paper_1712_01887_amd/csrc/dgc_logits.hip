@@ -673,9 +673,9 @@ struct PickTop {
     if (vectors <= 64) DGC_ROW(64, 1);
     if (vectors <= 256) DGC_ROW(256, 1);
     if (vectors <= 1024) DGC_ROW(256, 4);
-    // Few rows: what one of them takes is what counts, so fewer pieces (333 rows of 10000 in 32 bits, 64 pairs: 10.6 us in
-    // pieces of 8 vectors a thread, 13.3 in pieces of 4).  Many: workgroups to a compute unit (4096 of 32000 in bfloat16: 84.6
-    // and 79.6; 2048 of 131072, 256 pairs: 218 and 186; pieces of 8 to 256 threads 83.2 and 233).
+    // Few rows: what one of them takes is what counts, so fewer pieces (333 rows of 10000 in 32 bits, 64 pairs: 10.2 us in
+    // pieces of 8 vectors a thread, 12.2 in pieces of 4).  Many: workgroups to a compute unit (4096 of 32000 in bfloat16, 64
+    // pairs: 80.9 and 78.1; 2048 of 131072, 256 pairs: 186 and 161; pieces of 8 to 256 threads 83.7 and 188).
     if (a.rows <= 2 * compute_units()) DGC_ROW(512, 8);
     DGC_ROW(512, 4);
 #undef DGC_ROW
