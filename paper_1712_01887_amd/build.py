@@ -22,6 +22,7 @@ SOURCES = [os.path.join(HERE, "csrc", name) for name in
             "dgc_operators_api.hip", "dgc_logits.hip", "dgc_scan.hip")]
 HEADERS = [os.path.join(HERE, "csrc", "dgc_internal.h"), os.path.join(HERE, "csrc", "dgc_device.h"),
            os.path.join(HERE, "csrc", "dgc_probe.h"), os.path.join(HERE, "csrc", "dgc_operators.h"),
+           os.path.join(HERE, "csrc", "dgc_steps.h"),
            os.path.join(HERE, "csrc", "dgc_band.h"), os.path.join(ROOT, "include", "dgc.h")]
 
 

@@ -4,13 +4,13 @@
 #include <cmath>
 
 #include "dgc_operators.h"
+#include "dgc_steps.h"
 
 using namespace dgc;
 
 namespace {
 
 constexpr int64_t kIntLimit = (int64_t)1 << 31;
-constexpr int64_t kWidthLimit = (int64_t)1 << 24;  // channels and row strides of a scan: offsets inside a tile take 32 bits
 
 bool aligned_to(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 

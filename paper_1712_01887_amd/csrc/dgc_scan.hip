@@ -1,6 +1,7 @@
 // The gated linear recurrence: h_t = a_t h_{t-1} + b_t x_t with a = sigmoid(gate), forward and backward.
 
 #include "dgc_operators.h"
+#include "dgc_steps.h"
 
 namespace dgc {
 
@@ -51,6 +52,7 @@ struct Shape {
   static constexpr int kRows = GROUPS * S;                      // of a wavefront
   static constexpr int kStateWaves = kStateRows / kRows;        // wavefronts to a kept state
   static_assert(kStateRows % kRows == 0, "a kept state lies in front of a wavefront's first step");
+  static_assert(kRows <= kWaveRows && sizeof(T) <= 4, "offsets of a wavefront's rows take 32 bits");
 };
 
 // Where a tile lies, for the wavefronts that work on it.
@@ -103,26 +105,23 @@ __device__ __forceinline__ Share share_of(const ScanArgs& a, const Place& p, int
 // The wavefront's rows of an array as a buffer resource: an offset behind the last of them reads zeros and stores nothing,
 // and one register to a lane is all that addresses take.  (Data format 32 in word 3, no swizzle, offsets in bytes.)
 constexpr int kBufferFormat = 0x00020000;
-constexpr uint32_t kNowhere = 0xf0000000u;  // behind the end of every such buffer: up to 32 rows of less than 2^24 elements
 
 template <typename T, int VEC, int S>
 struct Steps {
   __amdgpu_buffer_rsrc_t rsrc;
-  uint32_t first, stride;  // bytes
-  __device__ __forceinline__ Steps(const void* array, int64_t stride_, const Share& h)
-      : rsrc(__builtin_amdgcn_make_buffer_rsrc((void*)(static_cast<const T*>(array) + h.at * stride_), 0,
-                                               (int)((uint32_t)h.rows * (uint32_t)stride_ * (uint32_t)sizeof(T)), kBufferFormat)),
-        stride((uint32_t)stride_ * (uint32_t)sizeof(T)) {
-    first = h.steps > 0 ? (uint32_t)(h.group * S) * stride + (uint32_t)h.d * (uint32_t)sizeof(T) : kNowhere;
-  }
+  StepOffsets offsets;
+  __device__ __forceinline__ Steps(const void* array, int64_t stride, const Share& h)
+      : rsrc(__builtin_amdgcn_make_buffer_rsrc((void*)(static_cast<const T*>(array) + h.at * stride), 0,
+                                               (int)StepOffsets::buffer_bytes(h.rows, (uint32_t)stride * (uint32_t)sizeof(T)), kBufferFormat)),
+        offsets(h.steps, h.group * S, (uint32_t)h.d * (uint32_t)sizeof(T), (uint32_t)stride * (uint32_t)sizeof(T)) {}
   __device__ __forceinline__ Pack<T, VEC> load(int i) const {
-    const uint32_t at = first + (uint32_t)i * stride;
+    const uint32_t at = offsets.at(i);
     if constexpr (sizeof(T) * VEC == 8) return __builtin_bit_cast(Pack<T, VEC>, __builtin_amdgcn_raw_buffer_load_b64(rsrc, at, 0, 0));
     else if constexpr (sizeof(T) * VEC == 4) return __builtin_bit_cast(Pack<T, VEC>, __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, 0, 0));
     else return __builtin_bit_cast(Pack<T, VEC>, __builtin_amdgcn_raw_buffer_load_b16(rsrc, at, 0, 0));
   }
   __device__ __forceinline__ void store(int i, const Pack<T, VEC>& v) const {
-    const uint32_t at = first + (uint32_t)i * stride;
+    const uint32_t at = offsets.at(i);
     typedef uint32_t two __attribute__((ext_vector_type(2)));
     if constexpr (sizeof(T) * VEC == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(two, v), rsrc, at, 0, 0);
     else if constexpr (sizeof(T) * VEC == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), rsrc, at, 0, 0);
