@@ -28,10 +28,9 @@ __device__ __forceinline__ void sequence_rows(const ScanArgs& a, int64_t s, int6
     length = a.max_length;
     return;
   }
-  const int64_t lo = a.row_offsets[s], hi = a.row_offsets[s + 1];
-  begin = lo < 0 ? 0 : lo > a.rows ? a.rows : lo;
-  length = (hi > a.rows ? a.rows : hi) - begin;
-  length = length < 0 ? 0 : length > a.max_length ? a.max_length : length;
+  const SequenceRows cut(a.row_offsets[s], a.row_offsets[s + 1], a.rows, a.max_length);
+  begin = cut.begin;
+  length = cut.length;
 }
 
 // Where the state in front of step c * kStateRows of a sequence is kept: no two of them at one place, all below

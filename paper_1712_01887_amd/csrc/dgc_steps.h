@@ -1,4 +1,4 @@
-// Where the steps of a scan lie in its arrays: plain arithmetic, for the host too.
+// Where the sequences and steps of a scan lie in its arrays: plain arithmetic, for the host too.
 #ifndef DGC_STEPS_H_
 #define DGC_STEPS_H_
 
@@ -8,6 +8,16 @@ namespace dgc {
 
 constexpr int64_t kWidthLimit = (int64_t)1 << 24;  // channels and row strides of a scan: offsets inside a tile take 32 bits
 constexpr int kWaveRows = 16;                      // a wavefront's at most, and so a lane's
+
+// Rows [begin, begin + length) of a sequence whose offsets are `lo` and `hi`, cut to the arrays and to max_length whatever
+// these are.
+struct SequenceRows {
+  int64_t begin, length;
+  constexpr SequenceRows(int64_t lo, int64_t hi, int64_t rows, int64_t max_length) : begin(inside(lo, rows)), length(inside(hi, rows) - begin) {
+    length = length < 0 ? 0 : length > max_length ? max_length : length;
+  }
+  static constexpr int64_t inside(int64_t row, int64_t rows) { return row < 0 ? 0 : row > rows ? rows : row; }
+};
 
 // Byte offsets of a lane's steps in the buffer of its wavefront's rows, which holds rows * stride bytes.  A lane asks for
 // all the steps of its shape, also for those that it does not have: these have to lie behind the buffer's end, where nothing
