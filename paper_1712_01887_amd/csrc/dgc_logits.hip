@@ -66,8 +66,8 @@ struct Row {
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(four, v), g, offset(thread, i), 0, 0);
   }
   __device__ __forceinline__ void read_rest(const T* z, int vocab) {
-    const int at = vocab / E * E + (int)threadIdx.x;
-    rest = z && at < vocab ? to_float(z[at]) : -kInf;
+    const uint32_t at = (uint32_t)(vocab / E * E) + threadIdx.x;  // may pass 2^31
+    rest = z && at < (uint32_t)vocab ? to_float(z[at]) : -kInf;
   }
   __device__ __forceinline__ void read(__amdgpu_buffer_rsrc_t from) {
 #pragma unroll
@@ -257,9 +257,9 @@ __device__ __forceinline__ void select_exactly(const T* z, int vocab, int k, Top
   for (int shift = 24; shift >= 0; shift -= 8) {
     for (int i = threadIdx.x; i < 256; i += NT) s.histogram[i] = 0;
     __syncthreads();
-    for (int first = 0; first < vocab; first += NT) {
-      const int j = first + (int)threadIdx.x;
-      const uint32_t key = j < vocab ? order_key(to_float(z[j])) : 0u;
+    for (uint32_t first = 0; first < (uint32_t)vocab; first += NT) {
+      const uint32_t j = first + threadIdx.x;
+      const uint32_t key = j < (uint32_t)vocab ? order_key(to_float(z[j])) : 0u;
       const bool counts = key != 0 && (shift == 24 || key >> (shift + 8) == prefix);
       const uint32_t bin = (key >> shift) & 255u;
       const unsigned long long all = __ballot(counts);
@@ -290,9 +290,9 @@ __device__ __forceinline__ void select_exactly(const T* z, int vocab, int k, Top
   if (threadIdx.x == 0) s.count = 0;
   __syncthreads();
   uint32_t seen = 0;  // equal ones before this turn, in ascending order
-  for (int first = 0; first < vocab; first += NT) {
-    const int j = first + (int)threadIdx.x;
-    const uint32_t key = j < vocab ? order_key(to_float(z[j])) : 0u;
+  for (uint32_t first = 0; first < (uint32_t)vocab; first += NT) {
+    const uint32_t j = first + threadIdx.x;
+    const uint32_t key = j < (uint32_t)vocab ? order_key(to_float(z[j])) : 0u;
     const unsigned long long equal = __ballot(key == prefix);
     bool taken = key > prefix;
     if (seen < wanted) {
@@ -306,7 +306,7 @@ __device__ __forceinline__ void select_exactly(const T* z, int vocab, int k, Top
       taken |= key == prefix && at < wanted;
       __syncthreads();
     }
-    if (taken) s.candidates[atomicAdd(&s.count, 1u)] = (unsigned long long)key << 32 | (uint32_t)~j;
+    if (taken) s.candidates[atomicAdd(&s.count, 1u)] = (unsigned long long)key << 32 | ~j;
   }
   __syncthreads();
 }
@@ -599,7 +599,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
     if (MODE == kOnce) cs += ch;  // one exponential stands for both
     const T* z_next = next_weight != 0.0f ? static_cast<const T*>(a.logits) + next * a.row_stride : nullptr;
     const __amdgpu_buffer_rsrc_t from = Row<T, NT, CH>::buffer(z_next, a.vocab);
-    const int whole = a.vocab / E, behind = whole * E + (int)threadIdx.x;
+    const uint32_t behind = (uint32_t)(a.vocab / E * E) + threadIdx.x;
     uint32_t thread = threadIdx.x;
     asm volatile("" : "+v"(thread));  // offsets of vectors are counted anew for every row, not kept in registers
     auto value = [&](float zj) {
@@ -616,7 +616,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
         return out;
       };
       if (!live)  // (what the sweep below forms of such a row is not stored)
-        for (int j = threadIdx.x; j < a.vocab; j += NT) grad[j] = from_float<T>(0.0f);
+        for (uint32_t j = threadIdx.x; j < (uint32_t)a.vocab; j += NT) grad[j] = from_float<T>(0.0f);
       if constexpr (CH > 0) {  // the next row comes in where this one goes out
         const __amdgpu_buffer_rsrc_t to = Row<T, NT, CH>::buffer(live ? grad : nullptr, a.vocab);
 #pragma unroll
@@ -630,7 +630,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
           reinterpret_cast<typename Row<T, NT, CH>::Loose*>(grad + (uint32_t)number * (uint32_t)E)->v = of(v);
         });
       }
-      if (live && behind < a.vocab) grad[behind] = from_float<T>(value(row.rest - shift));
+      if (live && behind < (uint32_t)a.vocab) grad[behind] = from_float<T>(value(row.rest - shift));
     } else {
 #pragma unroll
       for (int i = 0; i < CH; ++i) row.read(from, thread, i);
