@@ -518,10 +518,10 @@ class Distillation(_Plan):
     def __init__(self, rows: int, vocab: int, dtype, device="cuda"):
         self.lib = load()
         self.rows, self.vocab, self.dtype = int(rows), int(vocab), dtype
-        self._shape = DgcLogits(_dtype_code(dtype), 0, self.rows, self.vocab, self.vocab)
-        self._shape_ref = C.byref(self._shape)
+        self._code = _dtype_code(dtype)
+        self._whole = C.byref(DgcLogits(self._code, 0, self.rows, self.vocab, self.vocab))
         b = C.c_size_t()
-        _check(self.lib.dgc_logits_workspace_bytes(self._shape_ref, C.byref(b)), "dgc_logits_workspace_bytes")
+        _check(self.lib.dgc_logits_workspace_bytes(self._whole, C.byref(b)), "dgc_logits_workspace_bytes")
         self._on(device)
         self._allocate(int(b.value))
 
@@ -532,20 +532,23 @@ class Distillation(_Plan):
                 torch.empty(self.rows, k, dtype=torch.float32, device=self.device),
                 torch.empty(self.rows, dtype=torch.float32, device=self.device))
 
-    def _set_shape(self, logits) -> int:
+    def _shape_of(self, logits):
+        """(rows, the shape that the library reads) of a call: its own, or the plan's, which no call writes to: the library
+        reads it without the interpreter's lock, when another thread may be in a call of the same plan."""
         rows = logits.shape[0]
         if rows > self.rows:
             raise DgcError(DGC_ERR_CAPACITY, f"{rows} rows in a plan for {self.rows}")
-        self._shape.rows = rows
-        self._shape.row_stride = _rows_of(logits, "logits", self.dtype, (rows, self.vocab), self._index)
-        return rows
+        stride = _rows_of(logits, "logits", self.dtype, (rows, self.vocab), self._index)
+        if rows == self.rows and stride == self.vocab:
+            return rows, self._whole
+        return rows, C.byref(DgcLogits(self._code, 0, rows, self.vocab, stride))
 
     def dgc_top_logits(self, logits, out_idx, out_val, out_lse=None, temperature: float = 1.0) -> None:
         """The k largest logits of every row (k = out_idx.shape[1]) and, if wanted, the rows' log-sum-exp."""
-        rows, k, dev = self._set_shape(logits), out_idx.shape[-1], self._index
+        (rows, shape), k, dev = self._shape_of(logits), out_idx.shape[-1], self._index
         pairs = (rows, k)
         status = self.lib.dgc_top_logits(
-            self._shape_ref, logits.data_ptr(), temperature, k, _dense(out_idx, "out_idx", self._i32, pairs, dev),
+            shape, logits.data_ptr(), temperature, k, _dense(out_idx, "out_idx", self._i32, pairs, dev),
             _dense(out_val, "out_val", self._f32, pairs, dev), _dense(out_lse, "out_lse", self._f32, (rows,), dev),
             self._ws_ptr, self._ws_bytes, self._stream())
         if status:
@@ -555,14 +558,14 @@ class Distillation(_Plan):
                          temperature: float = 1.0, hard_weight: float = 0.0, diag_flags=None) -> None:
         """loss (or None) and grad (or None; may be `logits`) of every row; see the header for the formulas.
         top_idx and top_val may both be None: no teacher, hard labels alone."""
-        rows, dev, f32, i32 = self._set_shape(logits), self._index, self._f32, self._i32
+        (rows, shape), dev, f32, i32 = self._shape_of(logits), self._index, self._f32, self._i32
         k = 0 if top_idx is None else top_idx.shape[-1]
         if (top_idx is None) != (top_val is None):
             raise DgcError(DGC_ERR_INVALID_ARG, "top_idx and top_val: one without the other")
         one, pairs = (rows,), (rows, k)
         stride = self.vocab if grad is None else _rows_of(grad, "grad", self.dtype, (rows, self.vocab), dev)
         status = self.lib.dgc_distill_loss(
-            self._shape_ref, logits.data_ptr(), k, _dense(top_idx, "top_idx", i32, pairs, dev),
+            shape, logits.data_ptr(), k, _dense(top_idx, "top_idx", i32, pairs, dev),
             _dense(top_val, "top_val", f32, pairs, dev), _dense(top_lse, "top_lse", f32, one, dev),
             _dense(labels, "labels", i32, one, dev), _dense(row_weight, "row_weight", f32, one, dev), temperature,
             hard_weight, _dense(loss, "loss", f32, one, dev), 0 if grad is None else grad.data_ptr(), stride,
