@@ -423,10 +423,11 @@ constexpr int kShort = 4;
 constexpr int kShortThreads = 256;
 
 template <typename T, int VEC, bool FREE, bool REVERSE>
-__global__ __launch_bounds__(kShortThreads) void scan_short_kernel(ScanArgs a) {
+__global__ __launch_bounds__(kShortThreads) void scan_short_kernel(ScanArgs a, uint32_t first) {
   const uint32_t groups = (uint32_t)((a.channels / VEC + kShortThreads - 1) / kShortThreads);  // of a sequence
-  const int64_t s = blockIdx.x / groups;
-  const int64_t d = ((int64_t)(blockIdx.x - (uint32_t)s * groups) * kShortThreads + threadIdx.x) * VEC;
+  const uint32_t number = first + blockIdx.x;
+  const int64_t s = number / groups;
+  const int64_t d = ((int64_t)(number - (uint32_t)s * groups) * kShortThreads + threadIdx.x) * VEC;
   if (d >= a.channels) return;
   int64_t begin, length;
   sequence_rows(a, s, begin, length);
@@ -503,25 +504,25 @@ __global__ __launch_bounds__(kShortThreads) void scan_short_kernel(ScanArgs a) {
 // (Two wavefronts of a SIMD at least: left to itself the compiler takes registers for one, and tiles of twice as many steps
 // are no better either: 512 sequences of 128 x 2048 in bfloat16 188 and 430 us so, 152 and 334 as it is.)
 template <typename TILE, int W>
-__global__ __launch_bounds__(W * 64, 2) void scan_walk_kernel(ScanArgs a) {
+__global__ __launch_bounds__(W * 64, 2) void scan_walk_kernel(ScanArgs a, uint32_t first) {
   using SHAPE = typename TILE::SHAPE;
   constexpr int VEC = SHAPE::kVec, kBlock = SHAPE::kBlock, kRows = W * SHAPE::kRows;
   __shared__ typename TILE::Parts parts[2];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane % SHAPE::kLanes * VEC;
   const uint32_t blocks = (uint32_t)((a.channels + kBlock - 1) / kBlock);
-  const uint32_t s = blockIdx.x / blocks;
+  const uint32_t s = (first + blockIdx.x) / blocks, block = first + blockIdx.x - s * blocks;
   int64_t begin, length;
   sequence_rows(a, s, begin, length);
   const int64_t count = length > 0 ? (length + kRows - 1) / kRows : 1;
-  const int64_t d = (int64_t)(blockIdx.x - s * blocks) * kBlock + col;
+  const int64_t d = (int64_t)block * kBlock + col;
   float carry[VEC];
 #pragma unroll
   for (int j = 0; j < VEC; ++j) carry[j] = a.first && d + j < a.channels ? a.first[s * a.channels + d + j] : 0.0f;
   for (int64_t i = 0; i < count; ++i) {
     const int64_t index = TILE::kReverse ? count - 1 - i : i;
     const Place p{begin + index * kRows, length - index * kRows, state_row(s, begin, index * (kRows / kStateRows)), s, 0, i,
-                  (int32_t)(blockIdx.x - s * blocks), 0, 1};
+                  (int32_t)block, 0, 1};
     const Share h = share_of<SHAPE>(a, p, w, lane);
     typename TILE::Input in;
     TILE tile;
@@ -750,6 +751,18 @@ __global__ __launch_bounds__(W * 64 + TILE::kBlock, RESIDENT) void scan_chain_ke
 constexpr int kTileRows = 128;
 constexpr int kChainGroups = 4 * 256;
 
+// A launch has less than 2^32 threads: workgroups beyond them, of many short sequences, are launched behind the others.
+template <int THREADS>
+hipError_t launch_all(void (*kernel)(ScanArgs, uint32_t), const ScanArgs& a, int64_t groups, hipStream_t stream) {
+  constexpr int64_t kMost = (int64_t)UINT32_MAX / THREADS;
+  for (int64_t first = 0; first < groups; first += kMost) {
+    kernel<<<dim3((uint32_t)(groups - first < kMost ? groups - first : kMost)), THREADS, 0, stream>>>(a, (uint32_t)first);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 template <template <typename, int, bool> class TILE, typename SHAPE, bool FREE>
 hipError_t launch_tiles(const ScanArgs& a, void* workspace, hipStream_t stream) {
   const int64_t blocks = ceil_div(a.channels, SHAPE::kBlock);
@@ -757,13 +770,11 @@ hipError_t launch_tiles(const ScanArgs& a, void* workspace, hipStream_t stream) 
   if (a.max_length <= kShort) {
     using T = typename SHAPE::T;
     const int64_t groups = ceil_div(a.channels / SHAPE::kVec, kShortThreads) * a.sequences;
-    scan_short_kernel<T, SHAPE::kVec, FREE, TILE<SHAPE, kWaves, FREE>::kReverse><<<dim3((uint32_t)groups), kShortThreads, 0, stream>>>(a);
-    return hipGetLastError();
+    return launch_all<kShortThreads>(scan_short_kernel<T, SHAPE::kVec, FREE, TILE<SHAPE, kWaves, FREE>::kReverse>, a, groups, stream);
   }
   if (!scan_chained(a)) {
     constexpr int W = SHAPE::kStateWaves;
-    scan_walk_kernel<TILE<SHAPE, W, FREE>, W><<<dim3((uint32_t)(a.sequences * blocks)), W * 64, 0, stream>>>(a);
-    return hipGetLastError();
+    return launch_all<W * 64>(scan_walk_kernel<TILE<SHAPE, W, FREE>, W>, a, a.sequences * blocks, stream);
   }
   Chain chain{};
   chain.ticket = static_cast<uint32_t*>(workspace);
