@@ -483,6 +483,8 @@ dgc_status dgc_top_logits(const dgc_logits* shape, const void* logits, float tem
  *   grad[r][j] = w_r ((1 - a) T (q_j sum_p P_p - [j = i_p] P_p) + a (softmax(z)_j - [j = y]))
  *   top_idx, top_val  device, int32 / float[rows * k], k from 0 to DGC_TOP_MAX; the indices of a row are distinct; a
  *               negative one stands for no pair.  A row without pairs has no KL term
+ *   hard_weight  0: the labels are not looked at; 1: the pairs count nothing, also where KL is infinite (a pair whose
+ *               logit is -inf); their indices are looked at for the flag below
  *   labels      device, int32[rows], or NULL when hard_weight = 0; a negative one stands for no label (no CE term)
  *   row_weight  device, float[rows], or NULL for ones: a mask, a mean's 1 / rows, an incoming gradient.  A row of
  *               weight zero, and one whose logits are all -inf, has loss and gradient zero, whatever else it holds

@@ -513,7 +513,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
         const int p = i * 64 + lane;
         at[i] = p < a.k ? a.top_idx[r * a.k + p] : -1;
         bad |= at[i] >= a.vocab;
-        if (at[i] >= a.vocab) at[i] = -1;
+        if (at[i] >= a.vocab || a.hard_weight == 1.0f) at[i] = -1;  // without weight, also an infinite divergence counts nothing
         t[i] = at[i] >= 0 ? a.top_val[r * a.k + p] * inv_tau : -kInf;
         z_at[i] = at[i] >= 0 ? to_float(z[at[i]]) : 0.0f;
         named |= at[i] >= 0 && at[i] == y;
