@@ -466,7 +466,7 @@ dgc_status dgc_logits_workspace_bytes(const dgc_logits* shape, size_t* bytes);
  *            never chosen; where fewer than k others are left, the pairs behind them are (-1, -inf)
  *   out_lse  device, float[rows], or NULL: log sum_j exp(logits[r][j] / temperature) over the whole row (-inf
  *            where the row is nothing but -inf, NaN where it holds a NaN or +inf)
- *   temperature  > 0, finite; changes out_lse only
+ *   temperature  > 0, finite, log2(e) / temperature finite in binary32 (above some 4.3e-39); changes out_lse only
  *   workspace    device, >= dgc_logits_workspace_bytes, 256-byte aligned
  * Errors: INVALID_ARG, ALIGNMENT (an element straddles its own size; workspace), CAPACITY (workspace, rows), HIP.
  */

@@ -21,6 +21,9 @@ bool type_known(int32_t dtype) { return dtype == DGC_F32 || dtype == DGC_F16 || 
 // rows * stride elements must have an address
 bool addressable(int64_t rows, int64_t stride) { return rows == 0 || stride <= ((int64_t)1 << 60) / rows; }
 
+// The kernels take exponentials as powers of two, of logits times log2(e) / temperature.
+bool temperature_fits(float t) { return t > 0.0f && std::isfinite(t) && std::isfinite(1.0f / t * 1.44269504f); }
+
 dgc_status check_logits(const dgc_logits* s) {
   if (!s || !type_known(s->dtype) || s->reserved != 0) return DGC_ERR_INVALID_ARG;
   if (s->rows < 0 || s->vocab < 1 || s->row_stride < s->vocab) return DGC_ERR_INVALID_ARG;
@@ -75,7 +78,7 @@ dgc_status dgc_top_logits(const dgc_logits* shape, const void* logits, float tem
                           float* out_val, float* out_lse, void* workspace, size_t workspace_bytes, void* stream_) {
   dgc_status st = check_logits(shape);
   if (st != DGC_OK) return st;
-  if (k < 1 || k > DGC_TOP_MAX || !(temperature > 0.0f) || !std::isfinite(temperature)) return DGC_ERR_INVALID_ARG;
+  if (k < 1 || k > DGC_TOP_MAX || !temperature_fits(temperature)) return DGC_ERR_INVALID_ARG;
   if (shape->rows == 0) return DGC_OK;
   if (!logits || !out_idx || !out_val) return DGC_ERR_INVALID_ARG;
   if (!aligned_to(logits, element_bytes(shape->dtype)) || !aligned_to(out_idx, 4) || !aligned_to(out_val, 4) ||
@@ -104,7 +107,7 @@ dgc_status dgc_distill_loss(const dgc_logits* shape, const void* logits, int32_t
                             void* stream_) {
   dgc_status st = check_logits(shape);
   if (st != DGC_OK) return st;
-  if (k < 0 || k > DGC_TOP_MAX || !(temperature > 0.0f) || !std::isfinite(temperature)) return DGC_ERR_INVALID_ARG;
+  if (k < 0 || k > DGC_TOP_MAX || !temperature_fits(temperature)) return DGC_ERR_INVALID_ARG;
   if (!(hard_weight >= 0.0f) || !(hard_weight <= 1.0f) || (hard_weight > 0.0f && !labels)) return DGC_ERR_INVALID_ARG;
   if (!loss && !grad) return DGC_ERR_INVALID_ARG;
   if (grad && grad_stride < shape->vocab) return DGC_ERR_INVALID_ARG;
