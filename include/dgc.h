@@ -455,7 +455,7 @@ typedef struct dgc_logits {
   int64_t row_stride; /* >= vocab, in elements            */
 } dgc_logits;
 
-/* Bytes of device workspace dgc_top_logits and dgc_distill_loss need for logits of this shape (any k). */
+/* Bytes of device workspace dgc_top_logits and dgc_distill_loss need for logits of this shape (any k): none. */
 dgc_status dgc_logits_workspace_bytes(const dgc_logits* shape, size_t* bytes);
 
 /*
@@ -467,8 +467,8 @@ dgc_status dgc_logits_workspace_bytes(const dgc_logits* shape, size_t* bytes);
  *   out_lse  device, float[rows], or NULL: log sum_j exp(logits[r][j] / temperature) over the whole row (-inf
  *            where the row is nothing but -inf, NaN where it holds a NaN or +inf)
  *   temperature  > 0, finite, log2(e) / temperature finite in binary32 (above some 4.3e-39); changes out_lse only
- *   workspace    device, >= dgc_logits_workspace_bytes, 256-byte aligned
- * Errors: INVALID_ARG, ALIGNMENT (an element straddles its own size; workspace), CAPACITY (workspace, rows), HIP.
+ *   workspace    not looked at while dgc_logits_workspace_bytes is zero; may be NULL
+ * Errors: INVALID_ARG, ALIGNMENT (an element straddles its own size), CAPACITY (rows, vocab, or rows * row_stride), HIP.
  */
 dgc_status dgc_top_logits(const dgc_logits* shape, const void* logits, float temperature, int32_t k, int32_t* out_idx,
                           float* out_val, float* out_lse, void* workspace, size_t workspace_bytes, void* stream);

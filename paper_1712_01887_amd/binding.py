@@ -484,7 +484,7 @@ def _dense(t, name: str, dtype, shape, index: int) -> int:
 
 
 class _Plan:
-    """What the plans below share: a device, and a workspace on it, aligned as the library wants it."""
+    """What the plans below share: a device, and the stream that is current on it."""
 
     def _on(self, device) -> None:
         import torch
@@ -497,12 +497,6 @@ class _Plan:
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self._current = torch.cuda.current_device
 
-    def _allocate(self, nbytes: int) -> None:
-        import torch
-        self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device) if nbytes else None
-        self._ws_ptr = (self.workspace.data_ptr() + 255) // 256 * 256 if nbytes else 0
-        self._ws_bytes = nbytes
-
     def _stream(self) -> int:
         """The current stream of the plan's device, which has to be the current one."""
         if self._current() != self._index:
@@ -513,7 +507,8 @@ class _Plan:
 class Distillation(_Plan):
     """Rows of logits over one vocabulary: a teacher's pairs, and a student's loss and gradient against such pairs.
 
-    `rows`: of a call at most.  The plan owns a workspace: its calls belong on one stream (or are ordered by events)."""
+    `rows`: of a call at most.  The plan holds sizes only, no workspace: its calls may run on any streams, from any
+    threads."""
 
     def __init__(self, rows: int, vocab: int, dtype, device="cuda"):
         self.lib = load()
@@ -521,9 +516,8 @@ class Distillation(_Plan):
         self._code = _dtype_code(dtype)
         self._whole = C.byref(DgcLogits(self._code, 0, self.rows, self.vocab, self.vocab))
         b = C.c_size_t()
-        _check(self.lib.dgc_logits_workspace_bytes(self._whole, C.byref(b)), "dgc_logits_workspace_bytes")
+        _check(self.lib.dgc_logits_workspace_bytes(self._whole, C.byref(b)), "dgc_logits_workspace_bytes")   # checks the shape
         self._on(device)
-        self._allocate(int(b.value))
 
     def alloc_top_logits(self, k: int):
         """(out_idx, out_val, out_lse) for `rows` rows of k pairs."""
@@ -550,7 +544,7 @@ class Distillation(_Plan):
         status = self.lib.dgc_top_logits(
             shape, logits.data_ptr(), temperature, k, _dense(out_idx, "out_idx", self._i32, pairs, dev),
             _dense(out_val, "out_val", self._f32, pairs, dev), _dense(out_lse, "out_lse", self._f32, (rows,), dev),
-            self._ws_ptr, self._ws_bytes, self._stream())
+            0, 0, self._stream())
         if status:
             _check(status, "dgc_top_logits")
 
@@ -569,7 +563,7 @@ class Distillation(_Plan):
             _dense(top_val, "top_val", f32, pairs, dev), _dense(top_lse, "top_lse", f32, one, dev),
             _dense(labels, "labels", i32, one, dev), _dense(row_weight, "row_weight", f32, one, dev), temperature,
             hard_weight, _dense(loss, "loss", f32, one, dev), 0 if grad is None else grad.data_ptr(), stride,
-            _dense(diag_flags, "diag_flags", i32, (1,), dev), self._ws_ptr, self._ws_bytes, self._stream())
+            _dense(diag_flags, "diag_flags", i32, (1,), dev), 0, 0, self._stream())
         if status:
             _check(status, "dgc_distill_loss")
 
@@ -604,7 +598,9 @@ class GatedScan(_Plan):
         self.state_rows = int(n.value)
         self._steps, self._carried = (self.rows, self.channels), (self.sequences, self.channels)
         self._kept = (self.state_rows, self.channels)
-        self._allocate(int(b.value))
+        self._ws_bytes = int(b.value)
+        self.workspace = torch.empty(self._ws_bytes + 256, dtype=torch.uint8, device=self.device) if self._ws_bytes else None
+        self._ws_ptr = (self.workspace.data_ptr() + 255) // 256 * 256 if self._ws_bytes else 0   # as the library wants it
 
     def alloc_states(self):
         """What a forward call leaves for the backward call of the same inputs."""

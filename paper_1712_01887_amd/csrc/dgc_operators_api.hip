@@ -60,8 +60,6 @@ dgc_status check_scan(const dgc_scan* s) {
 
 int64_t state_rows(const dgc_scan* s) { return s->rows / DGC_SCAN_STATE_ROWS + s->sequences; }
 
-size_t logits_workspace(const dgc_logits*) { return 0; }
-
 }  // namespace
 
 extern "C" {
@@ -70,13 +68,13 @@ dgc_status dgc_logits_workspace_bytes(const dgc_logits* shape, size_t* bytes) {
   const dgc_status st = check_logits(shape);
   if (st != DGC_OK) return st;
   if (!bytes) return DGC_ERR_INVALID_ARG;
-  *bytes = logits_workspace(shape);
+  *bytes = 0;  // all of a row's work is one workgroup's
   return DGC_OK;
 }
 
 dgc_status dgc_top_logits(const dgc_logits* shape, const void* logits, float temperature, int32_t k, int32_t* out_idx,
-                          float* out_val, float* out_lse, void* workspace, size_t workspace_bytes, void* stream_) {
-  dgc_status st = check_logits(shape);
+                          float* out_val, float* out_lse, void* /*workspace*/, size_t /*workspace_bytes*/, void* stream_) {
+  const dgc_status st = check_logits(shape);
   if (st != DGC_OK) return st;
   if (k < 1 || k > DGC_TOP_MAX || !temperature_fits(temperature)) return DGC_ERR_INVALID_ARG;
   if (shape->rows == 0) return DGC_OK;
@@ -84,7 +82,6 @@ dgc_status dgc_top_logits(const dgc_logits* shape, const void* logits, float tem
   if (!aligned_to(logits, element_bytes(shape->dtype)) || !aligned_to(out_idx, 4) || !aligned_to(out_val, 4) ||
       !aligned_to(out_lse, 4))
     return DGC_ERR_ALIGNMENT;
-  if ((st = check_workspace(workspace, workspace_bytes, logits_workspace(shape))) != DGC_OK) return st;
   TopArgs a{};
   a.logits = logits;
   a.row_stride = shape->row_stride;
@@ -103,9 +100,9 @@ dgc_status dgc_top_logits(const dgc_logits* shape, const void* logits, float tem
 dgc_status dgc_distill_loss(const dgc_logits* shape, const void* logits, int32_t k, const int32_t* top_idx,
                             const float* top_val, const float* top_lse, const int32_t* labels,
                             const float* row_weight, float temperature, float hard_weight, float* loss, void* grad,
-                            int64_t grad_stride, uint32_t* diag_flags_dev, void* workspace, size_t workspace_bytes,
+                            int64_t grad_stride, uint32_t* diag_flags_dev, void* /*workspace*/, size_t /*workspace_bytes*/,
                             void* stream_) {
-  dgc_status st = check_logits(shape);
+  const dgc_status st = check_logits(shape);
   if (st != DGC_OK) return st;
   if (k < 0 || k > DGC_TOP_MAX || !temperature_fits(temperature)) return DGC_ERR_INVALID_ARG;
   if (!(hard_weight >= 0.0f) || !(hard_weight <= 1.0f) || (hard_weight > 0.0f && !labels)) return DGC_ERR_INVALID_ARG;
@@ -120,7 +117,6 @@ dgc_status dgc_distill_loss(const dgc_logits* shape, const void* logits, int32_t
       !aligned_to(top_lse, 4) || !aligned_to(labels, 4) || !aligned_to(row_weight, 4) || !aligned_to(loss, 4) ||
       !aligned_to(diag_flags_dev, 4))
     return DGC_ERR_ALIGNMENT;
-  if ((st = check_workspace(workspace, workspace_bytes, logits_workspace(shape))) != DGC_OK) return st;
   DistillArgs a{};
   a.logits = logits;
   a.grad = grad;
