@@ -552,7 +552,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
         float log_p[kPairs], from;
         if (a.top_lse) {
           from = a.top_lse[r];
-        } else {
+        } else {  // from their largest on: rounded beside it, the logarithm of their sum would move all shares alike
           float tm = t[0];
 #pragma unroll
           for (int i = 1; i < kPairs; ++i) tm = fmaxf(tm, t[i]);
@@ -560,9 +560,12 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
           tm = tm == -kInf ? 0.0f : tm;
           float total = 0.0f;
 #pragma unroll
-          for (int i = 0; i < kPairs; ++i) total += at[i] >= 0 ? __expf(t[i] - tm) : 0.0f;
+          for (int i = 0; i < kPairs; ++i) {
+            t[i] -= tm;
+            total += at[i] >= 0 ? __expf(t[i]) : 0.0f;
+          }
           total = wave_sum_f(total);
-          from = tm + (total > 0.0f ? __logf(total) : 0.0f);
+          from = total > 0.0f ? __logf(total) : 0.0f;
         }
         float mass = 0.0f, kl = 0.0f;  // of the divergence, what does not need the row's sum
 #pragma unroll
