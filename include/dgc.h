@@ -478,6 +478,7 @@ dgc_status dgc_top_logits(const dgc_logits* shape, const void* logits, float tem
  *   q   = softmax(z / T) over the row,     P_p = exp(t_p / T - c),
  *         c = top_lse[r] (the teacher's whole row, as dgc_top_logits leaves it for the same temperature), or, with
  *         top_lse = NULL, the log-sum-exp of the t_p / T themselves, so that the P_p add up to one
+ *         (with top_lse what the teacher has outside its pairs is left out of KL, which may be negative then)
  *   KL  = sum_p P_p (log P_p - log q[i_p]),     CE = log sum_j exp(z_j) - z_y
  *   loss[r]    = w_r ((1 - a) T^2 KL + a CE)
  *   grad[r][j] = w_r ((1 - a) T (q_j sum_p P_p - [j = i_p] P_p) + a (softmax(z)_j - [j = y]))
@@ -528,14 +529,16 @@ dgc_status dgc_gated_scan_state_rows(const dgc_scan* shape, int64_t* state_rows)
 
 /*
  *   a = sigmoid(gate),  b = 1 - a (or 1),  h_t = a_t h_{t-1} + b_t x_t    for every channel of every sequence
- * A gate of -inf starts the state again, one of +inf keeps it.
+ * A gate of -inf starts the state again, one of +inf keeps it; a state that is not finite stays so to the sequence's end (0
+ * times an infinity is a NaN), and whether as an infinity or a NaN is not told.
  *   gate, x, h  device, rows gate_stride, x_stride, h_stride elements apart (each >= channels)
  *   h0          device, float[sequences * channels], or NULL for zeros
  *   h_last      device, float[same], or NULL: the state behind the last step (h0 where a sequence has no step); may
  *               be h0 itself: a serving loop calls this with max_length = 1 and one state array
  *   states      device, float[state_rows * channels], or NULL: what dgc_gated_scan_backward needs
  * h must not overlap gate or x unless it is one of them, address and stride.
- * Errors: INVALID_ARG, ALIGNMENT, CAPACITY (workspace; channels or strides of 2^24 and more), HIP.
+ * Errors: INVALID_ARG, ALIGNMENT, CAPACITY (workspace; channels or strides of 2^24 and more, sequences or max_length of
+ * 2^31, rows of 2^40, and shapes of 2^31 workgroups or more), HIP.
  */
 dgc_status dgc_gated_scan_forward(const dgc_scan* shape, const void* gate, int64_t gate_stride, const void* x,
                                   int64_t x_stride, const float* h0, void* h, int64_t h_stride, float* h_last,

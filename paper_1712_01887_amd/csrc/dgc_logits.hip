@@ -317,8 +317,9 @@ __device__ __forceinline__ void select_exactly(const T* z, int vocab, int k, Top
 // their elements that reach the last floor, and these are ranked by counting.  Each logit is read once, and takes a maximum
 // and, for the log-sum-exp, an exponential against the thread's own largest so far.
 //   4096 x 131072 in bfloat16, 64 pairs: 218 us, 4.9 TB/s of 6.5 that a bare kernel reaches.  A row held in registers as a
-//   whole took 302: nothing was on its way while it was ranked.  8 x 32768 7.1 us, 700 x 10000 in 32 bits 15.4: a row's chain
-//   of piece, floor, list and rank, about 5 us behind its loads.
+//   whole took 302: nothing was on its way while it was ranked.  8 x 32768 7.1 us, 700 x 10000 in 32 bits 14.3: a row's chain
+//   of piece, floor, list and rank, about 5 us behind its loads.  Few rows leave most of the device idle, as a row is one
+//   workgroup's: 1 x 131072 takes 18 us, to 256 pairs 32.  With 512 threads 7 to 13 registers are spilled (24 to 48 bytes of scratch).
 template <typename T, int NT, int CH>
 __global__ __launch_bounds__(NT, NT < 512 || CH > 4 ? 4 : 6) void top_logits_kernel(TopArgs a) {
   using Piece = Row<T, NT, CH>;
@@ -469,16 +470,19 @@ struct DistillShared {
   float z_at[DGC_TOP_MAX], p[DGC_TOP_MAX];
 };
 
-// One workgroup takes a row at a time and reads it once: largest logit, sum of exponentials, gradient, all from registers, with
-// two exchanges through LDS.  The first wavefront sees to the pairs in between (their logits are gathered while the row
-// comes in), and writes the few elements that pairs and the label name once more behind the others.
-//   4096 x 131072 in bfloat16, loss and gradient, a temperature of two and hard labels: 499 us, 4.3 TB/s (2.1 GB; with the row
+// One workgroup takes a row at a time and, with CH > 0, reads it once: largest logit, sum of exponentials, gradient, all from
+// registers, with two exchanges through LDS.  The first wavefront sees to the pairs in between (their logits are gathered while
+// the row comes in), and writes the few elements that pairs and the label name once more behind the others.
+//   4096 x 131072 in bfloat16, loss and gradient, a temperature of two and hard labels: 500 us, 4.3 TB/s (2.1 GB; with the row
 //   read three times and 256 threads 1862).  Such a row takes half the registers of a compute unit, so that only one is there:
 //   its loads go out while the row before it is stored, but the exchanges stand alone, and the arithmetic, some 23
-//   instructions an element, is 310 us of the whole.  The loss alone 254 us, 4.2 TB/s.  1111 x 32771 in binary16 50 us (146 MB),
+//   instructions an element, is 310 us of the whole.  The loss alone 256 us, 4.2 TB/s.  1111 x 32771 in binary16 50 us (146 MB),
 //   20 x 10000 in 32 bits 6.5.
+// With CH = 0, rows that registers do not hold are read three times (the loss alone: twice), the later times from nearer
+// memory in part, and nothing is on its way between two of them: 2048 x 131072 in 32 bits 642 us and the loss alone 307 (2.1 and
+// 1.1 GB to move: 3.3 and 3.5 TB/s), 2048 x 140000 in bfloat16 395 and 194 (2.9 TB/s).
 // The exponentials of an element at the temperature and without one: not needed or the same, the square of the first (a
-// temperature of two), or one of its own.
+// temperature of two: 500 us where one of its own takes 525 for 4096 x 131072, 50.4 and 54.7 for 1111 x 32771), or one of its own.
 enum { kOnce, kSquare, kTwice };
 template <int MODE>
 __device__ __forceinline__ float2 powers(float z, float c) {
@@ -676,9 +680,9 @@ struct PickTop {
     if (vectors <= 64) DGC_ROW(64, 1);
     if (vectors <= 256) DGC_ROW(256, 1);
     if (vectors <= 1024) DGC_ROW(256, 4);
-    // Few rows: what one of them takes is what counts, so fewer pieces (333 rows of 10000 in 32 bits, 64 pairs: 10.2 us in
-    // pieces of 8 vectors a thread, 12.2 in pieces of 4).  Many: workgroups to a compute unit (4096 of 32000 in bfloat16, 64
-    // pairs: 80.9 and 78.1; 2048 of 131072, 256 pairs: 186 and 161; pieces of 8 to 256 threads 83.7 and 188).
+    // Few rows: what one of them takes is what counts, so fewer pieces (333 rows of 10000 in 32 bits, 64 pairs: 11.0 us in
+    // pieces of 8 vectors a thread, 12.4 in pieces of 4; 512 of 32000 in bfloat16 14.9 and 16.6).  Many: workgroups to a compute
+    // unit (1024 of those 27.4 and 24.7, 4096 77.6 and 74; 2048 of 131072, 256 pairs: 179 and 154).
     if (a.rows <= 2 * compute_units()) DGC_ROW(512, 8);
     DGC_ROW(512, 4);
 #undef DGC_ROW
@@ -691,9 +695,22 @@ struct PickDistill {
     const int64_t vectors = ceil_div(a.vocab, 16 / (int64_t)sizeof(T));
 #define DGC_ROW(NT, CH) return launch_rows<T, NT, CH, DistillArgs, &distill_kernel<T, NT, CH, MODE, GRAD>>(a, stream)
     // Few enough vectors to a thread that several rows are on a compute unit at a time, few enough threads that they do not wait
-    // for each other long.  In us, with 1024 threads for what is more than 1024 vectors, with 512 in steps of twice as many
-    // vectors, and as it is: 1024 x 50000 in bfloat16, the loss, 35.2, 28.1, 26.8; 1111 x 32771, loss and gradient, 68.6, 63.4, 50.0;
-    // 4096 x 131072 499, 506, 499.
+    // for each other long.  2048 rows, loss and gradient at a temperature of two with labels / the loss alone, in us:
+    //   vocabulary      512 x 6      512 x 10     512 x 14     1024 x 16    not held
+    //   16001 bfloat16  40 / 21      59 / 32      75 / 38      161 / 85     63 / 43
+    //   20000           40 / 22      59 / 31      75 / 40      161 / 81     63 / 42
+    //   32000                        67 / 33      83 / 41      161 / 83     98 / 52
+    //   40000                        77 / 37      91 / 41      165 / 85     117 / 53
+    //   50000                                     101 / 44     174 / 88     155 / 64
+    //   57000                                     112 / 46     181 / 90     175 / 70
+    //   64000                                                  186 / 93     194 / 80
+    //   100352                                                 225 / 114    284 / 142
+    //   131072                                                 266 / 128    357 / 177
+    //   10000 binary32  32 / 21      39 / 25      43 / 26      84 / 52      57 / 40
+    //   20000                        70 / 34      72 / 33      108 / 57     97 / 45
+    //   32768                                                  137 / 64     155 / 59
+    // Threads without a vector cost as much as the others: from one size to the next the time steps up, most behind 57344
+    // elements of 16 bits and 28672 of 32.  There the loss alone would do better without registers (64000 and 32768 above).
     if (vectors <= 64) DGC_ROW(64, 1);
     if (vectors <= 256) DGC_ROW(256, 1);
     if (vectors <= 1024) DGC_ROW(256, 4);

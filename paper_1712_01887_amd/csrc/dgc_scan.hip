@@ -417,8 +417,10 @@ struct BackwardTile {
 };
 
 // ---- a few steps: a thread walks VEC channels of one sequence --------------------------------------------------
-// What bounds this is the launch: 256 streams of 1500 channels in 32 bits, one step, took 20 us by tiles, of which a
-// wavefront uses one row then.
+// What bounds this is the launch: 256 streams of 1500 channels in 32 bits, one step, 3.0 us forward and 3.2 backward; by tiles,
+// of which a wavefront uses one row then, 19 and 37.  Four steps 4.8 and 6.2 us, by tiles 20 and 39.  Tiles do not win beyond
+// four either (five steps 21 and 40 us by them, 5.5 and 8.4 with room for 16 here, and 16 steps 22 and 40 against 14 and 21): the
+// limit keeps the registers of a single step few, which takes 3.4 and 4.2 us with room for 16 and 3.1 and 3.5 with room for 8.
 constexpr int kShort = 4;
 constexpr int kShortThreads = 256;
 
@@ -498,13 +500,13 @@ __global__ __launch_bounds__(kShortThreads) void scan_short_kernel(ScanArgs a, u
 }
 
 // ---- short sequences: a workgroup walks the tiles of one sequence and block ---------------------------------
-// One pass over the data: 512 sequences of 128 x 2048 in bfloat16 forward 153 us (5.3 TB/s), backward 331 (4.1); 20 x 35 x 1500 in
-// 32 bits 5.9 and 7.7, a launch and a chain of loads, steps, exchange and stores.  The backward pass is held up by its
-// registers (four to an element), which leave two wavefronts to a SIMD.
-// (Two wavefronts of a SIMD at least: left to itself the compiler takes registers for one, and tiles of twice as many steps
-// are no better either: 512 sequences of 128 x 2048 in bfloat16 188 and 430 us so, 152 and 334 as it is.)
+// One pass over the data: 512 sequences of 128 x 2048 in bfloat16 forward 153 us (5.3 TB/s), backward 258 (5.2); 20 x 35 x 1500 in
+// 32 bits 4.5 and 7.2, a launch and a chain of loads, steps, exchange and stores.  A tile has the rows of one kept state: with
+// twice as many 183 and 416 us, 6.0 and 12.5 (in 32 bits 512 x 128 x 1024 139 and 272, 149 and 249 as it is).  Backward, 170 to
+// 243 registers in 16 bits leave two wavefronts to a SIMD.  Of sequences shorter than 64 steps only a part of the rows is
+// there: 2048 x 32 x 2048 takes 204 and 484 us.
 template <typename TILE, int W>
-__global__ __launch_bounds__(W * 64, 2) void scan_walk_kernel(ScanArgs a, uint32_t first) {
+__global__ __launch_bounds__(W * 64) void scan_walk_kernel(ScanArgs a, uint32_t first) {
   using SHAPE = typename TILE::SHAPE;
   constexpr int VEC = SHAPE::kVec, kBlock = SHAPE::kBlock, kRows = W * SHAPE::kRows;
   __shared__ typename TILE::Parts parts[2];
@@ -670,9 +672,12 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 // Every element is read once: gates and inputs stay in registers (backward: the folded gates, and the states formed again)
-// while the chain brings the state.  65536 x 2048 in bfloat16, one sequence: forward 199 us (4.05 TB/s), backward 357 (3.8).
-// Two passes over the data would move 1.34 and 2.15 GB, 206 and 330 us at the 6.5 TB/s of a bare kernel.  What bounds it is
-// the chain: workgroups load side by side, all but the first of a group wait for what the others leave, and store side by side.
+// while the chain brings the state.  65536 x 2048 in bfloat16, one sequence, with the clear of the words (5.7 us): forward 197 us
+// (4.1 TB/s), backward 362 (3.7); 65536 x 1024 in 32 bits 179 and 306, 65536 x 2047 in bfloat16, two bytes a lane, 281 and 414.
+// What bounds it in 16 bits is that nothing covers a workgroup's wait for the chain: ten wavefronts of 97 or 98 registers
+// forward and of 168 backward (5 to 8 more of those are spilled, 24 to 36 bytes of scratch) leave room for one workgroup to a
+// compute unit, where 96 would for two, and all of them load, wait and store side by side.  Two passes over the data would
+// move 1.34 and 2.15 GB, 206 and 330 us at the 6.5 TB/s of a bare kernel.
 // Tried: the tile's own wavefronts seeing to the chain (224 to 247 and 332 to 357 us), tiles of 64 steps (288 and 397 at best), groups of
 // 8 and of 32 tiles (more hops, more words to read), tickets from several counters (240 to 292 and 348 to 390: rows of memory
 // are then read piece by piece), gates formed twice to have more workgroups (260 to 315 forward).
@@ -749,7 +754,7 @@ __global__ __launch_bounds__(W * 64 + TILE::kBlock, RESIDENT) void scan_chain_ke
 
 // Sequences of more steps than a tile holds are cut into tiles.
 constexpr int kTileRows = 128;
-constexpr int kChainGroups = 4 * 256;
+constexpr int kChainGroups = 4 * 256;  // more than are resident at a time: those that find no ticket left end at once
 
 // A launch has less than 2^32 threads: workgroups beyond them, of many short sequences, are launched behind the others.
 template <int THREADS>
@@ -821,10 +826,12 @@ int64_t scan_word_rows(const ScanArgs& a) {
 }
 
 // Long sequences are cut into tiles that wait for each other, unless there are so many of them (times blocks of 64
-// channels) that a workgroup to each fills the device, and none is much longer than the mean.  In us, tiles side by side and
-// one behind the other, forward / backward in bfloat16: 12 x 1500 x 1200 47/73 and 61/129, 24 (456 blocks) 80/155 and 70/167,
-// 48 155/277 and 140/243, 64 x 1024 x 2048 190/348 and 173/277, 48 of 187 to 1500 steps 108/188 and 97/168; in 32 bits 20 x
-// 200 x 1500 32/39 and 19/30.
+// channels, of which a workgroup has two in 16 bits at 8 or 4 bytes a lane) that walking them fills the device well enough, and
+// none is much longer than the mean.  In us, tiles side by side and one behind the other, forward / backward in bfloat16, by
+// that number: 228 (12 x 1500 x 1200) 45/71 and 59/127; 456 (24 of them) 78/151 and 68/163; 512 (16 x 1024 x 2048) 56/104 and
+// 45/108; 768 (24) 82/144 and 79/135; 912 (48 x 1500 x 1200) 155/276 and 141/251, of 187 to 1500 steps 111/183 and 95/169; 2048
+// (64 x 1024 x 2048) 191/350 and 172/277.  In 32 bits 480 (20 x 200 x 1500) 31/38 and 19/30.  Around the limit the two directions
+// do not agree, and sequences of two tiles would rather be walked below it as well: 192 (8 x 200 x 1500) 17/20 and 11/19.
 constexpr int64_t kWalkBlocks = 384;
 bool scan_chained(const ScanArgs& a) {
   if (a.max_length <= kTileRows) return false;
