@@ -559,6 +559,162 @@ dgc_status dgc_gated_scan_backward(const dgc_scan* shape, const void* gate, int6
                                    void* stream);
 
 /*
+ * ---- Recurrent language models with matrix states: their layers --------------------------------
+ *
+ * Under the conventions of the operators above.  Rows are tokens; a head's elements lie behind each other.
+ */
+
+/* Heads of rows: element j of head h of row r at data[r * row_stride + h * head_stride + j], strides in elements, >= 0.
+ * What is read may have a stride of 0 (heads or rows that share one vector); of what is written, no two elements may
+ * share an address: either a row's heads end before the next row begins, or a head's rows before the next head. */
+typedef struct dgc_heads {
+  void* data;
+  int64_t row_stride;
+  int64_t head_stride;
+} dgc_heads;
+
+#define DGC_HEAD_MAX 256   /* elements of a head at most                */
+#define DGC_ROTARY_MAX 4   /* arrays that one dgc_rotary call turns     */
+
+/* dgc_rotary.flags */
+enum {
+  DGC_ROTARY_HALF = 1u << 0,   /* pairs (i, i + rotary_dim / 2); otherwise (2 i, 2 i + 1)              */
+  DGC_ROTARY_INVERSE = 1u << 1 /* by the negative angle: the gradient of a call without this flag      */
+};
+
+typedef struct dgc_rotary_shape {
+  int32_t dtype;      /* DGC_F32, DGC_F16, DGC_BF16                                   */
+  uint32_t flags;     /* DGC_ROTARY_*                                                 */
+  int64_t rows;       /* >= 0, < 2^31                                                 */
+  int32_t head_dim;   /* 1 .. DGC_HEAD_MAX                                            */
+  int32_t rotary_dim; /* even, 0 .. head_dim: this many of a head's first elements are turned, the others copied */
+} dgc_rotary_shape;
+
+/*
+ * The frequencies f_i = base^(-2 i / rotary_dim), i < rotary_dim / 2, scaled for a context `factor` times as long as the
+ * original one of `context` positions: with n_i = context f_i / 2 pi turns in the original context and
+ * g_i = (n_i - low_turns) / (high_turns - low_turns) cut to [0, 1], f_i (g_i + (1 - g_i) / factor).  factor = 1 changes
+ * nothing, context = 0 divides all of them.
+ *   out  host, uint64[rotary_dim / 2]: fractions of a turn a position, in units of 2^-64, for a device array that the
+ *        calls below read
+ * Errors: INVALID_ARG (rotary_dim odd or outside 0 .. DGC_HEAD_MAX; base below 1, factor below 1 or context below 0 or not
+ * finite; low_turns < 0 or not below high_turns).
+ */
+dgc_status dgc_rotary_frequencies(int32_t rotary_dim, double base, double factor, double context, double low_turns,
+                                  double high_turns, uint64_t* out);
+
+/*
+ * Turns the pairs of every head by its row's position: (x, y) to m (x cos a - y sin a, x sin a + y cos a), a = position
+ * times frequency, taken modulo a turn in whole numbers: far positions lose nothing.
+ *   positions    device, int64[rows], of either sign (the angle is off by position * 2^-65 turns at most)
+ *   frequencies  device, uint64[rotary_dim / 2], 8-byte aligned; NULL where rotary_dim is 0
+ *   magnitude    m, finite
+ *   count, heads 1 .. DGC_ROTARY_MAX arrays (queries and keys, say) and the heads of each (1 .. 65535)
+ *   x, out       host, `count` descriptions of device arrays; out[i] may be x[i], address and strides
+ * Errors: INVALID_ARG, ALIGNMENT, CAPACITY (rows, heads, or strides whose products with rows or heads pass 2^60), HIP.
+ */
+dgc_status dgc_rotary(const dgc_rotary_shape* shape, const int64_t* positions, const uint64_t* frequencies,
+                      float magnitude, int32_t count, const int32_t* heads, const dgc_heads* x, const dgc_heads* out,
+                      void* stream);
+
+/*
+ * Linear attention with a decay for each head, over the sequences of an array of rows (as in dgc_scan: row t of sequence s
+ * is row s * max_length + t, or, with row_offsets, row row_offsets[s] + t).
+ */
+typedef struct dgc_attention {
+  int32_t dtype;      /* of q, k, v, o and their gradients                                     */
+  int32_t heads;      /* 1 .. 65535                                                            */
+  int32_t key_dim;    /* 1 .. DGC_HEAD_MAX: elements of a head of q and k                      */
+  int32_t value_dim;  /* 1 .. DGC_HEAD_MAX: of v and o                                         */
+  int64_t rows;       /* rows of the arrays, >= 0, < 2^40                                      */
+  int64_t sequences;  /* >= 0, < 2^31                                                          */
+  int64_t max_length; /* >= 0, < 2^31; without row_offsets, sequences * max_length = rows      */
+  const int64_t* row_offsets; /* as in dgc_scan                                                */
+  float scale;        /* finite                                                                */
+  uint32_t reserved;  /* zero                                                                  */
+} dgc_attention;
+
+/* Bytes of device workspace that the forward call (backward = 0) or the backward call (1) of this shape needs. */
+dgc_status dgc_linear_attention_workspace_bytes(const dgc_attention* shape, int32_t backward, size_t* bytes);
+
+/*
+ * For every sequence and head, with the head's decay d = exp(log_decay[head]) and a state S of key_dim x value_dim:
+ *   S_t = d S_{t-1} + k_t v_t^T,   o_t = scale q_t^T S_t
+ *   log_decay   device, float[heads], <= 0 (-inf: nothing is kept)
+ *   state0      device, float[sequences][heads][key_dim][value_dim], or NULL for zeros
+ *   o           must not overlap an input
+ *   state_last  device, float[same], or NULL: the state behind the last step (state0 where a sequence has none); may be
+ *               state0 itself: a serving loop calls this with max_length = 1 and one array of states
+ * Sums and states are binary32, also where the matrix units form them: 16-bit and 32-bit operands are taken apart into
+ * bfloat16 parts whose products are exact.  An element that is not finite makes what follows it in its head, and its
+ * neighbours up to 63 steps before it, not finite or unspecified.
+ * Errors: INVALID_ARG, ALIGNMENT, CAPACITY (workspace, or a shape or stride beyond the limits), HIP.
+ */
+dgc_status dgc_linear_attention_forward(const dgc_attention* shape, const dgc_heads* q, const dgc_heads* k,
+                                        const dgc_heads* v, const float* log_decay, const float* state0,
+                                        const dgc_heads* o, float* state_last, void* workspace, size_t workspace_bytes,
+                                        void* stream);
+
+/*
+ * Its gradients (the decays are constants).  With G the gradient of the state, G_t = d G_{t+1} + scale q_t do_t^T, where
+ * behind the last step dstate_last comes in without a decay:
+ *   dq_t = scale S_t do_t,   dk_t = G_t v_t,   dv_t = G_t^T k_t,   dstate0 = d G_0
+ * The states are formed again from the inputs.  A head that shares its vectors with others (a stride of 0) has gradients of
+ * its own: their sum is the shared vector's.
+ *   dstate_last  device, float[as state0], or NULL for zeros;  dstate0 device, float[same], or NULL; may be dstate_last
+ *   dq, dk, dv   must not overlap an input or each other
+ */
+dgc_status dgc_linear_attention_backward(const dgc_attention* shape, const dgc_heads* q, const dgc_heads* k,
+                                         const dgc_heads* v, const float* log_decay, const float* state0,
+                                         const dgc_heads* d_o, const float* dstate_last, const dgc_heads* dq,
+                                         const dgc_heads* dk, const dgc_heads* dv, float* dstate0, void* workspace,
+                                         size_t workspace_bytes, void* stream);
+
+/* An output layer: hidden rows x width, weight vocab x width; element (r, j) at r * stride + j. */
+typedef struct dgc_vocab {
+  int32_t dtype;         /* of hidden, weight and their gradients     */
+  uint32_t reserved;     /* zero                                      */
+  int64_t rows;          /* >= 0, < 2^24                              */
+  int64_t vocab;         /* >= 1, < 2^24                              */
+  int64_t width;         /* >= 1, < 2^20                              */
+  int64_t hidden_stride; /* >= width, < 2^24                          */
+  int64_t weight_stride; /* >= width, < 2^24                          */
+} dgc_vocab;
+
+/* Bytes of device workspace that the forward call (backward = 0) or the backward call (1) of this shape needs. */
+dgc_status dgc_vocab_loss_workspace_bytes(const dgc_vocab* shape, int32_t backward, size_t* bytes);
+
+/*
+ * Softmax cross entropy of the logits z = hidden weight^T, which are formed a piece of the vocabulary at a time and never
+ * kept:
+ *   lse[r] = log sum_j exp(z_rj),   loss[r] = w_r (lse[r] - z_ry)
+ *   labels      device, int32[rows]; a negative one stands for no label (loss 0)
+ *   row_weight  device, float[rows], or NULL for ones.  A row of weight zero has loss zero, whatever else it holds
+ *   loss, lse   device, float[rows], either may be NULL; lse is of every row, also of one without a label
+ *   diag_flags_dev  device uint32 or NULL: DGC_DIAG_BAD_INDEX is ORed in for a label >= vocab, which counts as none
+ * Products are exact and summed in binary32 (binary32 inputs are taken apart into three bfloat16 parts, of whose nine
+ * products the six largest are summed: 2^-23 of a product is left out at most).
+ * Errors: INVALID_ARG, ALIGNMENT, CAPACITY, HIP.
+ */
+dgc_status dgc_vocab_loss_forward(const dgc_vocab* shape, const void* hidden, const void* weight, const int32_t* labels,
+                                  const float* row_weight, float* loss, float* lse, uint32_t* diag_flags_dev,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradients, for the lse that the forward call left: with P_rj = exp(z_rj - lse[r]) - [j = y_r],
+ *   dhidden_r = w_r sum_j P_rj weight_j,   dweight_j = sum_r w_r P_rj hidden_r
+ * The logits are formed again.  A row without a label or of weight zero has a gradient of zero and adds nothing to dweight,
+ * whatever else it holds.
+ *   row_weight  as above; times the incoming gradient of the rows' losses
+ *   dhidden, dweight  device, of the inputs' type, either may be NULL; must not overlap an input
+ * With 16-bit inputs the P_rj, and the w_r P_rj of dweight, are rounded once to that type for the second products.
+ */
+dgc_status dgc_vocab_loss_backward(const dgc_vocab* shape, const void* hidden, const void* weight, const int32_t* labels,
+                                   const float* row_weight, const float* lse, void* dhidden, int64_t dhidden_stride,
+                                   void* dweight, int64_t dweight_stride, uint32_t* diag_flags_dev, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/*
  * Kernel timing for measurement harnesses.  After dgc_profile_enable the next
  * `max_calls` dgc_compress calls record HIP events on the caller's stream before
  * the norm kernel, after it, after the select kernel, after the streaming kernel

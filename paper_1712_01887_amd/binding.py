@@ -40,6 +40,10 @@ DGC_BF16 = 2
 DGC_TOP_MAX = 256
 DGC_SCAN_FREE_INPUT = 1 << 0
 DGC_SCAN_STATE_ROWS = 64
+DGC_HEAD_MAX = 256
+DGC_ROTARY_MAX = 4
+DGC_ROTARY_HALF = 1 << 0
+DGC_ROTARY_INVERSE = 1 << 1
 
 EXPORTS = [
     "dgc_config_default", "dgc_status_string", "dgc_create", "dgc_destroy", "dgc_invalidate_workspace",
@@ -53,6 +57,9 @@ EXPORTS = [
     "dgc_encode_max_entries", "dgc_encode", "dgc_decode_accumulate", "dgc_profile_stream_ceiling",
     "dgc_logits_workspace_bytes", "dgc_top_logits", "dgc_distill_loss", "dgc_gated_scan_workspace_bytes",
     "dgc_gated_scan_state_rows", "dgc_gated_scan_forward", "dgc_gated_scan_backward",
+    "dgc_rotary_frequencies", "dgc_rotary", "dgc_linear_attention_workspace_bytes", "dgc_linear_attention_forward",
+    "dgc_linear_attention_backward", "dgc_vocab_loss_workspace_bytes", "dgc_vocab_loss_forward",
+    "dgc_vocab_loss_backward",
 ]
 
 
@@ -86,6 +93,26 @@ class DgcLogits(C.Structure):
 class DgcScan(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("flags", C.c_uint32), ("rows", C.c_int64), ("sequences", C.c_int64),
                 ("max_length", C.c_int64), ("channels", C.c_int64), ("row_offsets", C.c_void_p)]
+
+
+class DgcHeads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class DgcRotaryShape(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("flags", C.c_uint32), ("rows", C.c_int64), ("head_dim", C.c_int32),
+                ("rotary_dim", C.c_int32)]
+
+
+class DgcAttention(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("heads", C.c_int32), ("key_dim", C.c_int32), ("value_dim", C.c_int32),
+                ("rows", C.c_int64), ("sequences", C.c_int64), ("max_length", C.c_int64), ("row_offsets", C.c_void_p),
+                ("scale", C.c_float), ("reserved", C.c_uint32)]
+
+
+class DgcVocab(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("reserved", C.c_uint32), ("rows", C.c_int64), ("vocab", C.c_int64),
+                ("width", C.c_int64), ("hidden_stride", C.c_int64), ("weight_stride", C.c_int64)]
 
 
 class DgcError(RuntimeError):
@@ -194,6 +221,24 @@ def load() -> C.CDLL:
     lib.dgc_gated_scan_backward.restype = i32
     lib.dgc_gated_scan_backward.argtypes = [P(DgcScan), vp, i64, vp, i64, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp,
                                             C.c_size_t, vp]
+    H = P(DgcHeads)
+    lib.dgc_rotary_frequencies.restype = i32
+    lib.dgc_rotary_frequencies.argtypes = [i32, dbl, dbl, dbl, dbl, dbl, vp]
+    lib.dgc_rotary.restype = i32
+    lib.dgc_rotary.argtypes = [P(DgcRotaryShape), vp, vp, f32, i32, P(i32), H, H, vp]
+    lib.dgc_linear_attention_workspace_bytes.restype = i32
+    lib.dgc_linear_attention_workspace_bytes.argtypes = [P(DgcAttention), i32, P(C.c_size_t)]
+    lib.dgc_linear_attention_forward.restype = i32
+    lib.dgc_linear_attention_forward.argtypes = [P(DgcAttention), H, H, H, vp, vp, H, vp, vp, C.c_size_t, vp]
+    lib.dgc_linear_attention_backward.restype = i32
+    lib.dgc_linear_attention_backward.argtypes = [P(DgcAttention), H, H, H, vp, vp, H, vp, H, H, H, vp, vp,
+                                                  C.c_size_t, vp]
+    lib.dgc_vocab_loss_workspace_bytes.restype = i32
+    lib.dgc_vocab_loss_workspace_bytes.argtypes = [P(DgcVocab), i32, P(C.c_size_t)]
+    lib.dgc_vocab_loss_forward.restype = i32
+    lib.dgc_vocab_loss_forward.argtypes = [P(DgcVocab), vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.dgc_vocab_loss_backward.restype = i32
+    lib.dgc_vocab_loss_backward.argtypes = [P(DgcVocab), vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, C.c_size_t, vp]
     _lib = lib
     return lib
 
@@ -497,6 +542,12 @@ class _Plan:
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self._current = torch.cuda.current_device
 
+    def _own(self, need: int) -> None:
+        """A workspace of `need` bytes, aligned as the library wants it."""
+        import torch
+        self.workspace = torch.empty(need + 256, dtype=torch.uint8, device=self.device) if need else None
+        self._ws_bytes, self._ws_ptr = need, (self.workspace.data_ptr() + 255) // 256 * 256 if need else 0
+
     def _stream(self) -> int:
         """The current stream of the plan's device, which has to be the current one."""
         if self._current() != self._index:
@@ -630,3 +681,175 @@ class GatedScan(_Plan):
             _dense(dh0, "dh0", f32, self._carried, dev), self._ws_ptr, self._ws_bytes, self._stream())
         if status:
             _check(status, "dgc_gated_scan_backward")
+
+
+# ---------------------------------------------------------------------------
+# Layers of recurrent language models with matrix states
+# ---------------------------------------------------------------------------
+def _heads_of(t, name: str, dtype, shape, index: int):
+    """What the library reads of a [rows, heads, elements] tensor whose heads are contiguous."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
+        _refuse(t, name, "heads", dtype, shape, index)
+    row, head, step = t.stride()
+    if step != 1 and shape[2] > 1:
+        raise DgcError(DGC_ERR_INVALID_ARG, f"{name}: strides {t.stride()} (the elements of a head must be contiguous)")
+    return t.data_ptr(), row, head
+
+
+class Rotary(_Plan):
+    """Heads turned by their rows' positions.  The first `rotary_dim` elements of a head (all that make pairs, if not
+    given) are turned, as pairs (2 i, 2 i + 1), or with `half` (i, i + rotary_dim / 2); `factor`, `context`, `low_turns`
+    and `high_turns` scale the frequencies for long contexts (see the header).  The plan holds the frequencies, which no
+    call writes to: its calls may run on any streams, from any threads."""
+
+    def __init__(self, head_dim: int, dtype, rotary_dim: int = None, base: float = 10000.0, half: bool = False,
+                 factor: float = 1.0, context: float = 0.0, low_turns: float = 1.0, high_turns: float = 32.0,
+                 magnitude: float = 1.0, device="cuda"):
+        import torch
+        self.lib = load()
+        self.head_dim, self.dtype, self.magnitude = int(head_dim), dtype, float(magnitude)
+        self.rotary_dim = self.head_dim // 2 * 2 if rotary_dim is None else int(rotary_dim)
+        self._code, self._flags = _dtype_code(dtype), DGC_ROTARY_HALF if half else 0
+        if not 1 <= self.head_dim <= DGC_HEAD_MAX or not 0 <= self.rotary_dim <= self.head_dim:
+            raise DgcError(DGC_ERR_INVALID_ARG, f"{rotary_dim} of {head_dim} elements of a head (1 .. {DGC_HEAD_MAX})")
+        table = (C.c_uint64 * max(1, self.rotary_dim // 2))()
+        _check(self.lib.dgc_rotary_frequencies(self.rotary_dim, base, factor, context, low_turns, high_turns, table),
+               "dgc_rotary_frequencies")
+        self._on(device)
+        self._i64 = torch.int64
+        # at most a turn's 1 / 2 pi each, so that none reaches the sign; a copy from pageable memory has ended when it returns
+        self.frequencies = torch.tensor(list(table), dtype=torch.int64).to(self.device)
+
+    def dgc_rotary(self, positions, x, out, inverse: bool = False) -> None:
+        """out[i] = x[i] ([rows, heads, head_dim] each, up to four; out[i] may be x[i]) turned by the rows' positions
+        (int64); `inverse`: turned back, which takes a gradient through the operator."""
+        dev, rows, n = self._index, positions.shape[0], len(x)
+        if len(out) != n or not 1 <= n <= DGC_ROTARY_MAX:
+            raise DgcError(DGC_ERR_INVALID_ARG, f"{n} arrays to turn into {len(out)} (1 .. {DGC_ROTARY_MAX})")
+        heads, src, dst = (C.c_int32 * n)(), (DgcHeads * n)(), (DgcHeads * n)()
+        for i in range(n):
+            h = x[i].shape[1]
+            heads[i] = h
+            src[i] = _heads_of(x[i], "x", self.dtype, (rows, h, self.head_dim), dev)
+            dst[i] = _heads_of(out[i], "out", self.dtype, (rows, h, self.head_dim), dev)
+        shape = DgcRotaryShape(self._code, self._flags | (DGC_ROTARY_INVERSE if inverse else 0), rows, self.head_dim,
+                               self.rotary_dim)
+        status = self.lib.dgc_rotary(C.byref(shape), _dense(positions, "positions", self._i64, (rows,), dev),
+                                     self.frequencies.data_ptr(), self.magnitude, n, heads, src, dst, self._stream())
+        if status:
+            _check(status, "dgc_rotary")
+
+
+class LinearAttention(_Plan):
+    """Sequences of one shape (or, with `row_offsets`, of different lengths behind each other in `rows` rows) under linear
+    attention with a decay for each head.  q, k: [rows, heads, key_dim], v: [rows, heads, value_dim], states: float32
+    [sequences, heads, key_dim, value_dim].  row_offsets: int64 on the device, sequences + 1 ascending row numbers.  The
+    plan owns a workspace, for the backward call too unless `backward` is false: its calls belong on one stream (or are
+    ordered by events)."""
+
+    def __init__(self, sequences: int, max_length: int, heads: int, key_dim: int, value_dim: int, dtype,
+                 scale: float = 1.0, row_offsets=None, rows: int = None, backward: bool = True, device="cuda"):
+        import torch
+        self.lib = load()
+        self._on(device)
+        self.sequences, self.heads, self.dtype = int(sequences), int(heads), dtype
+        self.key_dim, self.value_dim = int(key_dim), int(value_dim)
+        if row_offsets is None:
+            if rows is not None and rows != sequences * max_length:
+                raise DgcError(DGC_ERR_INVALID_ARG, f"{rows} rows are not {sequences} sequences of {max_length}")
+            self.rows = int(sequences) * int(max_length)
+        else:
+            if rows is None:
+                raise DgcError(DGC_ERR_INVALID_ARG, "row_offsets without rows")
+            self.rows = int(rows)
+        self.row_offsets = row_offsets                                # kept alive: its address is in the shape
+        self._shape = DgcAttention(_dtype_code(dtype), self.heads, self.key_dim, self.value_dim, self.rows, self.sequences,
+                                   int(max_length),
+                                   _dense(row_offsets, "row_offsets", torch.int64, (self.sequences + 1,), self._index),
+                                   scale, 0)
+        self._shape_ref = C.byref(self._shape)
+        self._keys, self._values = (self.rows, self.heads, self.key_dim), (self.rows, self.heads, self.value_dim)
+        self._carried = (self.sequences, self.heads, self.key_dim, self.value_dim)
+        need = C.c_size_t()
+        _check(self.lib.dgc_linear_attention_workspace_bytes(self._shape_ref, int(backward), C.byref(need)),
+               "dgc_linear_attention_workspace_bytes")
+        self._own(int(need.value))
+
+    def dgc_linear_attention_forward(self, q, k, v, log_decay, state0, o, state_last=None) -> None:
+        """o, and state_last (may be state0 itself) where given; state0 = None: zeros."""
+        t, dev, f32, keys, values = self.dtype, self._index, self._f32, self._keys, self._values
+        status = self.lib.dgc_linear_attention_forward(
+            self._shape_ref, DgcHeads(*_heads_of(q, "q", t, keys, dev)), DgcHeads(*_heads_of(k, "k", t, keys, dev)),
+            DgcHeads(*_heads_of(v, "v", t, values, dev)), _dense(log_decay, "log_decay", f32, (self.heads,), dev),
+            _dense(state0, "state0", f32, self._carried, dev), DgcHeads(*_heads_of(o, "o", t, values, dev)),
+            _dense(state_last, "state_last", f32, self._carried, dev), self._ws_ptr, self._ws_bytes, self._stream())
+        if status:
+            _check(status, "dgc_linear_attention_forward")
+
+    def dgc_linear_attention_backward(self, q, k, v, log_decay, state0, do, dstate_last, dq, dk, dv, dstate0=None) -> None:
+        """dq, dk, dv, and dstate0 (may be dstate_last itself) where given, from the inputs of the forward call;
+        dstate_last = None: zeros."""
+        t, dev, f32, keys, values = self.dtype, self._index, self._f32, self._keys, self._values
+        status = self.lib.dgc_linear_attention_backward(
+            self._shape_ref, DgcHeads(*_heads_of(q, "q", t, keys, dev)), DgcHeads(*_heads_of(k, "k", t, keys, dev)),
+            DgcHeads(*_heads_of(v, "v", t, values, dev)), _dense(log_decay, "log_decay", f32, (self.heads,), dev),
+            _dense(state0, "state0", f32, self._carried, dev), DgcHeads(*_heads_of(do, "do", t, values, dev)),
+            _dense(dstate_last, "dstate_last", f32, self._carried, dev), DgcHeads(*_heads_of(dq, "dq", t, keys, dev)),
+            DgcHeads(*_heads_of(dk, "dk", t, keys, dev)), DgcHeads(*_heads_of(dv, "dv", t, values, dev)),
+            _dense(dstate0, "dstate0", f32, self._carried, dev), self._ws_ptr, self._ws_bytes, self._stream())
+        if status:
+            _check(status, "dgc_linear_attention_backward")
+
+
+class VocabularyLoss(_Plan):
+    """Softmax cross entropy of an output layer (hidden: [rows, width], weight: [vocab, width]) without logits in memory, and
+    its gradients.  `rows`: of a call at most.  The plan owns a workspace, for the backward call too unless `backward` is
+    false: its calls belong on one stream (or are ordered by events)."""
+
+    def __init__(self, rows: int, vocab: int, width: int, dtype, backward: bool = True, device="cuda"):
+        self.lib = load()
+        self.rows, self.vocab, self.width, self.dtype = int(rows), int(vocab), int(width), dtype
+        self._code = _dtype_code(dtype)
+        need = C.c_size_t()
+        _check(self.lib.dgc_vocab_loss_workspace_bytes(self._shape(self.rows, self.width, self.width), int(backward),
+                                                       C.byref(need)), "dgc_vocab_loss_workspace_bytes")
+        self._on(device)
+        self._own(int(need.value))
+
+    def _shape(self, rows: int, hidden_stride: int, weight_stride: int):
+        return C.byref(DgcVocab(self._code, 0, rows, self.vocab, self.width, hidden_stride, weight_stride))
+
+    def _inputs(self, hidden, weight, labels, row_weight, diag_flags):
+        rows, t, dev = hidden.shape[0], self.dtype, self._index
+        if rows > self.rows:
+            raise DgcError(DGC_ERR_CAPACITY, f"{rows} rows in a plan for {self.rows}")
+        shape = self._shape(rows, _rows_of(hidden, "hidden", t, (rows, self.width), dev),
+                            _rows_of(weight, "weight", t, (self.vocab, self.width), dev))
+        return (rows, shape, _dense(labels, "labels", self._i32, (rows,), dev),
+                _dense(row_weight, "row_weight", self._f32, (rows,), dev),
+                _dense(diag_flags, "diag_flags", self._i32, (1,), dev))
+
+    def dgc_vocab_loss_forward(self, hidden, weight, labels, loss, lse=None, row_weight=None, diag_flags=None) -> None:
+        """loss (or None) and lse (or None) of every row."""
+        rows, shape, labels, row_weight, flags = self._inputs(hidden, weight, labels, row_weight, diag_flags)
+        dev, f32, one = self._index, self._f32, (rows,)
+        status = self.lib.dgc_vocab_loss_forward(
+            shape, hidden.data_ptr(), weight.data_ptr(), labels, row_weight, _dense(loss, "loss", f32, one, dev),
+            _dense(lse, "lse", f32, one, dev), flags, self._ws_ptr, self._ws_bytes, self._stream())
+        if status:
+            _check(status, "dgc_vocab_loss_forward")
+
+    def dgc_vocab_loss_backward(self, hidden, weight, labels, lse, dhidden, dweight, row_weight=None,
+                                diag_flags=None) -> None:
+        """dhidden (or None) and dweight (or None), from the lse of the forward call of the same inputs; row_weight: times
+        the incoming gradient of the rows' losses."""
+        rows, shape, labels, row_weight, flags = self._inputs(hidden, weight, labels, row_weight, diag_flags)
+        dev, t, w = self._index, self.dtype, self.width
+        hidden_stride = w if dhidden is None else _rows_of(dhidden, "dhidden", t, (rows, w), dev)
+        weight_stride = w if dweight is None else _rows_of(dweight, "dweight", t, (self.vocab, w), dev)
+        status = self.lib.dgc_vocab_loss_backward(
+            shape, hidden.data_ptr(), weight.data_ptr(), labels, row_weight, _dense(lse, "lse", self._f32, (rows,), dev),
+            0 if dhidden is None else dhidden.data_ptr(), hidden_stride, 0 if dweight is None else dweight.data_ptr(),
+            weight_stride, flags, self._ws_ptr, self._ws_bytes, self._stream())
+        if status:
+            _check(status, "dgc_vocab_loss_backward")

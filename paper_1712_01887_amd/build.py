@@ -19,10 +19,11 @@ ROOT = os.path.dirname(HERE)
 LIB_PATH = os.path.join(HERE, "libdgc.so")
 SOURCES = [os.path.join(HERE, "csrc", name) for name in
            ("dgc_api.hip", "dgc_compress.hip", "dgc_receive.hip", "dgc_wire.hip",
-            "dgc_operators_api.hip", "dgc_logits.hip", "dgc_scan.hip")]
+            "dgc_operators_api.hip", "dgc_logits.hip", "dgc_scan.hip",
+            "dgc_layers_api.hip", "dgc_rotary.hip", "dgc_attention.hip", "dgc_vocab.hip")]
 HEADERS = [os.path.join(HERE, "csrc", "dgc_internal.h"), os.path.join(HERE, "csrc", "dgc_device.h"),
            os.path.join(HERE, "csrc", "dgc_probe.h"), os.path.join(HERE, "csrc", "dgc_operators.h"),
-           os.path.join(HERE, "csrc", "dgc_steps.h"),
+           os.path.join(HERE, "csrc", "dgc_steps.h"), os.path.join(HERE, "csrc", "dgc_layers.h"),
            os.path.join(HERE, "csrc", "dgc_band.h"), os.path.join(ROOT, "include", "dgc.h")]
 
 
