@@ -674,7 +674,7 @@ dgc_status dgc_linear_attention_backward(const dgc_attention* shape, const dgc_h
 typedef struct dgc_vocab {
   int32_t dtype;         /* of hidden, weight and their gradients     */
   uint32_t reserved;     /* zero                                      */
-  int64_t rows;          /* >= 0, < 2^24                              */
+  int64_t rows;          /* >= 0, < 2^24; rows * vocab < 2^46        */
   int64_t vocab;         /* >= 1, < 2^24                              */
   int64_t width;         /* >= 1, < 2^20                              */
   int64_t hidden_stride; /* >= width, < 2^24                          */
@@ -692,8 +692,9 @@ dgc_status dgc_vocab_loss_workspace_bytes(const dgc_vocab* shape, int32_t backwa
  *   row_weight  device, float[rows], or NULL for ones.  A row of weight zero has loss zero, whatever else it holds
  *   loss, lse   device, float[rows], either may be NULL; lse is of every row, also of one without a label
  *   diag_flags_dev  device uint32 or NULL: DGC_DIAG_BAD_INDEX is ORed in for a label >= vocab, which counts as none
- * Products are exact and summed in binary32 (binary32 inputs are taken apart into three bfloat16 parts, of whose nine
- * products the six largest are summed: 2^-23 of a product is left out at most).
+ * Products are summed in binary32.  Those of 16-bit elements are exact.  Binary32 elements are scaled by a power of two and
+ * taken apart into two binary16 parts, and the product of the small parts is left out: 3 * 2^-22 of a product is lost at
+ * most, and 2^-39 of what the array's largest element would make of it.
  * Errors: INVALID_ARG, ALIGNMENT, CAPACITY, HIP.
  */
 dgc_status dgc_vocab_loss_forward(const dgc_vocab* shape, const void* hidden, const void* weight, const int32_t* labels,

@@ -58,7 +58,7 @@ dgc_status check_vocab(const dgc_vocab* s) {
     return DGC_ERR_INVALID_ARG;
   if (s->rows >= 1 << 24 || s->vocab >= 1 << 24 || s->width >= 1 << 20 || s->hidden_stride >= 1 << 24 || s->weight_stride >= 1 << 24)
     return DGC_ERR_CAPACITY;
-  return DGC_OK;
+  return s->rows * s->vocab < (int64_t)1 << 46 ? DGC_OK : DGC_ERR_CAPACITY;  // tiles that one launch numbers
 }
 
 VocabArgs vocab_args(const dgc_vocab* s, const void* hidden, const void* weight, const int32_t* labels, const float* row_weight,

@@ -1,0 +1,199 @@
+// Products of matrices of 16-bit elements on the matrix units, a tile to a workgroup: the common part of the kernels of
+// dgc_vocab.hip, which differ in what they do with a tile's sums.
+#ifndef DGC_PRODUCT_H_
+#define DGC_PRODUCT_H_
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace dgc {
+
+typedef float Sums __attribute__((ext_vector_type(16)));
+
+template <typename E>
+struct Matrix;
+template <>
+struct Matrix<__bf16> {
+  typedef __bf16 Fragment __attribute__((ext_vector_type(8)));
+  typedef __bf16 Half __attribute__((ext_vector_type(4)));
+  static __device__ __forceinline__ Sums multiply(Fragment a, Fragment b, Sums c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ Half turned(const __bf16* p) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) Half*)p);
+  }
+};
+template <>
+struct Matrix<_Float16> {
+  typedef _Float16 Fragment __attribute__((ext_vector_type(8)));
+  typedef _Float16 Half __attribute__((ext_vector_type(4)));
+  typedef __fp16 Read __attribute__((ext_vector_type(4)));
+  static __device__ __forceinline__ Sums multiply(Fragment a, Fragment b, Sums c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ Half turned(const _Float16* p) {
+    return __builtin_bit_cast(Half, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) Read*)p));
+  }
+};
+
+// A matrix in memory, `rows` rows `stride` bytes apart, `row_bytes` of each there; `plane` bytes on lies its second part.
+// Every row starts at a multiple of 16 bytes.
+struct Operand {
+  const char* data;
+  int64_t stride, plane;
+  int32_t rows, row_bytes;
+};
+
+constexpr int kDepth = 64;  // of the sum at a time
+
+// A tile of rows x columns, by waves_m x waves_n wavefronts.
+template <int M, int N, int WAVES_M, int WAVES_N>
+struct Tile {
+  static constexpr int kM = M, kN = N, kWavesM = WAVES_M, kWavesN = WAVES_N;
+  static constexpr int kWaves = WAVES_M * WAVES_N, kThreads = 64 * kWaves;
+  static constexpr int kBlocksM = M / WAVES_M / 32, kBlocksN = N / WAVES_N / 32;  // of 32 x 32 to a wavefront
+};
+
+// One side of a tile: SIDE rows (or, ACROSS, columns) of an operand, kDepth of the other kind at a time.
+//
+// Loads go from memory to LDS without registers in between: 64 lanes leave 64 pieces of 16 bytes behind each other, so that
+// what is swizzled is which piece a lane asks for.  Along: 128 bytes to a row, whose eight pieces are exchanged by half the
+// row's number, so that the 16 rows that 16 lanes read lie in 16 different places of 256 bytes, all the banks there are.
+// Across: the sum runs over the rows; blocks of 64 bytes are exchanged by the row's number, so that the four rows from which
+// 16 lanes take 4 elements of a column each lie in different banks.
+template <typename E, int SIDE, bool ACROSS, int WAVES>
+struct Side {
+  static constexpr int kElements = SIDE * kDepth;
+  static constexpr int kLoads = kElements * 2 / 1024 / WAVES;  // to a wavefront, of 1024 bytes
+  static_assert(kLoads * WAVES * 1024 == kElements * 2, "whole loads");
+  static constexpr int kPieces = (ACROSS ? SIDE : kDepth) / 8;  // of 16 bytes to a row in LDS
+  const char* base;
+  int64_t stride, plane;
+  int32_t rows, row_bytes;  // left from `base` on; rows of the array
+  uint32_t offset[kLoads];
+
+  static __device__ __forceinline__ int exchange(int row) { return ACROSS ? (SIDE >= 128 ? row & 3 : (row >> 1) & 1) : (row >> 1) & 7; }
+
+  // The tile begins at row (or column) `first`.
+  __device__ __forceinline__ void start(const Operand& o, int first, int wave, int lane) {
+    stride = o.stride;
+    plane = o.plane;
+    base = ACROSS ? o.data + (int64_t)first * 2 : o.data + first * o.stride;
+    rows = ACROSS ? o.rows : o.rows - first;
+    row_bytes = ACROSS ? o.row_bytes - first * 2 : o.row_bytes;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int piece = (wave * kLoads + i) * 64 + lane, row = piece / kPieces, at = piece % kPieces;
+      const int wanted = ACROSS ? (((at >> 2) ^ exchange(row)) << 2 | (at & 3)) : at ^ exchange(row);
+      offset[i] = (uint32_t)row * (uint32_t)stride + (uint32_t)wanted * 16u;
+    }
+  }
+
+  // Elements [k, k + kDepth) of the sum, of part `part`.  Behind the array's last row, zeros: the buffer ends there.
+  __device__ __forceinline__ void load(E* lds, int k, int part, int wave) const {
+    const char* from = base + part * plane + (ACROSS ? (int64_t)k * stride : (int64_t)k * 2);
+    const int have = ACROSS ? rows - k : rows, most = ACROSS ? kDepth : SIDE;
+    const int64_t bytes = have <= 0 ? 0 : (int64_t)((have < most ? have : most) - 1) * stride + row_bytes - (ACROSS ? 0 : k * 2);
+    const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, (int)(uint32_t)bytes, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (__attribute__((address_space(3))) void*)(lds + (wave * kLoads + i) * 512), 16, (int)offset[i], 0, 0, 0);
+  }
+
+  // What lane `lane` holds of 32 rows (or columns) from `at` on, 16 elements of the sum from `k` on: row lane % 32, eight
+  // elements from 8 (lane / 32) on.
+  static __device__ __forceinline__ typename Matrix<E>::Fragment fragment(const E* lds, int at, int k, int lane) {
+    if constexpr (ACROSS) {
+      const int l = lane & 15, row = k + 8 * (lane >> 5) + (l >> 2), column = at + (lane & 16) + 4 * (l & 3);
+      const E* p = lds + row * SIDE + (((column >> 5) ^ exchange(row)) << 5) + (column & 31);
+      const auto lo = Matrix<E>::turned(p), hi = Matrix<E>::turned(p + 4 * SIDE);
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      const int row = at + (lane & 31), piece = k / 8 + (lane >> 5);
+      return *reinterpret_cast<const typename Matrix<E>::Fragment*>(lds + row * kDepth + ((piece ^ exchange(row)) << 3));
+    }
+  }
+};
+
+// sums[i][j]: of rows m0 + 32 i + lane % 32 of a wavefront's part of the tile and its columns n0 + 32 j + 8 (e / 4) +
+// 4 (lane / 32) + e % 4 in element e, over `depth` (a multiple of kDepth, from `from` on) elements of the sum; with PARTS =
+// 2 operands of two parts, of which the product of the small ones is left out.
+//
+// While a tile in LDS is multiplied the next one is on its way to another; a barrier a tile.
+template <typename E, typename T, bool ACROSS_A, bool ACROSS_B, int PARTS>
+__device__ __forceinline__ void multiply_tile(Sums (&sums)[T::kBlocksM][T::kBlocksN], const Operand& a, const Operand& b, int m0, int n0, int from, int depth) {
+  using A = Side<E, T::kM, ACROSS_A, T::kWaves>;
+  using B = Side<E, T::kN, ACROSS_B, T::kWaves>;
+  __shared__ __align__(16) E a0[A::kElements], a1[A::kElements], b0[B::kElements], b1[B::kElements];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int wave_m = wave / T::kWavesN * (T::kBlocksM * 32), wave_n = wave % T::kWavesN * (T::kBlocksN * 32);
+  A side_a;
+  B side_b;
+  side_a.start(a, m0, wave, lane);
+  side_b.start(b, n0, wave, lane);
+#pragma unroll
+  for (int i = 0; i < T::kBlocksM; ++i)
+#pragma unroll
+    for (int j = 0; j < T::kBlocksN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sums[i][j][e] = 0.0f;
+  const int tiles = depth / kDepth, total = PARTS == 2 ? 3 * tiles : tiles;
+  int k = from, part = 0;  // of the tile that is loaded next
+  auto load = [&](E* to_a, E* to_b) {
+    side_a.load(to_a, k, PARTS == 2 && part == 2, wave);
+    side_b.load(to_b, k, PARTS == 2 && part == 1, wave);
+    k += kDepth;
+    if (PARTS == 2 && k == from + depth) {
+      k = from;
+      ++part;
+    }
+  };
+  // The fragments of a step of 16 are read while the step before it is multiplied, and no sooner: more of them do not fit
+  // beside the sums.
+  auto compute = [&](const E* from_a, const E* from_b) {
+    typename Matrix<E>::Fragment fa[2][T::kBlocksM], fb[2][T::kBlocksN];
+    auto read = [&](int set, int d) {
+#pragma unroll
+      for (int j = 0; j < T::kBlocksN; ++j) fb[set][j] = B::fragment(from_b, wave_n + 32 * j, d, lane);
+#pragma unroll
+      for (int i = 0; i < T::kBlocksM; ++i) fa[set][i] = A::fragment(from_a, wave_m + 32 * i, d, lane);
+    };
+    read(0, 0);
+#pragma unroll
+    for (int step = 0; step < kDepth / 16; ++step) {
+      if (step + 1 < kDepth / 16) read((step + 1) % 2, 16 * step + 16);
+#pragma unroll
+      for (int i = 0; i < T::kBlocksM; ++i)
+#pragma unroll
+        for (int j = 0; j < T::kBlocksN; ++j) sums[i][j] = Matrix<E>::multiply(fb[step % 2][j], fa[step % 2][i], sums[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  if (total == 0) return;
+  load(a0, b0);
+  int t = 0;
+  for (; t + 2 < total; t += 2) {
+    __syncthreads();
+    load(a1, b1);
+    compute(a0, b0);
+    __syncthreads();
+    load(a0, b0);
+    compute(a1, b1);
+  }
+  __syncthreads();
+  if (t + 1 < total) load(a1, b1);
+  compute(a0, b0);
+  __syncthreads();
+  if (t + 1 < total) compute(a1, b1);
+}
+
+// Which tile a workgroup takes.  Workgroups go to the eight dies in turn: a die gets neighbouring tiles, eight rows of tiles
+// at a time, so that what they share is in its own cache.
+__device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int& m, int& n) {
+  const int total = tiles_m * tiles_n, die = id & 7, q = total >> 3, r = total & 7;
+  int t = die * q + (die < r ? die : r) + (id >> 3);
+  const int group = 8 * tiles_n, first = t / group * 8;
+  const int height = tiles_m - first < 8 ? tiles_m - first : 8;
+  t -= first * tiles_n;
+  m = first + t % height;
+  n = t / height;
+}
+
+}  // namespace dgc
+#endif  // DGC_PRODUCT_H_

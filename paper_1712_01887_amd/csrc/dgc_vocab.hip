@@ -1,18 +1,54 @@
 // Softmax cross entropy of an output layer without its logits in memory, and its gradients.
+//
+// Four products: the logits hidden weight^T, formed once for their statistics and once for the shares P; P weight and
+// P^T hidden.  A piece of the vocabulary at a time, P of a piece is all that is kept.  Elements of 16 bits are multiplied as
+// they are; those of 32 are scaled by a power of two, so that the array's largest is some 2^14, and taken apart into two
+// parts of binary16, whose products (but that of the small parts) are summed: of an element x, 2^-22 |x| is lost at most,
+// and 2^-39 of the largest.
 
 #include "dgc_layers.h"
+#include "dgc_product.h"
 
 namespace dgc {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTile = 64;   // rows and columns of a workgroup's part of a product
-constexpr int kDepth = 16;  // of the sum at a time
-constexpr int kPiece = 8192;  // columns of the vocabulary whose P are kept at a time
+constexpr int kPad = 256;                  // rows and columns of P are whole tiles of the largest shape
+constexpr int64_t kShares = 1 << 25;       // elements of P that are kept at a time, if this many rows of kLeast columns fit
+constexpr int64_t kPacked = 1 << 26;       // elements of a packed piece of the weight
+constexpr int kLeast = 2048;               // columns of a piece at least, unless there are fewer
+constexpr int kSplitMax = 32;
 
 size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-// A row's weight, zero where it has no label; `label` is cut to a column that is there.
+template <typename T>
+struct Inner {  // what an element is multiplied as
+  using E = T;
+  static constexpr int kParts = 1;
+};
+template <>
+struct Inner<float> {
+  using E = _Float16;
+  static constexpr int kParts = 2;
+};
+
+using Large = Tile<256, 256, 2, 4>;
+using Middle = Tile<128, 128, 2, 2>;
+using Small = Tile<64, 64, 2, 2>;
+
+// ---- powers of two that elements are scaled by -----------------------------------------------
+// Bits of the largest absolute value: of row weights, of hidden and of weight.
+enum { kOfShares = 0, kOfHidden = 1, kOfWeight = 2, kScales = 3 };
+
+__device__ __forceinline__ int exponent_of(uint32_t largest) {
+  const int e = (int)(largest >> 23);
+  return e < 28 ? 28 : e;  // scales and their inverses stay normal
+}
+__device__ __forceinline__ float scale_of(uint32_t largest) { return __uint_as_float((uint32_t)(268 - exponent_of(largest)) << 23); }
+__device__ __forceinline__ float unscale_of(uint32_t largest) { return __uint_as_float((uint32_t)(exponent_of(largest) - 14) << 23); }
+
+// A row's weight, zero where it has no label; `label` is -1 then.
 __device__ __forceinline__ float live_weight(const VocabArgs& v, int row, int& label) {
   label = v.labels[row];
   if (label < 0 || label >= v.vocab) {
@@ -22,199 +58,478 @@ __device__ __forceinline__ float live_weight(const VocabArgs& v, int row, int& l
   return v.row_weight ? v.row_weight[row] : 1.0f;
 }
 
-// sum[i][j] = sum over k < depth of x(4 ty + i, k) y(4 tx + j, k) for a tile of 64 x 64.
-template <typename X, typename Y>
-__device__ __forceinline__ void multiply(float (&sum)[4][4], int depth, X x, Y y) {
-  __shared__ float xs[kDepth][kTile + 4], ys[kDepth][kTile + 4];
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) sum[i / 4][i % 4] = 0.0f;
-  for (int k0 = 0; k0 < depth; k0 += kDepth) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < kTile * kDepth; i += kThreads) {
-      const int r = i / kDepth, k = i % kDepth;
-      xs[k][r] = k0 + k < depth ? x(r, k0 + k) : 0.0f;
-      ys[k][r] = k0 + k < depth ? y(r, k0 + k) : 0.0f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kDepth; ++k)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sum[i / 4][i % 4] = fmaf(xs[k][4 * ty + i / 4], ys[k][4 * tx + i % 4], sum[i / 4][i % 4]);
-  }
+__device__ __forceinline__ uint32_t finite_size(float x) {
+  const uint32_t bits = __float_as_uint(x) & 0x7fffffffu;
+  return bits < 0x7f800000u ? bits : 0u;
 }
 
-template <typename T>
-__device__ __forceinline__ void logits_tile(float (&sum)[4][4], const VocabArgs& v, int row0, int column0) {
-  const T* hidden = static_cast<const T*>(v.hidden);
-  const T* weight = static_cast<const T*>(v.weight);
-  multiply(sum, v.width,
-           [&](int r, int k) { return row0 + r < v.rows ? to_float(hidden[(row0 + r) * v.hidden_stride + k]) : 0.0f; },
-           [&](int c, int k) { return column0 + c < v.vocab ? to_float(weight[(column0 + c) * v.weight_stride + k]) : 0.0f; });
-}
-
-// The largest logit and the sum of exponentials of every row of a tile; a label's logit where it lies in the tile.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void statistics_kernel(const VocabArgs v, float2* parts, float* at_label) {
-  const int row0 = blockIdx.y * kTile, column0 = blockIdx.x * kTile;
-  float z[4][4];
-  logits_tile<T>(z, v, row0, column0);
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  for (int i = 0; i < 4; ++i) {
-    const int row = row0 + 4 * ty + i;
-    float top = -INFINITY, sum = 0.0f;
-    for (int j = 0; j < 4; ++j) {
-      const int column = column0 + 4 * tx + j;
-      if (column >= v.vocab) z[i][j] = -INFINITY;
-      if (row < v.rows && column == v.labels[row]) at_label[row] = z[i][j];
-      top = fmaxf(top, z[i][j]);
-    }
-    for (int m = 1; m < 16; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
-    const float shift = top == -INFINITY ? 0.0f : top;
-    for (int j = 0; j < 4; ++j) sum += exp2f((z[i][j] - shift) * 1.44269504f);
-    for (int m = 1; m < 16; m *= 2) sum += __shfl_xor(sum, m);
-    if (tx == 0 && row < v.rows) parts[(int64_t)row * gridDim.x + blockIdx.x] = make_float2(shift, sum);
+// The largest row weight, one workgroup; the other two words are cleared for largest_kernel.
+__global__ __launch_bounds__(1024) void weights_kernel(const VocabArgs v, uint32_t* largest) {
+  __shared__ uint32_t waves[16];
+  uint32_t most = 0;
+  for (int r = threadIdx.x; r < v.rows; r += 1024) {
+    int label;
+    most = max(most, finite_size(live_weight(v, r, label)));
   }
-}
-
-__global__ __launch_bounds__(kThreads) void join_kernel(const VocabArgs v, const float2* parts, const float* at_label, int tiles) {
-  const int row = blockIdx.x, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-  __shared__ float2 waves[kThreads / 64];
-  float top = -INFINITY, sum = 0.0f;
-  for (int i = threadIdx.x; i < tiles; i += kThreads) top = fmaxf(top, parts[(int64_t)row * tiles + i].x);
-  for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
-  if (lane == 0) waves[wave].x = top;
-  __syncthreads();
-  for (int i = 0; i < kThreads / 64; ++i) top = fmaxf(top, waves[i].x);
-  for (int i = threadIdx.x; i < tiles; i += kThreads) {
-    const float2 p = parts[(int64_t)row * tiles + i];
-    sum += p.y * exp2f((p.x - top) * 1.44269504f);
-  }
-  for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
-  if (lane == 0) waves[wave].y = sum;
+  for (int m = 1; m < 64; m *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, m));
+  if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = most;
   __syncthreads();
   if (threadIdx.x == 0) {
-    sum = 0.0f;
-    for (int i = 0; i < kThreads / 64; ++i) sum += waves[i].y;
-    const float lse = top + logf(sum);
-    int label;
-    const float w = live_weight(v, row, label);
-    if (v.lse) v.lse[row] = lse;
-    if (v.loss) v.loss[row] = w != 0.0f ? w * (lse - at_label[row]) : 0.0f;
-    if (v.diag_flags && v.labels[row] >= v.vocab) atomicOr(v.diag_flags, (uint32_t)DGC_DIAG_BAD_INDEX);
+    for (int i = 1; i < 16; ++i) most = max(most, waves[i]);
+    largest[kOfShares] = most;
+    largest[kOfHidden] = 0;
+    largest[kOfWeight] = 0;
   }
 }
 
-// P of a piece of the vocabulary that begins at `first`.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void shares_kernel(const VocabArgs v, float* shares, int first) {
-  const int row0 = blockIdx.y * kTile, column0 = first + blockIdx.x * kTile;
-  float z[4][4];
-  logits_tile<T>(z, v, row0, column0);
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  for (int i = 0; i < 4; ++i) {
-    const int row = row0 + 4 * ty + i;
-    if (row >= v.rows) continue;
+// The largest element of an array, over rows with a weight if `masked`.  The order of the maxima does not matter.
+__global__ __launch_bounds__(kThreads) void largest_kernel(const VocabArgs v, const float* x, int64_t stride, int rows, bool masked, uint32_t* largest) {
+  uint32_t most = 0;
+  for (int r = blockIdx.x; r < rows; r += gridDim.x) {
     int label;
-    const float w = live_weight(v, row, label);
-    if (v.diag_flags && v.labels[row] >= v.vocab) atomicOr(v.diag_flags, (uint32_t)DGC_DIAG_BAD_INDEX);
-    for (int j = 0; j < 4; ++j) {
-      const int column = column0 + 4 * tx + j;
-      float p = exp2f((z[i][j] - v.lse[row]) * 1.44269504f) - (column == label ? 1.0f : 0.0f);
-      if (column >= v.vocab || w == 0.0f) p = 0.0f;
-      shares[(int64_t)row * kPiece + column - first] = p;
+    if (masked && live_weight(v, r, label) == 0.0f) continue;
+    for (int i = threadIdx.x; i < v.width; i += kThreads) most = max(most, finite_size(x[r * stride + i]));
+  }
+  for (int m = 1; m < 64; m *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, m));
+  if (threadIdx.x % 64 == 0 && most) atomicMax(largest, most);
+}
+
+// ---- packed copies ---------------------------------------------------------------------------
+// Rows of an array as the products read them: `columns` elements to a row, a multiple of 64, zeros behind `width`; binary32
+// in two parts; rows without a weight as zeros if `masked`.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void pack_kernel(const VocabArgs v, const T* x, int64_t stride, int rows, bool masked, const uint32_t* largest,
+                                                        typename Inner<T>::E* out, int columns, int64_t plane) {
+  using E = typename Inner<T>::E;
+  const int pieces = columns / 8;
+  const int64_t total = (int64_t)rows * pieces;
+  const float scale = Inner<T>::kParts == 2 ? scale_of(*largest) : 1.0f;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
+    const int row = (int)(i / pieces), column = (int)(i % pieces) * 8;
+    int label;
+    const bool dead = masked && live_weight(v, row, label) == 0.0f;
+    const T* from = x + row * stride + column;
+    alignas(16) E parts[Inner<T>::kParts][8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const bool there = !dead && column + j < v.width;
+      if constexpr (Inner<T>::kParts == 2) {
+        const float value = there ? from[j] * scale : 0.0f;
+        parts[0][j] = (E)value;
+        parts[1][j] = (E)(value - (float)parts[0][j]);
+      } else {
+        parts[0][j] = there ? from[j] : (T)0.0f;
+      }
     }
+#pragma unroll
+    for (int p = 0; p < Inner<T>::kParts; ++p)
+      *reinterpret_cast<uint4*>(out + p * plane + (int64_t)row * columns + column) = *reinterpret_cast<const uint4*>(parts[p]);
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void dhidden_kernel(const VocabArgs v, const float* shares, float* total, int first, int columns) {
-  const int row0 = blockIdx.y * kTile, column0 = blockIdx.x * kTile;
-  const T* weight = static_cast<const T*>(v.weight);
-  float sum[4][4];
-  multiply(sum, columns, [&](int r, int k) { return row0 + r < v.rows ? shares[(int64_t)(row0 + r) * kPiece + k] : 0.0f; },
-           [&](int c, int k) { return column0 + c < v.width ? to_float(weight[(int64_t)(first + k) * v.weight_stride + column0 + c]) : 0.0f; });
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int row = row0 + 4 * ty + i, column = column0 + 4 * tx + j;
-      if (row >= v.rows || column >= v.width) continue;
-      float x = sum[i][j];
-      float* t = total + (int64_t)row * v.width + column;
-      if (first) x += *t;
-      *t = x;
-      int label;
-      if (first + columns == v.vocab) static_cast<T*>(v.dhidden)[row * v.dhidden_stride + column] = from_float<T>(x * live_weight(v, row, label));
-    }
+// ---- statistics ------------------------------------------------------------------------------
+// The largest logit and the sum of exponentials of every row of a tile, at [tile of columns][row]; a label's logit.
+template <typename T, typename S>
+__global__ __launch_bounds__(S::kThreads) void statistics_kernel(const VocabArgs v, Operand hidden, Operand weight, int depth, int first, int columns,
+                                                                 const uint32_t* largest, float2* parts, float* at_label) {
+  constexpr int kParts = Inner<T>::kParts;
+  __shared__ float2 joined[S::kWavesN][S::kM];
+  int tile_m, tile_n;
+  tile_of(blockIdx.x, (v.rows + S::kM - 1) / S::kM, (columns + S::kN - 1) / S::kN, tile_m, tile_n);
+  const int m0 = tile_m * S::kM, n0 = tile_n * S::kN;
+  Sums z[S::kBlocksM][S::kBlocksN];
+  multiply_tile<typename Inner<T>::E, S, false, false, kParts>(z, hidden, weight, m0, n0, 0, depth);
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int wave_m = wave / S::kWavesN * (S::kBlocksM * 32), wave_n = wave % S::kWavesN * (S::kBlocksN * 32);
+  const float unscale_hidden = kParts == 2 ? unscale_of(largest[kOfHidden]) : 1.0f;
+  const float unscale_weight = kParts == 2 ? unscale_of(largest[kOfWeight]) : 1.0f;
+#pragma unroll
+  for (int i = 0; i < S::kBlocksM; ++i) {
+    const int row = wave_m + 32 * i + (lane & 31);
+    const int label = m0 + row < v.rows ? v.labels[m0 + row] - first - n0 : -1;
+    float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < S::kBlocksN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int column = wave_n + 32 * j + 8 * (e / 4) + 4 * (lane >> 5) + e % 4;
+        float x = z[i][j][e];
+        if constexpr (kParts == 2) x = x * unscale_hidden * unscale_weight;
+        if (n0 + column >= columns) x = -INFINITY;
+        else if (column == label) at_label[m0 + row] = x;
+        top = fmaxf(top, x);
+        z[i][j][e] = x;
+      }
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float shift = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+    for (int j = 0; j < S::kBlocksN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f((z[i][j][e] - shift) * 1.44269504f);
+    sum += __shfl_xor(sum, 32);
+    if (lane < 32) joined[wave % S::kWavesN][row] = make_float2(shift, sum);
+  }
+  __syncthreads();
+  for (int row = threadIdx.x; row < S::kM; row += S::kThreads) {
+    if (m0 + row >= v.rows) break;
+    float top = joined[0][row].x, sum = 0.0f;
+#pragma unroll
+    for (int i = 1; i < S::kWavesN; ++i) top = fmaxf(top, joined[i][row].x);
+#pragma unroll
+    for (int i = 0; i < S::kWavesN; ++i) sum += joined[i][row].y * __builtin_amdgcn_exp2f((joined[i][row].x - top) * 1.44269504f);
+    parts[(int64_t)(first / S::kN + tile_n) * v.rows + m0 + row] = make_float2(top, sum);
+  }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void dweight_kernel(const VocabArgs v, const float* shares, int first, int columns) {
-  const int row0 = blockIdx.y * kTile, column0 = blockIdx.x * kTile;
-  const T* hidden = static_cast<const T*>(v.hidden);
+// A row to 8 threads, which take its tiles in turn.
+__global__ __launch_bounds__(kThreads) void join_kernel(const VocabArgs v, const float2* parts, const float* at_label, int tiles) {
+  const int row = blockIdx.x * (kThreads / 8) + threadIdx.x % (kThreads / 8), part = threadIdx.x / (kThreads / 8);
+  __shared__ float2 joined[8][kThreads / 8];
+  float top = -INFINITY, sum = 0.0f;
+  if (row < v.rows)
+    for (int i = part; i < tiles; i += 8) {
+      const float2 p = parts[(int64_t)i * v.rows + row];
+      const float larger = fmaxf(top, p.x);
+      // -inf - -inf never meets a sum: the parts' maxima are finite
+      sum = sum * __builtin_amdgcn_exp2f((top - larger) * 1.44269504f) + p.y * __builtin_amdgcn_exp2f((p.x - larger) * 1.44269504f);
+      top = larger;
+    }
+  joined[part][threadIdx.x % (kThreads / 8)] = make_float2(top, sum);
+  __syncthreads();
+  if (part != 0 || row >= v.rows) return;
+  const int n = tiles < 8 ? tiles : 8;
+  for (int i = 1; i < n; ++i) {
+    const float2 p = joined[i][threadIdx.x];
+    const float larger = fmaxf(top, p.x);
+    sum = sum * __builtin_amdgcn_exp2f((top - larger) * 1.44269504f) + p.y * __builtin_amdgcn_exp2f((p.x - larger) * 1.44269504f);
+    top = larger;
+  }
+  const float lse = top + logf(sum);
   int label;
-  float sum[4][4];
-  multiply(sum, v.rows, [&](int r, int k) { return row0 + r < columns ? shares[(int64_t)k * kPiece + row0 + r] : 0.0f; },
-           [&](int c, int k) {
-             const float w = live_weight(v, k, label);
-             return column0 + c < v.width && w != 0.0f ? w * to_float(hidden[k * v.hidden_stride + column0 + c]) : 0.0f;
-           });
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int row = row0 + 4 * ty + i, column = column0 + 4 * tx + j;
-      if (row < columns && column < v.width) static_cast<T*>(v.dweight)[(first + row) * v.dweight_stride + column] = from_float<T>(sum[i][j]);
-    }
+  const float w = live_weight(v, row, label);
+  if (v.lse) v.lse[row] = lse;
+  if (v.loss) v.loss[row] = w != 0.0f ? w * (lse - at_label[row]) : 0.0f;
+  if (v.diag_flags && v.labels[row] >= v.vocab) atomicOr(v.diag_flags, (uint32_t)DGC_DIAG_BAD_INDEX);
 }
 
-int tiles_of(int64_t n) { return (int)((n + kTile - 1) / kTile); }
-
-template <typename T>
-hipError_t forward(const VocabArgs& v, void* workspace, hipStream_t stream) {
-  const int tiles = tiles_of(v.vocab);
-  float2* parts = static_cast<float2*>(workspace);
-  float* at_label = reinterpret_cast<float*>(static_cast<char*>(workspace) + whole((size_t)v.rows * tiles * 8));
-  statistics_kernel<T><<<dim3(tiles, tiles_of(v.rows)), kThreads, 0, stream>>>(v, parts, at_label);
-  join_kernel<<<v.rows, kThreads, 0, stream>>>(v, parts, at_label, tiles);
-  return hipGetLastError();
-}
-
-template <typename T>
-hipError_t backward(const VocabArgs& v, void* workspace, hipStream_t stream) {
-  float* shares = static_cast<float*>(workspace);
-  float* total = reinterpret_cast<float*>(static_cast<char*>(workspace) + whole((size_t)v.rows * kPiece * 4));
-  for (int first = 0; first < v.vocab; first += kPiece) {
-    const int columns = v.vocab - first < kPiece ? v.vocab - first : kPiece;
-    if (v.rows > 0) shares_kernel<T><<<dim3(tiles_of(columns), tiles_of(v.rows)), kThreads, 0, stream>>>(v, shares, first);
-    if (v.rows > 0 && v.dhidden)
-      dhidden_kernel<T><<<dim3(tiles_of(v.width), tiles_of(v.rows)), kThreads, 0, stream>>>(v, shares, total, first, columns);
-    if (v.dweight)
-      dweight_kernel<T><<<dim3(tiles_of(v.width), tiles_of(columns)), kThreads, 0, stream>>>(v, shares, first, columns);
+// ---- gradients -------------------------------------------------------------------------------
+// w_r P_rj of a piece, rounded to what it is multiplied as: whole tiles, zeros outside the rows and the vocabulary.
+template <typename T, typename S>
+__global__ __launch_bounds__(S::kThreads) void shares_kernel(const VocabArgs v, Operand hidden, Operand weight, int depth, int first, int columns,
+                                                             const uint32_t* largest, typename Inner<T>::E* shares, int64_t stride, int64_t plane) {
+  using E = typename Inner<T>::E;
+  constexpr int kParts = Inner<T>::kParts;
+  int tile_m, tile_n;
+  tile_of(blockIdx.x, (v.rows + S::kM - 1) / S::kM, (columns + S::kN - 1) / S::kN, tile_m, tile_n);
+  const int m0 = tile_m * S::kM, n0 = tile_n * S::kN;
+  Sums z[S::kBlocksM][S::kBlocksN];
+  multiply_tile<E, S, false, false, kParts>(z, hidden, weight, m0, n0, 0, depth);
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int wave_m = wave / S::kWavesN * (S::kBlocksM * 32), wave_n = wave % S::kWavesN * (S::kBlocksN * 32);
+  const float unscale_hidden = kParts == 2 ? unscale_of(largest[kOfHidden]) : 1.0f;
+  const float unscale_weight = kParts == 2 ? unscale_of(largest[kOfWeight]) : 1.0f;
+  const float scale = __is_same(E, _Float16) ? scale_of(largest[kOfShares]) : 1.0f;
+#pragma unroll
+  for (int i = 0; i < S::kBlocksM; ++i) {
+    const int row = m0 + wave_m + 32 * i + (lane & 31);
+    int label = -1;
+    float w = row < v.rows ? live_weight(v, row, label) : 0.0f;
+    const float lse = w != 0.0f ? v.lse[row] : 0.0f;
+    if (v.diag_flags && first + n0 + wave_n == 0 && lane < 32 && row < v.rows && v.labels[row] >= v.vocab) atomicOr(v.diag_flags, (uint32_t)DGC_DIAG_BAD_INDEX);
+    w *= scale;
+#pragma unroll
+    for (int j = 0; j < S::kBlocksN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int column = n0 + wave_n + 32 * j + 2 * e + 4 * (lane >> 5);
+        alignas(8) E four[kParts][4];
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+          float x = z[i][j][e + f];
+          if constexpr (kParts == 2) x = x * unscale_hidden * unscale_weight;
+          float p = __builtin_amdgcn_exp2f((x - lse) * 1.44269504f);
+          if (first + column + f == label) p -= 1.0f;
+          p = w == 0.0f || column + f >= columns ? 0.0f : p * w;
+          four[0][f] = (E)p;
+          if constexpr (kParts == 2) four[1][f] = (E)(p - (float)four[0][f]);
+        }
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) *reinterpret_cast<uint2*>(shares + p * plane + row * stride + column) = *reinterpret_cast<const uint2*>(four[p]);
+      }
   }
-  return hipGetLastError();
+}
+
+// Sums over a piece (blockIdx.y: a part of it) of shares weight, added to what earlier pieces have left.
+template <typename T, typename S>
+__global__ __launch_bounds__(S::kThreads) void dhidden_kernel(const VocabArgs v, Operand shares, Operand weight, int depth, int part, bool add, float* total) {
+  int tile_m, tile_n;
+  tile_of(blockIdx.x, (v.rows + S::kM - 1) / S::kM, (v.width + S::kN - 1) / S::kN, tile_m, tile_n);
+  const int m0 = tile_m * S::kM, n0 = tile_n * S::kN, from = blockIdx.y * part;
+  Sums x[S::kBlocksM][S::kBlocksN];
+  multiply_tile<typename Inner<T>::E, S, false, true, Inner<T>::kParts>(x, shares, weight, m0, n0, from, depth - from < part ? depth - from : part);
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int wave_m = wave / S::kWavesN * (S::kBlocksM * 32), wave_n = wave % S::kWavesN * (S::kBlocksN * 32);
+  const int64_t pitch = (v.width + 3) / 4 * 4;
+  float* out = total + (int64_t)blockIdx.y * v.rows * pitch;
+#pragma unroll
+  for (int i = 0; i < S::kBlocksM; ++i) {
+    const int row = m0 + wave_m + 32 * i + (lane & 31);
+    if (row >= v.rows) continue;
+#pragma unroll
+    for (int j = 0; j < S::kBlocksN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int column = n0 + wave_n + 32 * j + 2 * e + 4 * (lane >> 5);
+        if (column >= v.width) continue;
+        float4* to = reinterpret_cast<float4*>(out + row * pitch + column);
+        float4 y = make_float4(x[i][j][e], x[i][j][e + 1], x[i][j][e + 2], x[i][j][e + 3]);
+        if (add) {
+          const float4 before = *to;
+          y = make_float4(y.x + before.x, y.y + before.y, y.z + before.z, y.w + before.w);
+        }
+        *to = y;
+      }
+  }
+}
+
+// dhidden from the parts' sums, in their order.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void finish_kernel(const VocabArgs v, const float* total, int parts, const uint32_t* largest) {
+  const int64_t pitch = (v.width + 3) / 4 * 4, size = v.rows * pitch;
+  const float unscale_shares = __is_same(typename Inner<T>::E, _Float16) ? unscale_of(largest[kOfShares]) : 1.0f;
+  const float unscale_weight = Inner<T>::kParts == 2 ? unscale_of(largest[kOfWeight]) : 1.0f;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < size / 4; i += (int64_t)gridDim.x * kThreads) {
+    const int64_t row = i / (pitch / 4);
+    const int column = (int)(i % (pitch / 4)) * 4;
+    float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int p = 0; p < parts; ++p) {
+      const float4 y = *reinterpret_cast<const float4*>(total + p * size + i * 4);
+      x[0] += y.x, x[1] += y.y, x[2] += y.z, x[3] += y.w;
+    }
+    T* to = static_cast<T*>(v.dhidden) + row * v.dhidden_stride + column;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (column + j < v.width) to[j] = from_float<T>(x[j] * unscale_shares * unscale_weight);
+  }
+}
+
+template <typename T, typename S>
+__global__ __launch_bounds__(S::kThreads) void dweight_kernel(const VocabArgs v, Operand shares, Operand hidden, int first, int columns, const uint32_t* largest) {
+  int tile_m, tile_n;
+  tile_of(blockIdx.x, (columns + S::kM - 1) / S::kM, (v.width + S::kN - 1) / S::kN, tile_m, tile_n);
+  const int m0 = tile_m * S::kM, n0 = tile_n * S::kN;
+  Sums x[S::kBlocksM][S::kBlocksN];
+  multiply_tile<typename Inner<T>::E, S, true, true, Inner<T>::kParts>(x, shares, hidden, m0, n0, 0, (v.rows + kDepth - 1) / kDepth * kDepth);
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int wave_m = wave / S::kWavesN * (S::kBlocksM * 32), wave_n = wave % S::kWavesN * (S::kBlocksN * 32);
+  const float unscale_shares = __is_same(typename Inner<T>::E, _Float16) ? unscale_of(largest[kOfShares]) : 1.0f;
+  const float unscale_hidden = Inner<T>::kParts == 2 ? unscale_of(largest[kOfHidden]) : 1.0f;
+  const bool wide = v.dweight_stride % 4 == 0 && reinterpret_cast<uintptr_t>(v.dweight) % (4 * sizeof(T)) == 0;
+#pragma unroll
+  for (int i = 0; i < S::kBlocksM; ++i) {
+    const int row = m0 + wave_m + 32 * i + (lane & 31);
+    if (row >= columns) continue;
+#pragma unroll
+    for (int j = 0; j < S::kBlocksN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int column = n0 + wave_n + 32 * j + 2 * e + 4 * (lane >> 5);
+        T* to = static_cast<T*>(v.dweight) + (int64_t)(first + row) * v.dweight_stride + column;
+        alignas(16) T four[4];
+#pragma unroll
+        for (int f = 0; f < 4; ++f) four[f] = from_float<T>(x[i][j][e + f] * unscale_shares * unscale_hidden);
+        if (wide && column + 4 <= v.width) {
+          if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(four);
+          else *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(four);
+        } else {
+#pragma unroll
+          for (int f = 0; f < 4; ++f)
+            if (column + f < v.width) to[f] = four[f];
+        }
+      }
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------
+int parts_of(int32_t dtype) { return dtype == DGC_F32 ? 2 : 1; }
+
+// Where things lie in the workspace; sizes that do not fall when there are more rows.
+struct Layout {
+  int64_t columns;        // of a packed row
+  int64_t shares_elements, piece_packed;
+  size_t largest, parts, at_label, hidden, weight, shares, total, bytes;
+
+  Layout(int32_t dtype, int64_t rows, int64_t vocab, int64_t width, bool backward) {
+    const int p = parts_of(dtype);
+    columns = up(width, kDepth);
+    const int64_t vocab_pad = up(vocab, kPad), rows_pad = up(rows, kPad);
+    piece_packed = std::min(vocab_pad, std::max<int64_t>(kLeast, kPacked / columns / kPad * kPad));
+    shares_elements = std::min(rows_pad * vocab_pad, std::max(kShares, rows_pad * kLeast));
+    size_t at = 0;
+    auto take = [&](size_t n) {
+      const size_t here = at;
+      at += whole(n);
+      return here;
+    };
+    largest = take(kScales * 4);
+    hidden = take((size_t)rows * columns * 2 * p);
+    weight = take((size_t)piece_packed * columns * 2 * p);
+    if (backward) {
+      shares = take((size_t)shares_elements * 2 * p);
+      total = take((size_t)std::min(kSplitMax * rows, std::max<int64_t>(4096, rows)) * up(width, 4) * 4);
+    } else {
+      parts = take((size_t)rows * ((vocab + 63) / 64) * 8);
+      at_label = take((size_t)rows * 4);
+    }
+    bytes = at;
+  }
+  // Parts of the sums over a piece: more than one only where there are few rows, 4096 rows in all at most.
+  static int64_t splits_at_most(int64_t rows) { return rows == 0 ? 0 : std::max<int64_t>(1, std::min<int64_t>(kSplitMax, 4096 / rows)); }
+};
+
+enum Shape { kLarge, kMiddle, kSmall };
+
+// The largest shape whose tiles are enough for the device's 256 compute units; small ones take four to a unit.
+Shape shape_of(int64_t m, int64_t n) {
+  auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
+  return tiles(256) >= 200 ? kLarge : tiles(128) >= 200 ? kMiddle : kSmall;
+}
+
+template <typename F>
+void with_shape(Shape s, F f) {
+  if (s == kLarge) f(Large{});
+  else if (s == kMiddle) f(Middle{});
+  else f(Small{});
+}
+
+template <typename S>
+uint32_t tiles_of(S, int64_t m, int64_t n) {
+  return (uint32_t)(((m + S::kM - 1) / S::kM) * ((n + S::kN - 1) / S::kN));
+}
+
+template <typename T>
+struct Run {
+  using E = typename Inner<T>::E;
+  static constexpr int kParts = Inner<T>::kParts;
+  const VocabArgs& v;
+  const Layout& at;
+  char* workspace;
+  hipStream_t stream;
+  uint32_t* largest = reinterpret_cast<uint32_t*>(workspace + at.largest);
+
+  // Whether an array can be read as it lies: pieces of 16 bytes, whole steps of the sum, rows that a buffer's 32 bits span.
+  bool direct(const void* x, int64_t stride) const {
+    return kParts == 1 && v.width % kDepth == 0 && stride % 8 == 0 && stride <= 1 << 22 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
+  }
+  Operand as_it_lies(const void* x, int64_t stride, int first, int rows) const {
+    return {static_cast<const char*>(x) + first * stride * 2, stride * 2, 0, rows, v.width * 2};
+  }
+  Operand pack(const void* x, int64_t stride, int first, int rows, bool masked, int scale, size_t to) const {
+    E* out = reinterpret_cast<E*>(workspace + to);
+    const int64_t plane = (int64_t)rows * at.columns;
+    const uint32_t groups = (uint32_t)std::min<int64_t>((rows * at.columns / 8 + kThreads - 1) / kThreads, 8192);
+    pack_kernel<T><<<groups, kThreads, 0, stream>>>(v, static_cast<const T*>(x) + first * stride, stride, rows, masked, largest + scale, out, (int)at.columns, plane);
+    return {reinterpret_cast<const char*>(out), at.columns * 2, plane * 2, rows, (int32_t)at.columns * 2};
+  }
+  Operand weight(int first, int rows) const {
+    return direct(v.weight, v.weight_stride) ? as_it_lies(v.weight, v.weight_stride, first, rows)
+                                             : pack(v.weight, v.weight_stride, first, rows, false, kOfWeight, at.weight);
+  }
+  void scales(bool backward) const {
+    if (kParts == 2 || (backward && __is_same(E, _Float16))) weights_kernel<<<1, 1024, 0, stream>>>(v, largest);
+    if constexpr (kParts == 2) {
+      if (v.rows == 0) return;
+      largest_kernel<<<std::min(v.rows, 2048), kThreads, 0, stream>>>(v, static_cast<const float*>(v.hidden), v.hidden_stride, v.rows, backward, largest + kOfHidden);
+      largest_kernel<<<std::min(v.vocab, 2048), kThreads, 0, stream>>>(v, static_cast<const float*>(v.weight), v.weight_stride, v.vocab, false, largest + kOfWeight);
+    }
+  }
+
+  hipError_t forward() const {
+    float2* parts = reinterpret_cast<float2*>(workspace + at.parts);
+    float* at_label = reinterpret_cast<float*>(workspace + at.at_label);
+    scales(false);
+    const Operand hidden = direct(v.hidden, v.hidden_stride) ? as_it_lies(v.hidden, v.hidden_stride, 0, v.rows)
+                                                             : pack(v.hidden, v.hidden_stride, 0, v.rows, false, kOfHidden, at.hidden);
+    const int piece = direct(v.weight, v.weight_stride) ? v.vocab : (int)at.piece_packed;
+    const Shape s = shape_of(v.rows, std::min(piece, v.vocab));
+    int tiles = 0;
+    for (int first = 0; first < v.vocab; first += piece) {
+      const int columns = std::min(piece, v.vocab - first);
+      const Operand w = weight(first, columns);
+      with_shape(s, [&](auto shape) {
+        using S = decltype(shape);
+        statistics_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, w, (int)at.columns, first, columns, largest, parts, at_label);
+        tiles = (v.vocab + S::kN - 1) / S::kN;
+      });
+    }
+    join_kernel<<<(v.rows + kThreads / 8 - 1) / (kThreads / 8), kThreads, 0, stream>>>(v, parts, at_label, tiles);
+    return hipGetLastError();
+  }
+
+  hipError_t backward() const {
+    E* shares = reinterpret_cast<E*>(workspace + at.shares);
+    float* total = reinterpret_cast<float*>(workspace + at.total);
+    scales(true);
+    const Operand hidden = v.rows > 0 ? pack(v.hidden, v.hidden_stride, 0, v.rows, true, kOfHidden, at.hidden) : Operand{};
+    const int64_t rows_pad = up(v.rows, kPad);
+    int64_t piece = up(v.vocab, kPad);
+    if (rows_pad > 0) piece = std::min({piece, at.shares_elements / rows_pad / kPad * kPad, (int64_t)1 << 22});  // a tile's rows in a buffer's 32 bits
+    if (!direct(v.weight, v.weight_stride)) piece = std::min(piece, at.piece_packed);
+    const int64_t plane = rows_pad * piece;
+    int parts = 1;
+    for (int first = 0; first < v.vocab; first += (int)piece) {
+      const int columns = (int)std::min<int64_t>(piece, v.vocab - first);
+      const Operand w = v.rows > 0 ? weight(first, columns) : Operand{};
+      // whole tiles of shares were written, so that a sum over them may run to the next step's end
+      const Operand p{reinterpret_cast<const char*>(shares), piece * 2, plane * 2, (int32_t)rows_pad, (int32_t)piece * 2};
+      if (v.rows > 0)
+        with_shape(shape_of(v.rows, columns), [&](auto shape) {
+          using S = decltype(shape);
+          shares_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, w, (int)at.columns, first, columns, largest, shares, piece, plane);
+        });
+      if (v.rows > 0 && v.dhidden)
+        with_shape(shape_of(v.rows, v.width), [&](auto shape) {
+          using S = decltype(shape);
+          const uint32_t tiles = tiles_of(shape, v.rows, v.width);
+          const int depth = (int)up(columns, kDepth);
+          if (first == 0) parts = (int)std::max<int64_t>(1, std::min<int64_t>({Layout::splits_at_most(v.rows), (int64_t)(512 / tiles), (int64_t)(depth / 512)}));
+          const int part = (int)up((depth + parts - 1) / parts, kDepth);
+          dhidden_kernel<T, S><<<dim3(tiles, parts), S::kThreads, 0, stream>>>(v, p, w, depth, part, first > 0, total);
+        });
+      if (v.dweight)
+        with_shape(shape_of(columns, v.width), [&](auto shape) {
+          using S = decltype(shape);
+          dweight_kernel<T, S><<<tiles_of(shape, columns, v.width), S::kThreads, 0, stream>>>(v, p, hidden, first, columns, largest);
+        });
+    }
+    if (v.rows > 0 && v.dhidden) finish_kernel<T><<<(uint32_t)std::min<int64_t>(((int64_t)v.rows * up(v.width, 4) / 4 + kThreads - 1) / kThreads, 8192), kThreads, 0, stream>>>(v, total, parts, largest);
+    return hipGetLastError();
+  }
+};
+
+template <typename T>
+hipError_t run(const VocabArgs& v, void* workspace, int32_t dtype, bool backward, hipStream_t stream) {
+  const Layout at(dtype, v.rows, v.vocab, v.width, backward);
+  const Run<T> r{v, at, static_cast<char*>(workspace), stream};
+  return backward ? r.backward() : r.forward();
+}
+
+hipError_t run(const VocabArgs& v, void* workspace, int32_t dtype, bool backward, hipStream_t stream) {
+  switch (dtype) {
+    case DGC_F32: return run<float>(v, workspace, dtype, backward, stream);
+    case DGC_F16: return run<_Float16>(v, workspace, dtype, backward, stream);
+    default: return run<__bf16>(v, workspace, dtype, backward, stream);
+  }
 }
 
 }  // namespace
 
-size_t vocab_workspace_bytes(int32_t /*dtype*/, int32_t rows, int32_t vocab, int32_t width, bool backward) {
-  if (!backward) return whole((size_t)rows * tiles_of(vocab) * 8) + whole((size_t)rows * 4);
-  return whole((size_t)rows * kPiece * 4) + whole((size_t)rows * width * 4);
+size_t vocab_workspace_bytes(int32_t dtype, int32_t rows, int32_t vocab, int32_t width, bool backward) {
+  return Layout(dtype, rows, vocab, width, backward).bytes;
 }
 
-hipError_t launch_vocab_forward(const VocabArgs& v, void* workspace, int32_t dtype, hipStream_t stream) {
-  switch (dtype) {
-    case DGC_F32: return forward<float>(v, workspace, stream);
-    case DGC_F16: return forward<_Float16>(v, workspace, stream);
-    default: return forward<__bf16>(v, workspace, stream);
-  }
-}
+hipError_t launch_vocab_forward(const VocabArgs& a, void* workspace, int32_t dtype, hipStream_t stream) { return run(a, workspace, dtype, false, stream); }
 
-hipError_t launch_vocab_backward(const VocabArgs& v, void* workspace, int32_t dtype, hipStream_t stream) {
-  switch (dtype) {
-    case DGC_F32: return backward<float>(v, workspace, stream);
-    case DGC_F16: return backward<_Float16>(v, workspace, stream);
-    default: return backward<__bf16>(v, workspace, stream);
-  }
-}
+hipError_t launch_vocab_backward(const VocabArgs& a, void* workspace, int32_t dtype, hipStream_t stream) { return run(a, workspace, dtype, true, stream); }
 
 }  // namespace dgc
