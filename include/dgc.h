@@ -645,8 +645,9 @@ dgc_status dgc_linear_attention_workspace_bytes(const dgc_attention* shape, int3
  *   o           must not overlap an input
  *   state_last  device, float[same], or NULL: the state behind the last step (state0 where a sequence has none); may be
  *               state0 itself: a serving loop calls this with max_length = 1 and one array of states
- * Sums and states are binary32, also where the matrix units form them: 16-bit and 32-bit operands are taken apart into
- * bfloat16 parts whose products are exact.  An element that is not finite makes what follows it in its head, and its
+ * Sums and states are binary32, also where the matrix units form them: operands are taken apart into bfloat16 parts whose
+ * products are exact; what goes into a state, and 32-bit results, lose 2^-23 of a term at most, 16-bit results 2^-15 before
+ * they are rounded.  An element that is not finite makes what follows it in its head, and its
  * neighbours up to 63 steps before it, not finite or unspecified.
  * Errors: INVALID_ARG, ALIGNMENT, CAPACITY (workspace, or a shape or stride beyond the limits), HIP.
  */

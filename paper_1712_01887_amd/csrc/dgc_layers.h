@@ -53,7 +53,11 @@ struct VocabArgs {
 };
 
 hipError_t launch_rotary(const RotaryArgs& a, int32_t dtype, hipStream_t stream);
+// Where sequences are cut: the states in front of their segments (of b and c alone), which launch_walk reads from the
+// workspace, as they lie with the walk's state_a and state_c.
+hipError_t launch_walk_states(const WalkArgs& a, void* workspace, int32_t dtype, hipStream_t stream);
 hipError_t launch_walk(const WalkArgs& a, void* workspace, int32_t dtype, hipStream_t stream);
+size_t walk_workspace_bytes(int64_t rows, int64_t sequences, int64_t max_length, int32_t heads, int32_t da, int32_t dc);
 int64_t walk_workgroups(int64_t sequences, int32_t heads, int32_t dc);
 hipError_t launch_vocab_forward(const VocabArgs& a, void* workspace, int32_t dtype, hipStream_t stream);
 hipError_t launch_vocab_backward(const VocabArgs& a, void* workspace, int32_t dtype, hipStream_t stream);

@@ -148,7 +148,7 @@ dgc_status dgc_linear_attention_workspace_bytes(const dgc_attention* shape, int3
   const dgc_status st = check_attention(shape);
   if (st != DGC_OK) return st;
   if (!bytes || (backward != 0 && backward != 1)) return DGC_ERR_INVALID_ARG;
-  *bytes = 0;
+  *bytes = walk_workspace_bytes(shape->rows, shape->sequences, shape->max_length, shape->heads, shape->key_dim, shape->value_dim);
   return DGC_OK;
 }
 
@@ -190,7 +190,10 @@ dgc_status dgc_linear_attention_forward(const dgc_attention* s, const dgc_heads*
   w.row_offsets = s->row_offsets;
   w.scale = 1.0f;
   w.out_scale = s->scale;
-  return hip_ok(launch_walk(w, workspace, s->dtype, static_cast<hipStream_t>(stream_)), "launch attention kernels") ? DGC_OK : DGC_ERR_HIP;
+  const hipStream_t stream = static_cast<hipStream_t>(stream_);
+  hipError_t err = launch_walk_states(w, workspace, s->dtype, stream);
+  if (err == hipSuccess) err = launch_walk(w, workspace, s->dtype, stream);
+  return hip_ok(err, "launch attention kernels") ? DGC_OK : DGC_ERR_HIP;
 }
 
 dgc_status dgc_linear_attention_backward(const dgc_attention* s, const dgc_heads* q, const dgc_heads* k, const dgc_heads* v,
@@ -227,7 +230,17 @@ dgc_status dgc_linear_attention_backward(const dgc_attention* s, const dgc_heads
   w.sequences = s->sequences;
   w.max_length = s->max_length;
   w.row_offsets = s->row_offsets;
-  // dq: the forward walk with do in q's place, and k and v changed round, and so the state's rows and columns.
+  // The states as in the forward call, then dq: the forward walk with do in q's place, and k and v changed round, and so
+  // the state's rows and columns.
+  w.b = *k;
+  w.c = *v;
+  w.first = state0;
+  w.state_a = s->value_dim;
+  w.state_c = 1;
+  w.da = s->key_dim;
+  w.dc = s->value_dim;
+  w.scale = 1.0f;
+  hipError_t err = launch_walk_states(w, workspace, s->dtype, stream);
   w.a = *d_o;
   w.b = *v;
   w.c = *k;
@@ -239,7 +252,7 @@ dgc_status dgc_linear_attention_backward(const dgc_attention* s, const dgc_heads
   w.dc = s->key_dim;
   w.scale = 1.0f;
   w.out_scale = s->scale;
-  hipError_t err = launch_walk(w, workspace, s->dtype, stream);
+  if (err == hipSuccess) err = launch_walk(w, workspace, s->dtype, stream);
   // dk and dv: from the last step to the first, with the state's gradient for a state.  It is read by both before the
   // second one, which alone writes it, leaves it behind.
   w.reverse = true;
@@ -247,6 +260,17 @@ dgc_status dgc_linear_attention_backward(const dgc_attention* s, const dgc_heads
   w.scale = s->scale;
   w.out_scale = 1.0f;
   w.first = dstate_last;
+  w.b = *q;
+  w.c = *d_o;
+  w.state_a = s->value_dim;
+  w.state_c = 1;
+  w.da = s->key_dim;
+  w.dc = s->value_dim;
+  if (err == hipSuccess) err = launch_walk_states(w, workspace, s->dtype, stream);
+  w.state_a = 1;
+  w.state_c = s->value_dim;
+  w.da = s->value_dim;
+  w.dc = s->key_dim;
   w.a = *v;
   w.b = *d_o;
   w.c = *q;

@@ -32,12 +32,15 @@ def rotary(x, positions, f, half, magnitude, inverse):
 
 
 # --- linear attention ---------------------------------------------------------
-def _walk(a, b, c, log_decay, first, scale, out_scale, late):
+def _walk(a, b, c, log_decay, first, scale, out_scale, late, dtype):
     """out, last and their bounds for one sequence: a, b [steps, heads, da], c [steps, heads, dc].
 
     `size` is the same recurrence of absolute values, `off` bounds what a state is off: a step rounds it a few times (8:
     the product, the parts that are left out, sums of up to 64 products inside a matrix unit are counted where they are
-    read), and a power of the decay is off by the rounding of its exponent."""
+    read), and a power of the decay is off by the rounding of its exponent.  Shares and a state that is read are taken as two
+    bfloat16 parts for results in 16 bits, the first cut off (2^-7 of it is left at most), the second rounded (2^-8 of that):
+    2^-15 of each term."""
+    parts = 0.0 if dtype == "f32" else 2.0 ** -15
     steps, heads, da = a.shape
     d = np.exp(log_decay.astype(np.float64))[:, None, None]
     rate = np.abs(np.where(np.isinf(log_decay), 0.0, log_decay))[:, None, None]
@@ -59,13 +62,13 @@ def _walk(a, b, c, log_decay, first, scale, out_scale, late):
         out[t] = out_scale * np.einsum("hi,hij->hj", a[t], state)
         absolute = np.abs(a[t])
         bound[t] = abs(out_scale) * (np.einsum("hi,hij->hj", absolute, off) +
-                                     2 * (da + 8) * EPS * np.einsum("hi,hij->hj", absolute, size))
+                                     (2 * (da + 8) * EPS + parts) * np.einsum("hi,hij->hj", absolute, size))
         if late:
             decay()
     return out, bound, state, off
 
 
-def attention(q, k, v, log_decay, state0, scale, lengths, do=None, dstate_last=None):
+def attention(q, k, v, log_decay, state0, scale, lengths, do=None, dstate_last=None, dtype="f32"):
     """{name: (value, bound)}: o, state_last, and with `do` dq, dk, dv, dstate0."""
     n, heads, dk, dv = q.shape[0], q.shape[1], q.shape[2], v.shape[2]
     result = {name: (np.zeros((n, heads, d)), np.zeros((n, heads, d))) for name, d in
@@ -77,17 +80,17 @@ def attention(q, k, v, log_decay, state0, scale, lengths, do=None, dstate_last=N
     for s, length in enumerate(lengths):
         there = slice(start, start + length)
         first = None if state0 is None else state0[s]
-        out = _walk(q[there], k[there], v[there], log_decay, first, 1.0, scale, False)
+        out = _walk(q[there], k[there], v[there], log_decay, first, 1.0, scale, False, dtype)
         result["o"][0][there], result["o"][1][there] = out[:2]
         result["state_last"][0][s], result["state_last"][1][s] = out[2:]
         if do is not None:
             back = lambda x: x[there][::-1]
-            out = _walk(do[there], v[there], k[there], log_decay, turned(first), 1.0, scale, False)
+            out = _walk(do[there], v[there], k[there], log_decay, turned(first), 1.0, scale, False, dtype)
             result["dq"][0][there], result["dq"][1][there] = out[:2]
             flow = None if dstate_last is None else dstate_last[s]
-            out = _walk(back(v), back(do), back(q), log_decay, turned(flow), scale, 1.0, True)
+            out = _walk(back(v), back(do), back(q), log_decay, turned(flow), scale, 1.0, True, dtype)
             result["dk"][0][there], result["dk"][1][there] = out[0][::-1], out[1][::-1]
-            out = _walk(back(k), back(q), back(do), log_decay, flow, scale, 1.0, True)
+            out = _walk(back(k), back(q), back(do), log_decay, flow, scale, 1.0, True, dtype)
             result["dv"][0][there], result["dv"][1][there] = out[0][::-1], out[1][::-1]
             result["dstate0"][0][s], result["dstate0"][1][s] = out[2:]
         start += length

@@ -45,7 +45,7 @@ def check(lengths, heads, dk, dv, dtype, packed=True, max_length=None, carried=T
     rates = torch.from_numpy(decay).cuda()
     plan.dgc_linear_attention_forward(t["q"], t["k"], t["v"], rates, state0, out["o"][1], last)
     want = L.attention(x["q"], x["k"], x["v"], decay, x["state0"] if carried else None, scale, lengths,
-                       x["do"] if train else None, x["dstate_last"] if carried else None)
+                       x["do"] if train else None, x["dstate_last"] if carried else None, dtype)
     names = ["o"]
     if train:
         plan.dgc_linear_attention_backward(t["q"], t["k"], t["v"], rates, state0, t["do"], dlast, out["dq"][1],
@@ -133,7 +133,8 @@ def test_prompt_then_single_tokens(dtype):
     heads, dk, dv, count, prompt, more = 3, 64, 80, 5, 90, 6
     x = inputs(count * (prompt + more), count, heads, dk, dv, dtype, 9)
     rates = torch.from_numpy(np.resize(DECAYS, heads)).cuda()
-    want = L.attention(x["q"], x["k"], x["v"], np.resize(DECAYS, heads), None, 0.5, [prompt + more] * count)
+    want = L.attention(x["q"], x["k"], x["v"], np.resize(DECAYS, heads), None, 0.5, [prompt + more] * count,
+                       dtype=dtype)
     part = lambda name, lo, hi: torch.from_numpy(
         x[name].reshape(count, prompt + more, heads, -1)[:, lo:hi].reshape(count * (hi - lo), heads, -1)).to(dtype_of(dtype)).cuda()
     of = lambda r, lo, hi: r.reshape(count, prompt + more, heads, dv)[:, lo:hi].reshape(-1, heads, dv)
@@ -180,7 +181,7 @@ def test_large_values_in_sixteen_bits():
     o, last = torch.empty(n, 1, d, dtype=torch.float16, device="cuda"), torch.empty(1, 1, d, d, device="cuda")
     plan = B.LinearAttention(1, n, 1, d, d, torch.float16, backward=False)
     plan.dgc_linear_attention_forward(t["q"], t["k"], t["v"], torch.zeros(1, device="cuda"), None, o, last)
-    want = L.attention(x["q"], x["k"], x["v"], np.zeros(1, np.float32), None, 1.0, [n])
+    want = L.attention(x["q"], x["k"], x["v"], np.zeros(1, np.float32), None, 1.0, [n], dtype="f16")
     assert np.abs(want["state_last"][0]).max() > 1e6 and np.abs(want["o"][0]).max() < 65504
     close(o, *want["o"], "f16", "o")
     close(last, *want["state_last"], "f32", "state_last")
