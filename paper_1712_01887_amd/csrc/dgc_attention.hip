@@ -13,67 +13,101 @@
 namespace dgc {
 namespace {
 
-constexpr int kColumns = 32;   // columns of the state to a workgroup
-constexpr int kParts = 8;      // threads that share a column's rows
-constexpr int kThreads = kColumns * kParts;
-constexpr int kRows = DGC_HEAD_MAX / kParts;
+// ---- steps -------------------------------------------------------------------------------------
+constexpr int kColumns = 32;  // columns of the state to a workgroup, four to a thread
+constexpr int kThreads = 256;
+constexpr int kRowThreads = kThreads * 4 / kColumns;
+constexpr int kRows = DGC_HEAD_MAX / kRowThreads;  // to a thread, kRowThreads apart
 
-// One step after the other.  A workgroup has kColumns columns of a state: a thread has every kParts-th element of one of
-// them.  out_i = sum over the rows is added up over the kParts threads in LDS, in their order.
+// One step after the other: what bounds it is the state, which is read and written once.  A thread has four columns of up to
+// kRows of its rows in registers; o is summed over the eight rows of a wavefront by exchanges, over the wavefronts in LDS, in
+// their order.  Everything that a step reads is asked for at once.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void walk_steps_kernel(const WalkArgs w) {
-  __shared__ float vectors[2][DGC_HEAD_MAX];
-  __shared__ float sums[kParts][kColumns];
+  __shared__ float4 sums[2][kThreads / 64][kColumns / 4];
   const int tiles = (w.dc + kColumns - 1) / kColumns;
   const int tile = (int)(blockIdx.x % tiles), head = (int)(blockIdx.x / tiles % w.heads);
   const int64_t sequence = blockIdx.x / tiles / w.heads;
   const int64_t lo = w.row_offsets ? w.row_offsets[sequence] : sequence * w.max_length;
   const int64_t hi = w.row_offsets ? w.row_offsets[sequence + 1] : lo + w.max_length;
   const SequenceRows rows(lo, hi, w.rows, w.max_length);
-  const int column = tile * kColumns + (int)threadIdx.x % kColumns, part = (int)threadIdx.x / kColumns;
-  const bool mine = column < w.dc;
-  const int64_t state = (sequence * w.heads + head) * w.da * w.dc + (int64_t)column * w.state_c;
-  float s[kRows];
+  const int column = tile * kColumns + 4 * ((int)threadIdx.x % (kColumns / 4)), row0 = (int)threadIdx.x / (kColumns / 4);
+  const int columns = w.dc - column;  // that are there, from this thread's first on
+  const bool whole = columns >= 4 && w.state_c == 1 && w.state_a % 4 == 0;
+  const bool whole_first = whole && reinterpret_cast<uintptr_t>(w.first) % 16 == 0, whole_last = whole && reinterpret_cast<uintptr_t>(w.last) % 16 == 0;
+  const int64_t at = (sequence * w.heads + head) * w.da * w.dc + (int64_t)column * w.state_c;
+  float s[kRows][4];
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
-    const int r = i * kParts + part;
-    s[i] = w.first && mine && r < w.da ? w.first[state + (int64_t)r * w.state_a] : 0.0f;
+    const int r = row0 + i * kRowThreads;
+    const float* from = w.first + at + (int64_t)r * w.state_a;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[i][j] = 0.0f;
+    if (!w.first || r >= w.da) continue;
+    if (whole_first) {
+      const float4 x = *reinterpret_cast<const float4*>(from);
+      s[i][0] = x.x, s[i][1] = x.y, s[i][2] = x.z, s[i][3] = x.w;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < columns) s[i][j] = from[(int64_t)j * w.state_c];
+    }
   }
-  const float d = exp2f(w.log_decay[head] * 1.44269504f);
+  const float d = exp2f(w.log_decay[head] * 1.44269504f), before = w.late ? 1.0f : d, after = w.late ? d : 1.0f;
   const T* a = static_cast<const T*>(w.a.data) + head * w.a.head_stride;
   const T* b = static_cast<const T*>(w.b.data) + head * w.b.head_stride;
-  const T* c = static_cast<const T*>(w.c.data) + head * w.c.head_stride;
-  T* out = static_cast<T*>(w.out.data) + head * w.out.head_stride;
+  const T* c = static_cast<const T*>(w.c.data) + head * w.c.head_stride + column;
+  T* out = static_cast<T*>(w.out.data) + head * w.out.head_stride + column;
   for (int64_t t = 0; t < rows.length; ++t) {
     const int64_t row = rows.begin + (w.reverse ? rows.length - 1 - t : t);
-    __syncthreads();
-    for (int i = threadIdx.x; i < w.da; i += kThreads) {
-      vectors[0][i] = to_float(a[row * w.a.row_stride + i]);
-      vectors[1][i] = to_float(b[row * w.b.row_stride + i]);
-    }
-    const float value = mine ? to_float(c[row * w.c.row_stride + column]) * w.scale : 0.0f;
-    __syncthreads();
-    float sum = 0.0f;
+    float x[kRows], y[kRows], z[4], sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-      const int r = i * kParts + part;
-      if (r < w.da) {
-        s[i] = fmaf(vectors[1][r], value, w.late ? s[i] : d * s[i]);
-        sum = fmaf(vectors[0][r], s[i], sum);
-        if (w.late) s[i] *= d;
-      }
+      const int r = row0 + i * kRowThreads;
+      x[i] = r < w.da ? to_float(a[row * w.a.row_stride + r]) : 0.0f;
+      y[i] = r < w.da ? to_float(b[row * w.b.row_stride + r]) : 0.0f;
     }
-    sums[part][threadIdx.x % kColumns] = sum;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) z[j] = j < columns ? to_float(c[row * w.c.row_stride + j]) * w.scale : 0.0f;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i)
+      if (row0 + i * kRowThreads < w.da)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[i][j] = fmaf(y[i], z[j], before * s[i][j]);
+          sum[j] = fmaf(x[i], s[i][j], sum[j]);
+          s[i][j] *= after;
+        }
+#pragma unroll
+    for (int m = kColumns / 4; m < 64; m *= 2)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum[j] += __shfl_xor(sum[j], m);
+    // of two rows of sums the other one may still be read
+    if (threadIdx.x % 64 < kColumns / 4) sums[t & 1][threadIdx.x / 64][threadIdx.x % 64] = make_float4(sum[0], sum[1], sum[2], sum[3]);
     __syncthreads();
-    if (part == 0 && mine) {
-      for (int i = 1; i < kParts; ++i) sum += sums[i][threadIdx.x];
-      out[row * w.out.row_stride + column] = from_float<T>(sum * w.out_scale);
+    if (threadIdx.x < kColumns / 4) {
+      for (int i = 1; i < kThreads / 64; ++i) {
+        const float4 other = sums[t & 1][i][threadIdx.x];
+        sum[0] += other.x, sum[1] += other.y, sum[2] += other.z, sum[3] += other.w;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < columns) out[row * w.out.row_stride + j] = from_float<T>(sum[j] * w.out_scale);
     }
   }
+  if (!w.last) return;
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
-    const int r = i * kParts + part;
-    if (w.last && mine && r < w.da) w.last[state + (int64_t)r * w.state_a] = s[i];
+    const int r = row0 + i * kRowThreads;
+    float* to = w.last + at + (int64_t)r * w.state_a;
+    if (r >= w.da) continue;
+    if (whole_last) {
+      *reinterpret_cast<float4*>(to) = make_float4(s[i][0], s[i][1], s[i][2], s[i][3]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < columns) to[(int64_t)j * w.state_c] = s[i][j];
+    }
   }
 }
 
@@ -131,7 +165,7 @@ __device__ __forceinline__ void multiply_parts(const Eight (&a)[A], const Eight 
 // d^n of a head.
 struct Decay {
   float log2;
-  __device__ __forceinline__ float power(int64_t n) const { return n > 0 ? __builtin_amdgcn_exp2f((float)n * log2) : 1.0f; }
+  __device__ __forceinline__ float power(int n) const { return n > 0 ? __builtin_amdgcn_exp2f((float)n * log2) : 1.0f; }
 };
 
 // Where rows of a and b lie in LDS, and of c.  A row of a or b is read two ways: 16 bytes by each of 16 lanes that have a row
@@ -167,35 +201,50 @@ struct Rows {
   }
 };
 
-// Pieces of 8 elements of a chunk's rows on their way from memory to LDS, by THREADS threads.
-template <typename T, int DIM, int THREADS>
+// 16 bytes at any element's address, which loads take.
+typedef uint32_t Loose __attribute__((ext_vector_type(4), aligned(2)));
+
+// Pieces of 8 elements of a chunk's rows on their way from memory to LDS, by THREADS threads.  NARROW: of rows that may be
+// shorter than a piece, element by element; were both ways in one kernel, what they leave in registers would be waited for
+// where they meet.
+template <typename T, int DIM, int THREADS, bool NARROW>
 struct Pieces {
   static constexpr int kCount = kChunk * DIM / 8 / THREADS;
   static_assert(kCount * THREADS * 8 == kChunk * DIM, "whole pieces");
   alignas(16) T held[kCount][8];
 
-  // `rows` rows from `base` on, `stride` elements apart, `dim` elements of each; zeros elsewhere.
-  __device__ __forceinline__ void load(const T* base, int64_t stride, int rows, int dim, bool wide) {
+  // Rows [skipped, kChunk) of the chunk, of which row `skipped` is at base + skipped * stride; `dim` elements of each; zeros
+  // elsewhere.  A piece that the row ends
+  // in is loaded as the row's last eight elements; store() moves them down, so that nothing waits for the load here.
+  __device__ __forceinline__ void load(const T* base, int64_t stride, int skipped, int dim) {
 #pragma unroll
     for (int i = 0; i < kCount; ++i) {
       const int piece = i * THREADS + (int)threadIdx.x, row = piece / (DIM / 8), column = piece % (DIM / 8) * 8;
-      const T* from = base + row * stride + column;
-      if (wide) {
-        uint4* to = reinterpret_cast<uint4*>(held[i]);
-        const bool there = row < rows && column < dim;
+      const bool there = row >= skipped && column < dim;
+      Loose* to = reinterpret_cast<Loose*>(held[i]);
+      if constexpr (!NARROW) {
+        const T* from = base + row * stride + (column + 8 <= dim ? column : dim - 8);
 #pragma unroll
-        for (int w = 0; w < (int)sizeof(T) / 2; ++w) to[w] = there ? reinterpret_cast<const uint4*>(from)[w] : make_uint4(0, 0, 0, 0);
+        for (int w = 0; w < (int)sizeof(T) / 2; ++w) to[w] = there ? reinterpret_cast<const Loose*>(from)[w] : Loose{0, 0, 0, 0};
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) held[i][j] = row < rows && column + j < dim ? from[j] : (T)0.0f;
+        for (int j = 0; j < 8; ++j) held[i][j] = there && column + j < dim ? base[row * stride + column + j] : (T)0.0f;
       }
     }
   }
   template <typename Store>
-  __device__ __forceinline__ void store(Store put) const {
+  __device__ __forceinline__ void store(int dim, Store put) {
+    const int missing = NARROW ? 0 : -dim & 7;  // of the last piece
 #pragma unroll
     for (int i = 0; i < kCount; ++i) {
-      const int piece = i * THREADS + (int)threadIdx.x, row = piece / (DIM / 8);
+      const int piece = i * THREADS + (int)threadIdx.x, row = piece / (DIM / 8), column = piece % (DIM / 8) * 8;
+      if (missing) {
+        const int down = column < dim && column + 8 > dim ? missing : 0;
+#pragma unroll
+        for (int by = 4; by > 0; by /= 2)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) held[i][j] = down & by ? (j + by < 8 ? held[i][(j + by) & 7] : (T)0.0f) : held[i][j];
+      }
       Eight parts[kPartsOf<T>];
       if constexpr (__is_same(T, __bf16)) {
         parts[0] = *reinterpret_cast<const Eight*>(held[i]);
@@ -274,7 +323,7 @@ struct Slots {
 //
 // Of a chunk every wavefront forms a b^T for itself, as 32 x 32 shares whose layout is that of the operand they are next, and
 // so is the state's: neither goes through LDS.  While a chunk is worked on the next one's rows are on their way to registers.
-template <typename T, int DA, int WAVES, bool OUT>
+template <typename T, int DA, int WAVES, bool OUT, bool NARROW>
 __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) void walk_chunks_kernel(const WalkArgs w, const Slots slots) {
   constexpr int kThreads = 64 * WAVES, kInput = kPartsOf<T>, kMiddle = kMiddleParts<T>, kBlocks = DA / 32, DC = 32 * WAVES;
   constexpr int kWeight = __is_same(T, __bf16) ? 2 : 3, kWeightIn = 3;
@@ -293,52 +342,53 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
 
   Block state[kBlocks];
   const float* from = OUT && slots.steps > 0 && !seg.first ? slots.states + (seg.slot * w.heads + head) * w.da * w.dc : OUT && w.first ? w.first + (seg.sequence * w.heads + head) * w.da * w.dc : nullptr;
+  if (from) from += (int64_t)(4 * h) * w.state_a + (int64_t)column * w.state_c;
 #pragma unroll
   for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int r = 32 * i + 8 * (e / 4) + 4 * h + e % 4;
-      state[i][e] = from && r < w.da && column < w.dc ? from[(int64_t)r * w.state_a + (int64_t)column * w.state_c] : 0.0f;
-    }
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool there = from && 32 * i + 8 * q + 4 * h + j < w.da && column < w.dc;
+        state[i][4 * q + j] = there ? from[(32 * i + 8 * q + j) * w.state_a] : 0.0f;
+      }
 
   const int64_t sign = w.reverse ? -1 : 1;
   const int64_t step_a = sign * w.a.row_stride, step_b = sign * w.b.row_stride, step_c = sign * w.c.row_stride;
   const T* a = OUT ? static_cast<const T*>(w.a.data) + head * w.a.head_stride + seg.row * w.a.row_stride : nullptr;
   const T* b = static_cast<const T*>(w.b.data) + head * w.b.head_stride + seg.row * w.b.row_stride;
   const T* c = static_cast<const T*>(w.c.data) + head * w.c.head_stride + seg.row * w.c.row_stride + column0;
-  auto wide = [](const dgc_heads& x, int dim) {
-    return reinterpret_cast<uintptr_t>(x.data) % 16 == 0 && (x.row_stride * sizeof(T)) % 16 == 0 && (x.head_stride * sizeof(T)) % 16 == 0 && dim % 8 == 0;
-  };
-  const bool wide_a = OUT && wide(w.a, w.da), wide_b = wide(w.b, w.da), wide_c = wide(w.c, w.dc);
-
-  // weights: of a share of step j in step i = lane % 32, of a step that goes into the state
-  float share_weight[16], state_weight[2][8];
+  // Weights.  Of a share of step j in step i = lane % 32: d^(i - j), from LDS at j - i + 31, zeros behind 31.  Of a step j that
+  // goes into the state: d^(31 - j); of the lane's eight, j = 16 k + 4 h + {0 .. 3, 8 .. 11}, a power of its own for either k,
+  // times one that all lanes have.  A segment's first chunk is the short one, if one is, and takes the window's end.
+  __shared__ float share_weights[2 * kChunk];
+  if (threadIdx.x < 2 * kChunk) share_weights[threadIdx.x] = threadIdx.x < kChunk ? d.power(kChunk - 1 - (int)threadIdx.x) * w.scale : 0.0f;
+  const int behind = 4 * h - (lane & 31) + kChunk - 1;
+  float uniform[8];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int j = 8 * (e / 4) + 4 * h + e % 4;
-    share_weight[e] = j <= (lane & 31) ? d.power((lane & 31) - j) * w.scale : 0.0f;
-    state_weight[e / 8][e % 8] = d.power(kChunk - 1 - j + w.late) * w.scale;
-  }
-  const float query_weight = d.power((lane & 31) + 1 - w.late);
+  for (int e = 0; e < 8; ++e) uniform[e] = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, d.power(e < 4 ? 11 - e : 7 - e) * w.scale)));
+  const float into_weight[2] = {d.power(20 - 4 * h + w.late), d.power(4 - 4 * h + w.late)};
+  const int short_by = (int)(-seg.length & (kChunk - 1));
+  float query_weight = d.power((lane & 31) - short_by + 1 - w.late), kept = d.power(kChunk - short_by);
 
-  Pieces<T, DA, kThreads> next_a, next_b;
-  Pieces<T, DC, kThreads> next_c;
+  Pieces<T, DA, kThreads, NARROW> next_a, next_b;
+  Pieces<T, DC, kThreads, NARROW> next_c;
   auto load = [&](int64_t at) {
-    const int rows = (int)(seg.length - at < kChunk ? seg.length - at : kChunk);
-    if constexpr (OUT) next_a.load(a + at * step_a, step_a, rows, w.da, wide_a);
-    next_b.load(b + at * step_b, step_b, rows, w.da, wide_b);
-    next_c.load(c + at * step_c, step_c, rows, w.dc - column0, wide_c);
+    const int skipped = at < 0 ? (int)-at : 0;
+    if constexpr (OUT) next_a.load(a + at * step_a, step_a, skipped, w.da);
+    next_b.load(b + at * step_b, step_b, skipped, w.da);
+    next_c.load(c + at * step_c, step_c, skipped, w.dc - column0);
   };
-  if (seg.length > 0) load(0);
+  if (seg.length > 0) load(-short_by);
   int buffer = 0;
-  for (int64_t at = 0; at < seg.length; at += kChunk, buffer = (buffer + 1) % kBuffers) {
-    const int rows = (int)(seg.length - at < kChunk ? seg.length - at : kChunk);
-    if (kBuffers == 1 && at > 0) __syncthreads();
-    if constexpr (OUT) next_a.store([&](int p, int row, int piece, Eight x) { R::store(lds_a[buffer] + p * R::kElements, row, piece, x); });
-    next_b.store([&](int p, int row, int piece, Eight x) { R::store(lds_b[buffer] + p * R::kElements, row, piece, x); });
-    next_c.store([&](int p, int row, int piece, Eight x) { Cs::store(lds_c[buffer] + p * Cs::kElements, row, piece, x); });
+  for (int64_t at = -short_by; at < seg.length; at += kChunk, buffer = (buffer + 1) % kBuffers) {
+    if (kBuffers == 1) __syncthreads();
+    if constexpr (OUT) next_a.store(w.da, [&](int p, int row, int piece, Eight x) { R::store(lds_a[buffer] + p * R::kElements, row, piece, x); });
+    next_b.store(w.da, [&](int p, int row, int piece, Eight x) { R::store(lds_b[buffer] + p * R::kElements, row, piece, x); });
+    next_c.store(w.dc - column0, [&](int p, int row, int piece, Eight x) { Cs::store(lds_c[buffer] + p * Cs::kElements, row, piece, x); });
     __syncthreads();  // of two buffers, the other one was read before the barrier of the chunk before this one
     if (at + kChunk < seg.length) load(at + kChunk);
+    __builtin_amdgcn_sched_barrier(0);
 
     Eight turned_c[2][kInput];
 #pragma unroll
@@ -375,7 +425,7 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         out[e] *= query_weight;
-        shares[e] *= share_weight[e];
+        shares[e] *= share_weights[behind + 8 * (e / 4) + e % 4];
       }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -386,7 +436,7 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
         take_apart(s, part);
         multiply_parts<kWeight>(turned_c[k], part, out);
       }
-      if ((lane & 31) < rows) {
+      if (at + (lane & 31) >= 0) {
         T* to = static_cast<T*>(w.out.data) + head * w.out.head_stride + (seg.row + sign * (at + (lane & 31))) * w.out.row_stride + column0 + 32 * wave;
         const bool whole = reinterpret_cast<uintptr_t>(w.out.data) % (4 * sizeof(T)) == 0 && (w.out.row_stride | w.out.head_stride) % 4 == 0;
 #pragma unroll
@@ -407,11 +457,7 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
       }
     }
 
-    if (rows < kChunk) {  // the segment's last chunk
-#pragma unroll
-      for (int e = 0; e < 16; ++e) state_weight[e / 8][e % 8] = d.power(rows - 1 - (8 * (e / 4) + 4 * h + e % 4) + w.late) * w.scale;
-    }
-    const float kept = d.power(rows);
+    __builtin_amdgcn_sched_barrier(0);
     Eight into[2][kIntoState];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -421,10 +467,11 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
         x[e] = 0.0f;
 #pragma unroll
         for (int p = kInput - 1; p >= 0; --p) x[e] += (float)turned_c[k][p][e];
-        x[e] *= state_weight[k][e];
+        x[e] *= into_weight[k] * uniform[e];
       }
       take_apart(x, into[k]);
     }
+    __builtin_amdgcn_sched_barrier(0);
     Eight turned_b[2][kInput];
     auto read = [&](int k) {
 #pragma unroll
@@ -438,17 +485,27 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
       multiply_parts<kWeightIn>(turned_b[k % 2], into[k % 2], state[k / 2]);
       __builtin_amdgcn_sched_barrier(0);
     }
+    if (at < 0) {
+      query_weight = d.power((lane & 31) + 1 - w.late);
+      kept = d.power(kChunk);
+    }
   }
 
   float* to = OUT ? (seg.last && w.last ? w.last + (seg.sequence * w.heads + head) * w.da * w.dc : nullptr)
                   : slots.states + ((seg.slot + 1) * w.heads + head) * w.da * w.dc;
+  // the compiler would keep the addresses of the first loads until here
+  int again = lane;
+  asm volatile("" : "+v"(again));
+  const int column_again = column0 + 32 * wave + (again & 31);
+  if (!to || column_again >= w.dc) return;
+  float* first = to + (int64_t)(4 * (again >> 5)) * w.state_a + (int64_t)column_again * w.state_c;
 #pragma unroll
   for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int r = 32 * i + 8 * (e / 4) + 4 * h + e % 4;
-      if (to && r < w.da && column < w.dc) to[(int64_t)r * w.state_a + (int64_t)column * w.state_c] = state[i][e];
-    }
+    for (int q = 0; q < 4; ++q, first += 8 * (int64_t)w.state_a)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (32 * i + 8 * q + 4 * (again >> 5) + j < w.da) first[j * w.state_a] = state[i][4 * q + j];
 }
 
 // What the segments of a sequence add, joined to the state in front of each: slot i + 1 of a sequence holds what its segment i
@@ -460,7 +517,7 @@ __global__ __launch_bounds__(256) void join_kernel(const WalkArgs w, const Slots
   const int64_t sequence = blockIdx.x / groups / w.heads, element = blockIdx.x % groups * 256 + threadIdx.x;
   const int64_t length = Segment::rows_of(w, sequence).length, segments = (length + slots.steps - 1) / slots.steps;
   if (element >= size) return;
-  const float kept = Decay{w.log_decay[head] * 1.44269504f}.power(slots.steps);
+  const float kept = Decay{w.log_decay[head] * 1.44269504f}.power((int)slots.steps);
   float state = w.first ? w.first[(sequence * w.heads + head) * size + element] : 0.0f;
   float* at = slots.states + ((Segment::first_slot(w, sequence, slots.steps) + 1) * w.heads + head) * size + element;
   for (int64_t i = 0; i + 1 < segments; i += kAhead) {
@@ -476,18 +533,22 @@ __global__ __launch_bounds__(256) void join_kernel(const WalkArgs w, const Slots
   }
 }
 
+template <typename T, int DA, int WAVES, bool OUT, bool NARROW>
+hipError_t launch_chunks(const WalkArgs& w, const Slots& slots, hipStream_t stream) {
+  const uint32_t groups = (uint32_t)(slots.count * w.heads * ((w.dc + 32 * WAVES - 1) / (32 * WAVES)));
+  walk_chunks_kernel<T, DA, WAVES, OUT, NARROW><<<groups, 64 * WAVES, 0, stream>>>(w, slots);
+  return hipGetLastError();
+}
+
 template <typename T, int DA, bool OUT>
 hipError_t launch_chunks(const WalkArgs& w, const Slots& slots, hipStream_t stream) {
-  const int waves = w.dc <= 32 ? 1 : w.dc <= 64 ? 2 : 4;
-  const uint32_t groups = (uint32_t)(slots.count * w.heads * ((w.dc + 32 * waves - 1) / (32 * waves)));
-  if (waves == 1) walk_chunks_kernel<T, DA, 1, OUT><<<groups, 64, 0, stream>>>(w, slots);
-  else if (waves == 2) walk_chunks_kernel<T, DA, 2, OUT><<<groups, 128, 0, stream>>>(w, slots);
-  else walk_chunks_kernel<T, DA, 4, OUT><<<groups, 256, 0, stream>>>(w, slots);
-  return hipGetLastError();
+  return w.dc <= 32 ? launch_chunks<T, DA, 1, OUT, false>(w, slots, stream)
+         : w.dc <= 64 ? launch_chunks<T, DA, 2, OUT, false>(w, slots, stream) : launch_chunks<T, DA, 4, OUT, false>(w, slots, stream);
 }
 
 template <typename T, bool OUT>
 hipError_t launch_chunks(const WalkArgs& w, const Slots& slots, hipStream_t stream) {
+  if (w.da < 8 || w.dc < 8) return w.da <= 64 ? launch_chunks<T, 64, 4, OUT, true>(w, slots, stream) : launch_chunks<T, 256, 4, OUT, true>(w, slots, stream);
   return w.da <= 64 ? launch_chunks<T, 64, OUT>(w, slots, stream) : w.da <= 128 ? launch_chunks<T, 128, OUT>(w, slots, stream) : launch_chunks<T, 256, OUT>(w, slots, stream);
 }
 

@@ -6,6 +6,7 @@ namespace dgc {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWorkgroups = 2048;  // that fill the device
 
 // cos and sin of an angle given as a fraction of a turn in 64 bits.  The nearest quarter is taken off in whole numbers; what
 // is left, an eighth of a turn at most in size, goes through the first terms of the series of sin and cos, whose next ones
@@ -29,45 +30,117 @@ __device__ __forceinline__ void turn(uint64_t fraction, float& cosine, float& si
   sine = quarter & 2 ? -b : b;
 }
 
-// A thread to a pair, or to an element that is only copied.
+// 16 bytes of elements.  Loads and stores of them take any address, so that a head may begin at any element.
+typedef uint32_t Loose __attribute__((ext_vector_type(4), aligned(2)));
 template <typename T>
-__global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
-  const int which = blockIdx.y;
-  const int pairs = a.rotary_dim / 2, units = a.head_dim - pairs, heads = a.heads[which];
-  const int64_t total = (int64_t)a.rows * heads * units;
-  const T* x = static_cast<const T*>(a.x[which].data);
-  T* out = static_cast<T*>(a.out[which].data);
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
-    const int unit = (int)(i % units);
-    const int64_t rest = i / units;
-    const int head = (int)(rest % heads);
-    const int64_t row = rest / heads;
-    const T* from = x + row * a.x[which].row_stride + head * a.x[which].head_stride;
-    T* to = out + row * a.out[which].row_stride + head * a.out[which].head_stride;
-    if (unit >= pairs) {
-      to[unit + pairs] = from[unit + pairs];
+constexpr int kElements = 16 / sizeof(T);
+
+// `count` elements from `from` on, or to `to` on.
+template <typename T>
+__device__ __forceinline__ void read(float (&x)[kElements<T>], const T* from, int count) {
+  if (count == kElements<T>) {
+    const Loose words = *reinterpret_cast<const Loose*>(from);
+    const auto piece = __builtin_bit_cast(Pack<T, kElements<T>>, words);
+#pragma unroll
+    for (int i = 0; i < kElements<T>; ++i) x[i] = piece.get(i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kElements<T>; ++i) x[i] = i < count ? to_float(from[i]) : 0.0f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void write(T* to, const float (&x)[kElements<T>], int count) {
+  if (count == kElements<T>) {
+    Pack<T, kElements<T>> piece;
+    piece.set(x);
+    *reinterpret_cast<Loose*>(to) = __builtin_bit_cast(Loose, piece);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kElements<T>; ++i)
+      if (i < count) to[i] = from_float<T>(x[i]);
+  }
+}
+
+// A thread has a piece of a row's heads (half: two, a half apart), forms the angles of its pairs once and turns the piece of
+// every head of its group.  The pieces behind the turned ones are copied.
+template <typename T, bool HALF>
+__global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, int pieces, int turned, int group) {
+  constexpr int N = kElements<T>, kPairs = HALF ? N : N / 2, kAhead = 4;
+  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t row = id / pieces;
+  if (row >= a.rows) return;
+  const int piece = (int)(id - row * pieces);
+  const bool turns = piece < turned;
+  const int half = a.rotary_dim / 2;
+  const int at = turns ? piece * N : a.rotary_dim + (piece - turned) * N;
+  const int left = turns ? (HALF ? half : a.rotary_dim) - at : a.head_dim - at, count = left < N ? left : N;
+  float c[kPairs], s[kPairs];
+  if (turns) {
+    const uint64_t position = (uint64_t)a.positions[row];
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+      const int pair = HALF ? at + i : at / 2 + i;
+      uint64_t fraction = pair < half ? position * a.frequencies[pair] : 0;
+      if (a.inverse) fraction = 0 - fraction;
+      turn(fraction, c[i], s[i]);
+      c[i] *= a.magnitude;
+      s[i] *= a.magnitude;
+    }
+  }
+  int first = blockIdx.y * group, rest = group;  // heads of this workgroup, of those of all arrays behind each other
+  for (int which = 0; which < a.count && rest > 0; ++which) {
+    if (first >= a.heads[which]) {
+      first -= a.heads[which];
       continue;
     }
-    uint64_t fraction = (uint64_t)a.positions[row] * a.frequencies[unit];
-    if (a.inverse) fraction = 0 - fraction;
-    float c, s;
-    turn(fraction, c, s);
-    c *= a.magnitude;
-    s *= a.magnitude;
-    const int p = a.half ? unit : 2 * unit, q = a.half ? unit + pairs : 2 * unit + 1;
-    const float u = to_float(from[p]), v = to_float(from[q]);
-    to[p] = from_float<T>(u * c - v * s);
-    to[q] = from_float<T>(u * s + v * c);
+    const int heads = a.heads[which] - first < rest ? a.heads[which] - first : rest;
+    const int64_t step_x = a.x[which].head_stride, step_out = a.out[which].head_stride;
+    const T* x = static_cast<const T*>(a.x[which].data) + row * a.x[which].row_stride + first * step_x + at;
+    T* out = static_cast<T*>(a.out[which].data) + row * a.out[which].row_stride + first * step_out + at;
+    // a few heads are read before the first of them is written: to the compiler they might overlap
+    for (int h = 0; h < heads; h += kAhead, x += kAhead * step_x, out += kAhead * step_out) {
+      float u[kAhead][N], v[HALF ? kAhead : 1][N];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (h + j < heads) {
+          read(u[j], x + j * step_x, count);
+          if constexpr (HALF)
+            if (turns) read(v[j], x + j * step_x + half, count);
+        }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        if (h + j >= heads) break;
+        if (turns) {
+#pragma unroll
+          for (int i = 0; i < kPairs; ++i) {
+            float& p = u[j][HALF ? i : 2 * i];
+            float& q = HALF ? v[HALF ? j : 0][i] : u[j][HALF ? i : 2 * i + 1];
+            const float one = p * c[i] - q * s[i], two = p * s[i] + q * c[i];
+            p = one;
+            q = two;
+          }
+          if constexpr (HALF) write(out + j * step_out + half, v[j], count);
+        }
+        write(out + j * step_out, u[j], count);
+      }
+    }
+    rest -= heads;
+    first = 0;
   }
 }
 
 template <typename T>
 hipError_t launch(const RotaryArgs& a, hipStream_t stream) {
-  int64_t most = 0;
-  for (int i = 0; i < a.count; ++i) most = std::max<int64_t>(most, a.heads[i]);
-  const int64_t groups = ((int64_t)a.rows * most * (a.head_dim - a.rotary_dim / 2) + kThreads - 1) / kThreads;
-  const dim3 grid((uint32_t)std::min<int64_t>(groups, 1 << 20), (uint32_t)a.count);
-  rotary_kernel<T><<<grid, kThreads, 0, stream>>>(a);
+  constexpr int N = kElements<T>;
+  const int turned = ((a.half ? a.rotary_dim / 2 : a.rotary_dim) + N - 1) / N, pieces = turned + (a.head_dim - a.rotary_dim + N - 1) / N;
+  int heads = 0;
+  for (int i = 0; i < a.count; ++i) heads += a.heads[i];
+  const int64_t groups = ((int64_t)a.rows * pieces + kThreads - 1) / kThreads;
+  // all heads to a thread where the rows alone fill the device, fewer where they do not
+  const int parts = (int)std::min<int64_t>(std::max<int64_t>(1, kWorkgroups / groups), heads), group = (heads + parts - 1) / parts;
+  const dim3 grid((uint32_t)groups, (uint32_t)((heads + group - 1) / group));
+  if (a.half) rotary_kernel<T, true><<<grid, kThreads, 0, stream>>>(a, pieces, turned, group);
+  else rotary_kernel<T, false><<<grid, kThreads, 0, stream>>>(a, pieces, turned, group);
   return hipGetLastError();
 }
 
