@@ -8,10 +8,16 @@
 // passes the type's end, and the last one is rounded: two parts leave 2^-15 of a value out, three 2^-23.  A result in 16 bits,
 // which is rounded to 2^-9 or 2^-12 at the end, is formed from two, one in 32 bits and every state from three.
 
+#include <type_traits>
+
 #include "dgc_layers.h"
 
 namespace dgc {
 namespace {
+
+struct Walks {  // of one launch, a row of the grid each
+  WalkArgs walk[kWalksMax];
+};
 
 // ---- steps -------------------------------------------------------------------------------------
 constexpr int kColumns = 32;  // columns of the state to a workgroup, four to a thread
@@ -23,11 +29,13 @@ constexpr int kRows = DGC_HEAD_MAX / kRowThreads;  // to a thread, kRowThreads a
 // kRows of its rows in registers; o is summed over the eight rows of a wavefront by exchanges, over the wavefronts in LDS, in
 // their order.  Everything that a step reads is asked for at once.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void walk_steps_kernel(const WalkArgs w) {
+__global__ __launch_bounds__(kThreads) void walk_steps_kernel(const Walks walks) {
+  const WalkArgs& w = walks.walk[blockIdx.y];
   __shared__ float4 sums[2][kThreads / 64][kColumns / 4];
   const int tiles = (w.dc + kColumns - 1) / kColumns;
   const int tile = (int)(blockIdx.x % tiles), head = (int)(blockIdx.x / tiles % w.heads);
   const int64_t sequence = blockIdx.x / tiles / w.heads;
+  if (sequence >= w.sequences) return;  // of several walks the one with the most tiles is the grid's
   const int64_t lo = w.row_offsets ? w.row_offsets[sequence] : sequence * w.max_length;
   const int64_t hi = w.row_offsets ? w.row_offsets[sequence + 1] : lo + w.max_length;
   const SequenceRows rows(lo, hi, w.rows, w.max_length);
@@ -212,38 +220,52 @@ struct Pieces {
   static constexpr int kCount = kChunk * DIM / 8 / THREADS;
   static_assert(kCount * THREADS * 8 == kChunk * DIM, "whole pieces");
   alignas(16) T held[kCount][8];
+  uint32_t offset[kCount];  // bytes from the chunk's row with the lowest address
 
-  // Rows [skipped, kChunk) of the chunk, of which row `skipped` is at base + skipped * stride; `dim` elements of each; zeros
-  // elsewhere.  A piece that the row ends
-  // in is loaded as the row's last eight elements; store() moves them down, so that nothing waits for the load here.
-  __device__ __forceinline__ void load(const T* base, int64_t stride, int skipped, int dim) {
+  static __device__ __forceinline__ int row(int i) { return (i * THREADS + (int)threadIdx.x) / (DIM / 8); }
+  static __device__ __forceinline__ int column(int i) { return (i * THREADS + (int)threadIdx.x) % (DIM / 8) * 8; }
+
+  // Elements from `first` on, `dim` of them to the end, of rows that are `stride` elements apart.  Every piece is loaded, one
+  // that is not there from a place that is, and what is wrong with it is put right when it is stored: were loads masked, or
+  // two ways of loading in one kernel, the registers they leave would be waited for here.  A piece that the row ends in is
+  // loaded as the row's last eight elements, which may begin in front of `first`, but not of the row.
+  __device__ __forceinline__ void start(int64_t stride, int first, int dim, bool reverse, int skipped) {
 #pragma unroll
     for (int i = 0; i < kCount; ++i) {
-      const int piece = i * THREADS + (int)threadIdx.x, row = piece / (DIM / 8), column = piece % (DIM / 8) * 8;
-      const bool there = row >= skipped && column < dim;
-      Loose* to = reinterpret_cast<Loose*>(held[i]);
-      if constexpr (!NARROW) {
-        const T* from = base + row * stride + (column + 8 <= dim ? column : dim - 8);
+      const int there = row(i) < skipped ? skipped : row(i);
+      const int at = first + (NARROW ? (column(i) < dim ? column(i) : 0) : column(i) + 8 <= dim ? column(i) : dim - 8);
+      offset[i] = ((uint32_t)(reverse ? kChunk - 1 - there : there) * (uint32_t)stride + (uint32_t)at) * (uint32_t)sizeof(T);
+    }
+  }
+  // The chunk whose row with the lowest address is at `lowest`.
+  __device__ __forceinline__ void load(const T* lowest, int dim) {
 #pragma unroll
-        for (int w = 0; w < (int)sizeof(T) / 2; ++w) to[w] = there ? reinterpret_cast<const Loose*>(from)[w] : Loose{0, 0, 0, 0};
+    for (int i = 0; i < kCount; ++i) {
+      const char* from = reinterpret_cast<const char*>(lowest) + offset[i];
+      if constexpr (!NARROW) {
+#pragma unroll
+        for (int w = 0; w < (int)sizeof(T) / 2; ++w) reinterpret_cast<Loose*>(held[i])[w] = reinterpret_cast<const Loose*>(from)[w];
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) held[i][j] = there && column + j < dim ? base[row * stride + column + j] : (T)0.0f;
+        for (int j = 0; j < 8; ++j) held[i][j] = column(i) + j < dim ? reinterpret_cast<const T*>(from)[j] : (T)0.0f;
       }
     }
   }
+  // Zeros for rows in front of `skipped` and elements behind the row's end.
   template <typename Store>
-  __device__ __forceinline__ void store(int dim, Store put) {
-    const int missing = NARROW ? 0 : -dim & 7;  // of the last piece
+  __device__ __forceinline__ void store(int dim, int skipped, Store put) {
+    const bool right = dim >= DIM && skipped == 0;  // nothing is wrong
 #pragma unroll
     for (int i = 0; i < kCount; ++i) {
-      const int piece = i * THREADS + (int)threadIdx.x, row = piece / (DIM / 8), column = piece % (DIM / 8) * 8;
-      if (missing) {
-        const int down = column < dim && column + 8 > dim ? missing : 0;
+      if (!right) {
+        const int left = row(i) < skipped ? 0 : dim - column(i);
+        const int down = !NARROW && left > 0 && left < 8 ? 8 - left : 0;
 #pragma unroll
         for (int by = 4; by > 0; by /= 2)
 #pragma unroll
           for (int j = 0; j < 8; ++j) held[i][j] = down & by ? (j + by < 8 ? held[i][(j + by) & 7] : (T)0.0f) : held[i][j];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) held[i][j] = left > 0 ? held[i][j] : (T)0.0f;
       }
       Eight parts[kPartsOf<T>];
       if constexpr (__is_same(T, __bf16)) {
@@ -255,7 +277,7 @@ struct Pieces {
         take_apart(x, parts);
       }
 #pragma unroll
-      for (int p = 0; p < kPartsOf<T>; ++p) put(p, row, piece % (DIM / 8), parts[p]);
+      for (int p = 0; p < kPartsOf<T>; ++p) put(p, row(i), column(i) / 8, parts[p]);
     }
   }
 };
@@ -315,7 +337,6 @@ struct Segment {
 
 struct Slots {
   int64_t count, steps;  // steps of a segment, a multiple of kChunk; 0: sequences are not cut
-  float* states;         // [slot][head][...] as w.first; may be null
 };
 
 // A workgroup walks a segment of a sequence for one head and WAVES * 32 columns of c, a wavefront with 32 columns of the state
@@ -324,7 +345,8 @@ struct Slots {
 // Of a chunk every wavefront forms a b^T for itself, as 32 x 32 shares whose layout is that of the operand they are next, and
 // so is the state's: neither goes through LDS.  While a chunk is worked on the next one's rows are on their way to registers.
 template <typename T, int DA, int WAVES, bool OUT, bool NARROW>
-__global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) void walk_chunks_kernel(const WalkArgs w, const Slots slots) {
+__global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) void walk_chunks_kernel(const Walks walks, const Slots slots) {
+  const WalkArgs& w = walks.walk[blockIdx.y];
   constexpr int kThreads = 64 * WAVES, kInput = kPartsOf<T>, kMiddle = kMiddleParts<T>, kBlocks = DA / 32, DC = 32 * WAVES;
   constexpr int kWeight = __is_same(T, __bf16) ? 2 : 3, kWeightIn = 3;
   using R = Rows<DA>;
@@ -335,13 +357,14 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane >> 5;
   const int tiles = (w.dc + DC - 1) / DC;
   const int tile = (int)(blockIdx.x % tiles), head = (int)(blockIdx.x / tiles % w.heads);
+  if (blockIdx.x / tiles / w.heads >= slots.count) return;  // of several walks the one with the most tiles is the grid's
   const Segment seg(w, blockIdx.x / tiles / w.heads, slots.steps);
   if (seg.length < 0 || (!OUT && seg.last)) return;
   const int column0 = tile * DC, column = column0 + 32 * wave + (lane & 31);
   const Decay d{w.log_decay[head] * 1.44269504f};
 
   Block state[kBlocks];
-  const float* from = OUT && slots.steps > 0 && !seg.first ? slots.states + (seg.slot * w.heads + head) * w.da * w.dc : OUT && w.first ? w.first + (seg.sequence * w.heads + head) * w.da * w.dc : nullptr;
+  const float* from = OUT && slots.steps > 0 && !seg.first ? w.states + (seg.slot * w.heads + head) * w.da * w.dc : OUT && w.first ? w.first + (seg.sequence * w.heads + head) * w.da * w.dc : nullptr;
   if (from) from += (int64_t)(4 * h) * w.state_a + (int64_t)column * w.state_c;
 #pragma unroll
   for (int i = 0; i < kBlocks; ++i)
@@ -354,10 +377,10 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
       }
 
   const int64_t sign = w.reverse ? -1 : 1;
-  const int64_t step_a = sign * w.a.row_stride, step_b = sign * w.b.row_stride, step_c = sign * w.c.row_stride;
-  const T* a = OUT ? static_cast<const T*>(w.a.data) + head * w.a.head_stride + seg.row * w.a.row_stride : nullptr;
-  const T* b = static_cast<const T*>(w.b.data) + head * w.b.head_stride + seg.row * w.b.row_stride;
-  const T* c = static_cast<const T*>(w.c.data) + head * w.c.head_stride + seg.row * w.c.row_stride + column0;
+  const T* a = OUT ? static_cast<const T*>(w.a.data) + head * w.a.head_stride : nullptr;
+  const T* b = static_cast<const T*>(w.b.data) + head * w.b.head_stride;
+  const T* c = static_cast<const T*>(w.c.data) + head * w.c.head_stride;
+
   // Weights.  Of a share of step j in step i = lane % 32: d^(i - j), from LDS at j - i + 31, zeros behind 31.  Of a step j that
   // goes into the state: d^(31 - j); of the lane's eight, j = 16 k + 4 h + {0 .. 3, 8 .. 11}, a power of its own for either k,
   // times one that all lanes have.  A segment's first chunk is the short one, if one is, and takes the window's end.
@@ -369,23 +392,37 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
   for (int e = 0; e < 8; ++e) uniform[e] = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, d.power(e < 4 ? 11 - e : 7 - e) * w.scale)));
   const float into_weight[2] = {d.power(20 - 4 * h + w.late), d.power(4 - 4 * h + w.late)};
   const int short_by = (int)(-seg.length & (kChunk - 1));
-  float query_weight = d.power((lane & 31) - short_by + 1 - w.late), kept = d.power(kChunk - short_by);
+  // The state in registers is the state without the decay of the last `since` steps, `factor`: to multiply all of it once a
+  // chunk would be a tenth of the arithmetic.  Decays that leave less than 2^-20 are caught up with.
+  float query_weight = d.power((lane & 31) - short_by + 1 - w.late), factor = 1.0f;
+  int since = 0;
 
   Pieces<T, DA, kThreads, NARROW> next_a, next_b;
   Pieces<T, DC, kThreads, NARROW> next_c;
-  auto load = [&](int64_t at) {
-    const int skipped = at < 0 ? (int)-at : 0;
-    if constexpr (OUT) next_a.load(a + at * step_a, step_a, skipped, w.da);
-    next_b.load(b + at * step_b, step_b, skipped, w.da);
-    next_c.load(c + at * step_c, step_c, skipped, w.dc - column0);
+  const int64_t stride_a = w.a.row_stride, stride_b = w.b.row_stride, stride_c = w.c.row_stride;
+  const bool reverse = w.reverse;
+  const int da = w.da, dc = w.dc - column0;
+  auto start = [&](int skipped) {
+    if constexpr (OUT) next_a.start(stride_a, 0, da, reverse, skipped);
+    next_b.start(stride_b, 0, da, reverse, skipped);
+    next_c.start(stride_c, column0, dc, reverse, skipped);
   };
+  auto load = [&](int64_t at) {
+    const int64_t lowest = seg.row + (reverse ? -at - (kChunk - 1) : at);
+    if constexpr (OUT) next_a.load(a + lowest * stride_a, da);
+    next_b.load(b + lowest * stride_b, da);
+    next_c.load(c + lowest * stride_c, dc);
+  };
+  start(short_by);
   if (seg.length > 0) load(-short_by);
+  start(0);
   int buffer = 0;
   for (int64_t at = -short_by; at < seg.length; at += kChunk, buffer = (buffer + 1) % kBuffers) {
+    const int skipped = at < 0 ? short_by : 0;
     if (kBuffers == 1) __syncthreads();
-    if constexpr (OUT) next_a.store(w.da, [&](int p, int row, int piece, Eight x) { R::store(lds_a[buffer] + p * R::kElements, row, piece, x); });
-    next_b.store(w.da, [&](int p, int row, int piece, Eight x) { R::store(lds_b[buffer] + p * R::kElements, row, piece, x); });
-    next_c.store(w.dc - column0, [&](int p, int row, int piece, Eight x) { Cs::store(lds_c[buffer] + p * Cs::kElements, row, piece, x); });
+    if constexpr (OUT) next_a.store(da, skipped, [&](int p, int row, int piece, Eight x) { R::store(lds_a[buffer] + p * R::kElements, row, piece, x); });
+    next_b.store(da, skipped, [&](int p, int row, int piece, Eight x) { R::store(lds_b[buffer] + p * R::kElements, row, piece, x); });
+    next_c.store(dc, skipped, [&](int p, int row, int piece, Eight x) { Cs::store(lds_c[buffer] + p * Cs::kElements, row, piece, x); });
     __syncthreads();  // of two buffers, the other one was read before the barrier of the chunk before this one
     if (at + kChunk < seg.length) load(at + kChunk);
     __builtin_amdgcn_sched_barrier(0);
@@ -422,9 +459,10 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
         multiply_parts<kWeight>(part, row_a[k % 2], out);
         __builtin_amdgcn_sched_barrier(0);
       }
+      const float query = query_weight * factor;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        out[e] *= query_weight;
+        out[e] *= query;
         shares[e] *= share_weights[behind + 8 * (e / 4) + e % 4];
       }
 #pragma unroll
@@ -458,16 +496,26 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
     }
 
     __builtin_amdgcn_sched_barrier(0);
+    const float before = factor;
+    since += at < 0 ? kChunk - short_by : kChunk;
+    factor = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, d.power(since))));
+    if (!(factor >= 0x1p-20f && factor <= 0x1p20f)) {
+#pragma unroll
+      for (int i = 0; i < kBlocks; ++i) state[i] *= d.power(at < 0 ? kChunk - short_by : kChunk) * before;
+      since = 0;
+      factor = 1.0f;
+    }
+    const float inverse = __builtin_amdgcn_rcpf(factor), into_scale[2] = {into_weight[0] * inverse, into_weight[1] * inverse};
     Eight into[2][kIntoState];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       float x[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        x[e] = 0.0f;
+        x[e] = (float)turned_c[k][kInput - 1][e];
 #pragma unroll
-        for (int p = kInput - 1; p >= 0; --p) x[e] += (float)turned_c[k][p][e];
-        x[e] *= into_weight[k] * uniform[e];
+        for (int p = kInput - 2; p >= 0; --p) x[e] += (float)turned_c[k][p][e];
+        x[e] *= into_scale[k] * uniform[e];
       }
       take_apart(x, into[k]);
     }
@@ -481,18 +529,14 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
 #pragma unroll
     for (int k = 0; k < 2 * kBlocks; ++k) {
       if (k + 1 < 2 * kBlocks) read(k + 1);
-      if (k % 2 == 0) state[k / 2] *= kept;
       multiply_parts<kWeightIn>(turned_b[k % 2], into[k % 2], state[k / 2]);
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (at < 0) {
-      query_weight = d.power((lane & 31) + 1 - w.late);
-      kept = d.power(kChunk);
-    }
+    if (at < 0) query_weight = d.power((lane & 31) + 1 - w.late);
   }
 
   float* to = OUT ? (seg.last && w.last ? w.last + (seg.sequence * w.heads + head) * w.da * w.dc : nullptr)
-                  : slots.states + ((seg.slot + 1) * w.heads + head) * w.da * w.dc;
+                  : w.states + ((seg.slot + 1) * w.heads + head) * w.da * w.dc;
   // the compiler would keep the addresses of the first loads until here
   int again = lane;
   asm volatile("" : "+v"(again));
@@ -505,12 +549,13 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
     for (int q = 0; q < 4; ++q, first += 8 * (int64_t)w.state_a)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (32 * i + 8 * q + 4 * (again >> 5) + j < w.da) first[j * w.state_a] = state[i][4 * q + j];
+        if (32 * i + 8 * q + 4 * (again >> 5) + j < w.da) first[j * w.state_a] = state[i][4 * q + j] * factor;
 }
 
 // What the segments of a sequence add, joined to the state in front of each: slot i + 1 of a sequence holds what its segment i
 // adds, and is left with the state in front of segment i + 1.  A thread to an element; a few segments' loads on their way.
-__global__ __launch_bounds__(256) void join_kernel(const WalkArgs w, const Slots slots) {
+__global__ __launch_bounds__(256) void join_kernel(const Walks walks, const Slots slots) {
+  const WalkArgs& w = walks.walk[blockIdx.y];
   constexpr int kAhead = 8;
   const int64_t size = (int64_t)w.da * w.dc, groups = (size + 255) / 256;
   const int head = (int)(blockIdx.x / groups % w.heads);
@@ -519,7 +564,7 @@ __global__ __launch_bounds__(256) void join_kernel(const WalkArgs w, const Slots
   if (element >= size) return;
   const float kept = Decay{w.log_decay[head] * 1.44269504f}.power((int)slots.steps);
   float state = w.first ? w.first[(sequence * w.heads + head) * size + element] : 0.0f;
-  float* at = slots.states + ((Segment::first_slot(w, sequence, slots.steps) + 1) * w.heads + head) * size + element;
+  float* at = w.states + ((Segment::first_slot(w, sequence, slots.steps) + 1) * w.heads + head) * size + element;
   for (int64_t i = 0; i + 1 < segments; i += kAhead) {
     float added[kAhead];
 #pragma unroll
@@ -533,40 +578,60 @@ __global__ __launch_bounds__(256) void join_kernel(const WalkArgs w, const Slots
   }
 }
 
-template <typename T, int DA, int WAVES, bool OUT, bool NARROW>
-hipError_t launch_chunks(const WalkArgs& w, const Slots& slots, hipStream_t stream) {
-  const uint32_t groups = (uint32_t)(slots.count * w.heads * ((w.dc + 32 * WAVES - 1) / (32 * WAVES)));
-  walk_chunks_kernel<T, DA, WAVES, OUT, NARROW><<<groups, 64 * WAVES, 0, stream>>>(w, slots);
-  return hipGetLastError();
-}
-
-template <typename T, int DA, bool OUT>
-hipError_t launch_chunks(const WalkArgs& w, const Slots& slots, hipStream_t stream) {
-  return w.dc <= 32 ? launch_chunks<T, DA, 1, OUT, false>(w, slots, stream)
-         : w.dc <= 64 ? launch_chunks<T, DA, 2, OUT, false>(w, slots, stream) : launch_chunks<T, DA, 4, OUT, false>(w, slots, stream);
-}
+// What the kernels of a walk are made for: rows of the state and its columns to a workgroup, OUT: as above.
+struct Made {
+  int rows, waves;
+  bool narrow;
+  explicit Made(const WalkArgs& w) : rows(w.da <= 64 ? 64 : w.da <= 128 ? 128 : 256), waves(w.dc <= 32 ? 1 : w.dc <= 64 ? 2 : 4), narrow(w.da < 8 || w.dc < 8) {
+    if (narrow) {
+      waves = 4;
+      if (rows == 128) rows = 256;
+    }
+  }
+  bool operator==(const Made& o) const { return rows == o.rows && waves == o.waves && narrow == o.narrow; }
+};
 
 template <typename T, bool OUT>
-hipError_t launch_chunks(const WalkArgs& w, const Slots& slots, hipStream_t stream) {
-  if (w.da < 8 || w.dc < 8) return w.da <= 64 ? launch_chunks<T, 64, 4, OUT, true>(w, slots, stream) : launch_chunks<T, 256, 4, OUT, true>(w, slots, stream);
-  return w.da <= 64 ? launch_chunks<T, 64, OUT>(w, slots, stream) : w.da <= 128 ? launch_chunks<T, 128, OUT>(w, slots, stream) : launch_chunks<T, 256, OUT>(w, slots, stream);
+void launch_chunks(const Walks& walks, int count, const Slots& slots, hipStream_t stream) {
+  const Made made(walks.walk[0]);
+  int32_t dc = 0;
+  for (int i = 0; i < count; ++i) dc = std::max(dc, walks.walk[i].dc);
+  const dim3 grid((uint32_t)(slots.count * walks.walk[0].heads * ((dc + 32 * made.waves - 1) / (32 * made.waves))), (uint32_t)count);
+  auto go = [&](auto rows, auto waves, auto narrow) {
+    walk_chunks_kernel<T, decltype(rows)::value, decltype(waves)::value, OUT, decltype(narrow)::value><<<grid, 64 * decltype(waves)::value, 0, stream>>>(walks, slots);
+  };
+  auto with_waves = [&](auto rows) {
+    if (made.waves == 1) go(rows, std::integral_constant<int, 1>(), std::false_type());
+    else if (made.waves == 2) go(rows, std::integral_constant<int, 2>(), std::false_type());
+    else go(rows, std::integral_constant<int, 4>(), std::false_type());
+  };
+  if (made.narrow && made.rows == 64) go(std::integral_constant<int, 64>(), std::integral_constant<int, 4>(), std::true_type());
+  else if (made.narrow) go(std::integral_constant<int, 256>(), std::integral_constant<int, 4>(), std::true_type());
+  else if (made.rows == 64) with_waves(std::integral_constant<int, 64>());
+  else if (made.rows == 128) with_waves(std::integral_constant<int, 128>());
+  else with_waves(std::integral_constant<int, 256>());
 }
 
-template <bool OUT>
-hipError_t launch_chunks(const WalkArgs& w, const Slots& slots, int32_t dtype, hipStream_t stream) {
-  switch (dtype) {
-    case DGC_F32: return launch_chunks<float, OUT>(w, slots, stream);
-    case DGC_F16: return launch_chunks<_Float16, OUT>(w, slots, stream);
-    default: return launch_chunks<__bf16, OUT>(w, slots, stream);
-  }
+template <typename T>
+void launch_steps(const Walks& walks, int count, hipStream_t stream) {
+  int64_t groups = 0;
+  for (int i = 0; i < count; ++i) groups = std::max(groups, walk_workgroups(walks.walk[i].sequences, walks.walk[i].heads, walks.walk[i].dc));
+  walk_steps_kernel<T><<<dim3((uint32_t)groups, (uint32_t)count), kThreads, 0, stream>>>(walks);
+}
+
+template <typename F>
+void with_type(int32_t dtype, F f) {
+  if (dtype == DGC_F32) f(0.0f);
+  else if (dtype == DGC_F16) f((_Float16)0.0f);
+  else f((__bf16)0.0f);
 }
 
 constexpr int64_t kStepsAtMost = 4;      // of sequences that go step by step
 constexpr int64_t kWorkgroups = 512;     // that fill the device
 constexpr int64_t kSegmentLeast = 256;
 
-Slots slots_of(int64_t rows, int64_t sequences, int64_t max_length, int32_t heads, int32_t dims, void* workspace) {
-  Slots s{sequences, 0, static_cast<float*>(workspace)};
+Slots slots_of(int64_t rows, int64_t sequences, int64_t max_length, int32_t heads, int32_t dims) {
+  Slots s{sequences, 0};
   const int64_t tiles = (dims + 127) / 128, whole = sequences * heads * tiles;
   if (max_length <= 2 * kSegmentLeast || whole >= kWorkgroups / 2) return s;
   // as many segments as fill the device, of kSegmentLeast steps at least
@@ -577,6 +642,25 @@ Slots slots_of(int64_t rows, int64_t sequences, int64_t max_length, int32_t head
   return s;
 }
 
+Slots slots_of(const WalkArgs& w) { return slots_of(w.rows, w.sequences, w.max_length, w.heads, std::max(w.da, w.dc)); }
+
+// Calls f(walks, count) for the walks that one kernel can take together.
+template <typename F>
+void together(const WalkArgs* w, int count, F f) {
+  bool done[kWalksMax] = {};
+  for (int i = 0; i < count; ++i) {
+    if (done[i]) continue;
+    Walks walks{};
+    int n = 0;
+    for (int j = i; j < count; ++j)
+      if (!done[j] && Made(w[j]) == Made(w[i])) {
+        walks.walk[n++] = w[j];
+        done[j] = true;
+      }
+    f(walks, n);
+  }
+}
+
 }  // namespace
 
 int64_t walk_workgroups(int64_t sequences, int32_t heads, int32_t dc) {
@@ -584,27 +668,30 @@ int64_t walk_workgroups(int64_t sequences, int32_t heads, int32_t dc) {
 }
 
 size_t walk_workspace_bytes(int64_t rows, int64_t sequences, int64_t max_length, int32_t heads, int32_t da, int32_t dc) {
-  const Slots s = slots_of(rows, sequences, max_length, heads, std::max(da, dc), nullptr);
+  const Slots s = slots_of(rows, sequences, max_length, heads, std::max(da, dc));
   return s.steps == 0 ? 0 : ((size_t)(s.count + 1) * heads * da * dc * 4 + 255) / 256 * 256;
 }
 
-hipError_t launch_walk_states(const WalkArgs& w, void* workspace, int32_t dtype, hipStream_t stream) {
-  const Slots slots = slots_of(w.rows, w.sequences, w.max_length, w.heads, std::max(w.da, w.dc), workspace);
+hipError_t launch_walk_states(const WalkArgs* w, int count, int32_t dtype, hipStream_t stream) {
+  const Slots slots = slots_of(w[0]);
   if (slots.steps == 0) return hipSuccess;
-  const hipError_t err = launch_chunks<false>(w, slots, dtype, stream);
-  if (err != hipSuccess) return err;
-  const int64_t groups = ((int64_t)w.da * w.dc + 255) / 256;
-  join_kernel<<<(uint32_t)(w.sequences * w.heads * groups), 256, 0, stream>>>(w, slots);
+  together(w, count, [&](const Walks& walks, int n) {
+    with_type(dtype, [&](auto t) { launch_chunks<decltype(t), false>(walks, n, slots, stream); });
+    const int64_t groups = ((int64_t)w[0].da * w[0].dc + 255) / 256;
+    join_kernel<<<dim3((uint32_t)(w[0].sequences * w[0].heads * groups), (uint32_t)n), 256, 0, stream>>>(walks, slots);
+  });
   return hipGetLastError();
 }
 
-hipError_t launch_walk(const WalkArgs& w, void* workspace, int32_t dtype, hipStream_t stream) {
-  if (w.max_length > kStepsAtMost) return launch_chunks<true>(w, slots_of(w.rows, w.sequences, w.max_length, w.heads, std::max(w.da, w.dc), workspace), dtype, stream);
-  const uint32_t groups = (uint32_t)walk_workgroups(w.sequences, w.heads, w.dc);
-  switch (dtype) {
-    case DGC_F32: walk_steps_kernel<float><<<groups, kThreads, 0, stream>>>(w); break;
-    case DGC_F16: walk_steps_kernel<_Float16><<<groups, kThreads, 0, stream>>>(w); break;
-    default: walk_steps_kernel<__bf16><<<groups, kThreads, 0, stream>>>(w); break;
+hipError_t launch_walks(const WalkArgs* w, int count, int32_t dtype, hipStream_t stream) {
+  if (w[0].max_length > kStepsAtMost) {
+    together(w, count, [&](const Walks& walks, int n) {
+      with_type(dtype, [&](auto t) { launch_chunks<decltype(t), true>(walks, n, slots_of(w[0]), stream); });
+    });
+  } else {
+    Walks walks{};
+    for (int i = 0; i < count; ++i) walks.walk[i] = w[i];
+    with_type(dtype, [&](auto t) { launch_steps<decltype(t)>(walks, count, stream); });
   }
   return hipGetLastError();
 }

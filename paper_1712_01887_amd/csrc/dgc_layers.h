@@ -33,6 +33,7 @@ struct WalkArgs {
   int64_t rows, sequences, max_length;
   const int64_t* row_offsets;  // may be null
   float scale, out_scale;
+  float* states;  // workspace of the walk, where sequences are cut: as many states as they have segments
   int32_t late;  // 1: the state comes in and leaves with the decay of the step between done
   bool reverse;
 };
@@ -53,10 +54,12 @@ struct VocabArgs {
 };
 
 hipError_t launch_rotary(const RotaryArgs& a, int32_t dtype, hipStream_t stream);
-// Where sequences are cut: the states in front of their segments (of b and c alone), which launch_walk reads from the
-// workspace, as they lie with the walk's state_a and state_c.
-hipError_t launch_walk_states(const WalkArgs& a, void* workspace, int32_t dtype, hipStream_t stream);
-hipError_t launch_walk(const WalkArgs& a, void* workspace, int32_t dtype, hipStream_t stream);
+constexpr int kWalksMax = 3;
+// Up to kWalksMax walks of the same sequences, of which none needs what another one leaves; da and dc may be exchanged.
+// Where sequences are cut, launch_walk_states forms the states in front of their segments (of b and c alone), which
+// launch_walks reads, from `states`, as they lie with a walk's own state_a and state_c.
+hipError_t launch_walk_states(const WalkArgs* w, int count, int32_t dtype, hipStream_t stream);
+hipError_t launch_walks(const WalkArgs* w, int count, int32_t dtype, hipStream_t stream);
 size_t walk_workspace_bytes(int64_t rows, int64_t sequences, int64_t max_length, int32_t heads, int32_t da, int32_t dc);
 int64_t walk_workgroups(int64_t sequences, int32_t heads, int32_t dc);
 hipError_t launch_vocab_forward(const VocabArgs& a, void* workspace, int32_t dtype, hipStream_t stream);

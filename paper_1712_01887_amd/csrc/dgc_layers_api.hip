@@ -33,6 +33,12 @@ dgc_status check_heads(const dgc_heads* x, int64_t rows, int64_t heads, int64_t 
   return aligned_to(x->data, element) ? DGC_OK : DGC_ERR_ALIGNMENT;
 }
 
+// Of an attention array also: the rows of a chunk have offsets of 32 bits.
+dgc_status check_rows_of_heads(const dgc_heads* x, int64_t rows, int64_t heads, int64_t dim, size_t element, bool written) {
+  if (x && x->row_stride >= kWidthLimit) return DGC_ERR_CAPACITY;
+  return check_heads(x, rows, heads, dim, element, written);
+}
+
 dgc_status check_workspace(const void* workspace, size_t have, size_t need) {
   if (need == 0) return DGC_OK;
   if (!workspace) return DGC_ERR_INVALID_ARG;
@@ -148,7 +154,7 @@ dgc_status dgc_linear_attention_workspace_bytes(const dgc_attention* shape, int3
   const dgc_status st = check_attention(shape);
   if (st != DGC_OK) return st;
   if (!bytes || (backward != 0 && backward != 1)) return DGC_ERR_INVALID_ARG;
-  *bytes = walk_workspace_bytes(shape->rows, shape->sequences, shape->max_length, shape->heads, shape->key_dim, shape->value_dim);
+  *bytes = walk_workspace_bytes(shape->rows, shape->sequences, shape->max_length, shape->heads, shape->key_dim, shape->value_dim) * (backward ? 2 : 1);
   return DGC_OK;
 }
 
@@ -159,9 +165,9 @@ dgc_status dgc_linear_attention_forward(const dgc_attention* s, const dgc_heads*
   if (st != DGC_OK) return st;
   const size_t e = element_bytes(s->dtype);
   for (const dgc_heads* x : {q, k})
-    if ((st = check_heads(x, s->rows, s->heads, s->key_dim, e, false)) != DGC_OK) return st;
-  if ((st = check_heads(v, s->rows, s->heads, s->value_dim, e, false)) != DGC_OK) return st;
-  if ((st = check_heads(o, s->rows, s->heads, s->value_dim, e, true)) != DGC_OK) return st;
+    if ((st = check_rows_of_heads(x, s->rows, s->heads, s->key_dim, e, false)) != DGC_OK) return st;
+  if ((st = check_rows_of_heads(v, s->rows, s->heads, s->value_dim, e, false)) != DGC_OK) return st;
+  if ((st = check_rows_of_heads(o, s->rows, s->heads, s->value_dim, e, true)) != DGC_OK) return st;
   if (!log_decay) return DGC_ERR_INVALID_ARG;
   if (s->rows > 0)
     for (const dgc_heads* x : {q, k, v})
@@ -190,9 +196,10 @@ dgc_status dgc_linear_attention_forward(const dgc_attention* s, const dgc_heads*
   w.row_offsets = s->row_offsets;
   w.scale = 1.0f;
   w.out_scale = s->scale;
+  w.states = static_cast<float*>(workspace);
   const hipStream_t stream = static_cast<hipStream_t>(stream_);
-  hipError_t err = launch_walk_states(w, workspace, s->dtype, stream);
-  if (err == hipSuccess) err = launch_walk(w, workspace, s->dtype, stream);
+  hipError_t err = launch_walk_states(&w, 1, s->dtype, stream);
+  if (err == hipSuccess) err = launch_walks(&w, 1, s->dtype, stream);
   return hip_ok(err, "launch attention kernels") ? DGC_OK : DGC_ERR_HIP;
 }
 
@@ -204,12 +211,12 @@ dgc_status dgc_linear_attention_backward(const dgc_attention* s, const dgc_heads
   if (st != DGC_OK) return st;
   const size_t e = element_bytes(s->dtype);
   for (const dgc_heads* x : {q, k})
-    if ((st = check_heads(x, s->rows, s->heads, s->key_dim, e, false)) != DGC_OK) return st;
+    if ((st = check_rows_of_heads(x, s->rows, s->heads, s->key_dim, e, false)) != DGC_OK) return st;
   for (const dgc_heads* x : {v, d_o})
-    if ((st = check_heads(x, s->rows, s->heads, s->value_dim, e, false)) != DGC_OK) return st;
+    if ((st = check_rows_of_heads(x, s->rows, s->heads, s->value_dim, e, false)) != DGC_OK) return st;
   for (const dgc_heads* x : {dq, dk})
-    if ((st = check_heads(x, s->rows, s->heads, s->key_dim, e, true)) != DGC_OK) return st;
-  if ((st = check_heads(dv, s->rows, s->heads, s->value_dim, e, true)) != DGC_OK) return st;
+    if ((st = check_rows_of_heads(x, s->rows, s->heads, s->key_dim, e, true)) != DGC_OK) return st;
+  if ((st = check_rows_of_heads(dv, s->rows, s->heads, s->value_dim, e, true)) != DGC_OK) return st;
   if (!log_decay) return DGC_ERR_INVALID_ARG;
   if (s->rows > 0) {
     for (const dgc_heads* x : {q, k, v, d_o})
@@ -223,69 +230,61 @@ dgc_status dgc_linear_attention_backward(const dgc_attention* s, const dgc_heads
   if ((st = check_workspace(workspace, workspace_bytes, need)) != DGC_OK) return st;
   if (s->sequences == 0) return DGC_OK;
   const hipStream_t stream = static_cast<hipStream_t>(stream_);
-  WalkArgs w{};
-  w.log_decay = log_decay;
-  w.heads = s->heads;
-  w.rows = s->rows;
-  w.sequences = s->sequences;
-  w.max_length = s->max_length;
-  w.row_offsets = s->row_offsets;
-  // The states as in the forward call, then dq: the forward walk with do in q's place, and k and v changed round, and so
-  // the state's rows and columns.
-  w.b = *k;
-  w.c = *v;
-  w.first = state0;
-  w.state_a = s->value_dim;
-  w.state_c = 1;
-  w.da = s->key_dim;
-  w.dc = s->value_dim;
-  w.scale = 1.0f;
-  hipError_t err = launch_walk_states(w, workspace, s->dtype, stream);
-  w.a = *d_o;
-  w.b = *v;
-  w.c = *k;
-  w.out = *dq;
-  w.first = state0;
-  w.state_a = 1;
-  w.state_c = s->value_dim;
-  w.da = s->value_dim;
-  w.dc = s->key_dim;
-  w.scale = 1.0f;
-  w.out_scale = s->scale;
-  if (err == hipSuccess) err = launch_walk(w, workspace, s->dtype, stream);
-  // dk and dv: from the last step to the first, with the state's gradient for a state.  It is read by both before the
-  // second one, which alone writes it, leaves it behind.
-  w.reverse = true;
-  w.late = 1;
-  w.scale = s->scale;
-  w.out_scale = 1.0f;
-  w.first = dstate_last;
-  w.b = *q;
-  w.c = *d_o;
-  w.state_a = s->value_dim;
-  w.state_c = 1;
-  w.da = s->key_dim;
-  w.dc = s->value_dim;
-  if (err == hipSuccess) err = launch_walk_states(w, workspace, s->dtype, stream);
-  w.state_a = 1;
-  w.state_c = s->value_dim;
-  w.da = s->value_dim;
-  w.dc = s->key_dim;
-  w.a = *v;
-  w.b = *d_o;
-  w.c = *q;
-  w.out = *dk;
-  if (err == hipSuccess) err = launch_walk(w, workspace, s->dtype, stream);
-  w.a = *k;
-  w.b = *q;
-  w.c = *d_o;
-  w.out = *dv;
-  w.last = dstate0;
-  w.state_a = s->value_dim;
-  w.state_c = 1;
-  w.da = s->key_dim;
-  w.dc = s->value_dim;
-  if (err == hipSuccess) err = launch_walk(w, workspace, s->dtype, stream);
+  WalkArgs forward{};  // with k and v: the states as in the forward call
+  forward.b = *k;
+  forward.c = *v;
+  forward.log_decay = log_decay;
+  forward.first = state0;
+  forward.states = static_cast<float*>(workspace);
+  forward.state_a = s->value_dim;
+  forward.state_c = 1;
+  forward.heads = s->heads;
+  forward.da = s->key_dim;
+  forward.dc = s->value_dim;
+  forward.rows = s->rows;
+  forward.sequences = s->sequences;
+  forward.max_length = s->max_length;
+  forward.row_offsets = s->row_offsets;
+  forward.scale = 1.0f;
+  WalkArgs w[3] = {forward, forward, forward};
+  WalkArgs &walk_dq = w[0], &walk_dk = w[1], &walk_dv = w[2];
+  // dv: from the last step to the first, with the state's gradient for a state
+  walk_dv.a = *k;
+  walk_dv.b = *q;
+  walk_dv.c = *d_o;
+  walk_dv.out = *dv;
+  walk_dv.first = dstate_last;
+  walk_dv.last = dstate0;
+  walk_dv.states = forward.states + need / 2 / sizeof(float);
+  walk_dv.scale = s->scale;
+  walk_dv.out_scale = 1.0f;
+  walk_dv.late = 1;
+  walk_dv.reverse = true;
+  // dk: the same with v for k, and q and do changed round, and so the state's rows and columns
+  walk_dk = walk_dv;
+  walk_dk.a = *v;
+  walk_dk.b = *d_o;
+  walk_dk.c = *q;
+  walk_dk.out = *dk;
+  walk_dk.last = nullptr;
+  // dq: the forward walk with do for q, and k and v changed round
+  walk_dq.a = *d_o;
+  walk_dq.b = *v;
+  walk_dq.c = *k;
+  walk_dq.out = *dq;
+  walk_dq.out_scale = s->scale;
+  for (WalkArgs* x : {&walk_dq, &walk_dk}) {
+    x->state_a = 1;
+    x->state_c = s->value_dim;
+    x->da = s->value_dim;
+    x->dc = s->key_dim;
+  }
+  const WalkArgs states[2] = {forward, walk_dv};
+  hipError_t err = launch_walk_states(states, 2, s->dtype, stream);
+  // dk reads dstate_last; dv may leave dstate0 in its place
+  const bool in_place = dstate0 && dstate0 == dstate_last;
+  if (err == hipSuccess) err = launch_walks(w, in_place ? 2 : 3, s->dtype, stream);
+  if (err == hipSuccess && in_place) err = launch_walks(&walk_dv, 1, s->dtype, stream);
   return hip_ok(err, "launch attention kernels") ? DGC_OK : DGC_ERR_HIP;
 }
 

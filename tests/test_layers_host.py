@@ -123,7 +123,7 @@ def test_attention_refusals(dgc_lib):
         s = attention_shape()
         for kw, status in ((dict(q=None), BAD), (dict(k=heads(None)), BAD), (dict(v=heads(P + 2)), ODD), (dict(decay=None), BAD),
                            (dict(decay=P + 1), ODD), (dict(state0=P + 2), ODD), (dict(q=heads(row=-8)), BAD),
-                           (dict(k=heads(head=1 << 60)), BIG)):
+                           (dict(k=heads(head=1 << 60)), BIG), (dict(v=heads(row=1 << 24)), BIG)):
             assert call(dgc_lib, s, **kw) == status, kw
     for name in ("o",):
         for x, status in ((None, BAD), (heads(None), BAD), (heads(row=56), BAD), (heads(head=0), BAD), (heads(P), BAD),
