@@ -10,14 +10,25 @@
 
 #include <type_traits>
 
+#include "dgc_device.h"
 #include "dgc_layers.h"
 
 namespace dgc {
 namespace {
 
-struct Walks {  // of one launch, a row of the grid each
+struct Walks {  // of one launch
   WalkArgs walk[kWalksMax];
+  int32_t count;
 };
+
+// Which walk a workgroup takes part in, and as which of a walk's workgroups.  Those of several walks that read the same rows
+// stand side by side, on one die (workgroups go to the eight dies in turn), so that one's rows are in its cache for the others.
+__device__ __forceinline__ int64_t place(const Walks& walks, int& walk) {
+  const uint32_t round = 8 * (uint32_t)walks.count, in = blockIdx.x % round;
+  walk = (int)(in / 8);
+  return (int64_t)(blockIdx.x / round) * 8 + in % 8;
+}
+inline uint32_t places(int64_t groups, int count) { return (uint32_t)((groups + 7) / 8 * 8 * count); }
 
 // ---- steps -------------------------------------------------------------------------------------
 constexpr int kColumns = 32;  // columns of the state to a workgroup, four to a thread
@@ -30,12 +41,14 @@ constexpr int kRows = DGC_HEAD_MAX / kRowThreads;  // to a thread, kRowThreads a
 // their order.  Everything that a step reads is asked for at once.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void walk_steps_kernel(const Walks walks) {
-  const WalkArgs& w = walks.walk[blockIdx.y];
+  int which;
+  const int64_t group = place(walks, which);
+  const WalkArgs& w = walks.walk[which];
   __shared__ float4 sums[2][kThreads / 64][kColumns / 4];
   const int tiles = (w.dc + kColumns - 1) / kColumns;
-  const int tile = (int)(blockIdx.x % tiles), head = (int)(blockIdx.x / tiles % w.heads);
-  const int64_t sequence = blockIdx.x / tiles / w.heads;
-  if (sequence >= w.sequences) return;  // of several walks the one with the most tiles is the grid's
+  const int tile = (int)(group % tiles), head = (int)(group / tiles % w.heads);
+  const int64_t sequence = group / tiles / w.heads;
+  if (sequence >= w.sequences) return;  // whole rounds of the dies, and the walk with the most tiles
   const int64_t lo = w.row_offsets ? w.row_offsets[sequence] : sequence * w.max_length;
   const int64_t hi = w.row_offsets ? w.row_offsets[sequence + 1] : lo + w.max_length;
   const SequenceRows rows(lo, hi, w.rows, w.max_length);
@@ -346,7 +359,9 @@ struct Slots {
 // so is the state's: neither goes through LDS.  While a chunk is worked on the next one's rows are on their way to registers.
 template <typename T, int DA, int WAVES, bool OUT, bool NARROW>
 __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) void walk_chunks_kernel(const Walks walks, const Slots slots) {
-  const WalkArgs& w = walks.walk[blockIdx.y];
+  int which;
+  const int64_t group = place(walks, which);
+  const WalkArgs& w = walks.walk[which];
   constexpr int kThreads = 64 * WAVES, kInput = kPartsOf<T>, kMiddle = kMiddleParts<T>, kBlocks = DA / 32, DC = 32 * WAVES;
   constexpr int kWeight = __is_same(T, __bf16) ? 2 : 3, kWeightIn = 3;
   using R = Rows<DA>;
@@ -354,11 +369,13 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
   // two buffers where they leave room for a second workgroup, or fit at all
   constexpr int kBuffers = kInput * (2 * R::kElements + Cs::kElements) * 2 <= 40960 ? 2 : 1;
   __shared__ __align__(16) __bf16 lds_a[kBuffers][OUT ? kInput * R::kElements : 8], lds_b[kBuffers][kInput * R::kElements], lds_c[kBuffers][kInput * Cs::kElements];
+  constexpr int kPitch = 40;
+  __shared__ __align__(16) T staged[OUT && sizeof(T) == 2 ? WAVES : 1][OUT && sizeof(T) == 2 ? kChunk * kPitch : 8];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane >> 5;
   const int tiles = (w.dc + DC - 1) / DC;
-  const int tile = (int)(blockIdx.x % tiles), head = (int)(blockIdx.x / tiles % w.heads);
-  if (blockIdx.x / tiles / w.heads >= slots.count) return;  // of several walks the one with the most tiles is the grid's
-  const Segment seg(w, blockIdx.x / tiles / w.heads, slots.steps);
+  const int tile = (int)(group % tiles), head = (int)(group / tiles % w.heads);
+  if (group / tiles / w.heads >= slots.count) return;  // whole rounds of the dies, and the walk with the most tiles
+  const Segment seg(w, group / tiles / w.heads, slots.steps);
   if (seg.length < 0 || (!OUT && seg.last)) return;
   const int column0 = tile * DC, column = column0 + 32 * wave + (lane & 31);
   const Decay d{w.log_decay[head] * 1.44269504f};
@@ -380,6 +397,9 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
   const T* a = OUT ? static_cast<const T*>(w.a.data) + head * w.a.head_stride : nullptr;
   const T* b = static_cast<const T*>(w.b.data) + head * w.b.head_stride;
   const T* c = static_cast<const T*>(w.c.data) + head * w.c.head_stride;
+
+  const int64_t step_out = sign * w.out.row_stride;
+  T* out_rows = OUT ? static_cast<T*>(w.out.data) + head * w.out.head_stride + seg.row * w.out.row_stride + column0 + 32 * wave : nullptr;
 
   // Weights.  Of a share of step j in step i = lane % 32: d^(i - j), from LDS at j - i + 31, zeros behind 31.  Of a step j that
   // goes into the state: d^(31 - j); of the lane's eight, j = 16 k + 4 h + {0 .. 3, 8 .. 11}, a power of its own for either k,
@@ -446,17 +466,34 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
           row_b[k % 2][p] = R::along(lds_b[buffer] + p * R::kElements, k, lane);
         }
       };
-      read(0);
-#pragma unroll
-      for (int k = 0; k < 2 * kBlocks; ++k) {
-        if (k + 1 < 2 * kBlocks) read(k + 1);
-        multiply_parts<3>(row_b[k % 2], row_a[k % 2], shares);
-        Eight part[kMiddle];
+      // and the state's next elements are taken apart: a product of matrices occupies its unit for as long as the other one
+      // takes for eight instructions, so that a third of them goes behind each of three products
+      Eight part[2][kMiddle];
+      auto apart = [&](int k) {
         float s[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[e] = state[k / 2][k % 2 * 8 + e];
-        take_apart(s, part);
-        multiply_parts<kWeight>(part, row_a[k % 2], out);
+        take_apart(s, part[k % 2]);
+      };
+      read(0);
+      apart(0);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k = 0; k < 2 * kBlocks; ++k) {
+        if (k + 1 < 2 * kBlocks) {
+          read(k + 1);
+          apart(k + 1);
+        }
+        multiply_parts<3>(row_b[k % 2], row_a[k % 2], shares);
+        multiply_parts<kWeight>(part[k % 2], row_a[k % 2], out);
+        if constexpr (__is_same(T, __bf16)) {
+          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+          for (int i = 0; i < 3; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 8, 0);
+          }
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
       const float query = query_weight * factor;
@@ -474,28 +511,55 @@ __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) vo
         take_apart(s, part);
         multiply_parts<kWeight>(turned_c[k], part, out);
       }
-      if (at + (lane & 31) >= 0) {
-        T* to = static_cast<T*>(w.out.data) + head * w.out.head_stride + (seg.row + sign * (at + (lane & 31))) * w.out.row_stride + column0 + 32 * wave;
-        const bool whole = reinterpret_cast<uintptr_t>(w.out.data) % (4 * sizeof(T)) == 0 && (w.out.row_stride | w.out.head_stride) % 4 == 0;
+      float result[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) result[e] = out[e] * w.out_scale;
+      if constexpr (sizeof(T) == 2) {
+        // Through LDS, so that a lane has 16 bytes of a row and a store 64 bytes of each row that it meets.  As the lanes hold
+        // them, 8 bytes of 32 rows each, a chunk is four times as many requests to the cache: 65536 x 16 x 128 forward and
+        // backward 1650 us, this way 1575.
+        T* mine = staged[wave];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          Pack<T, 4> four;
+          const float x[4] = {result[4 * q], result[4 * q + 1], result[4 * q + 2], result[4 * q + 3]};
+          four.set(x);
+          *reinterpret_cast<Pack<T, 4>*>(mine + (lane & 31) * kPitch + 8 * q + 4 * h) = four;
+        }
+        wave_lds_fence();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int row = i * 16 + lane / 4, piece = lane % 4 * 8, left = w.dc - column0 - 32 * wave - piece;
+          const T* from = mine + row * kPitch + piece;
+          T* to = out_rows + (at + row) * step_out + piece;
+          if (at + row < 0) continue;
+          if (left >= 8) {
+            *reinterpret_cast<Loose*>(to) = *reinterpret_cast<const Words*>(from);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 7; ++j)
+              if (j < left) to[j] = from[j];
+          }
+        }
+        wave_lds_fence();
+      } else if (at + (lane & 31) >= 0) {
+        // 16 bytes of 32 rows each; through LDS 20 x 350 x 12 x 64 took 196 us instead of 142, in more registers
+        T* to = out_rows + (at + (lane & 31)) * step_out;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const int n = 8 * q + 4 * h, left = w.dc - column0 - 32 * wave - n;
-          alignas(16) T four[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) four[j] = from_float<T>(out[4 * q + j] * w.out_scale);
-          if (whole && left >= 4) {
-            if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4*>(to + n) = *reinterpret_cast<const uint4*>(four);
-            else *reinterpret_cast<uint2*>(to + n) = *reinterpret_cast<const uint2*>(four);
+          if (left >= 4) {
+            const float4 x = make_float4(result[4 * q], result[4 * q + 1], result[4 * q + 2], result[4 * q + 3]);
+            *reinterpret_cast<Loose*>(to + n) = __builtin_bit_cast(Loose, x);
           } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (j < left) to[n + j] = four[j];
+            for (int j = 0; j < 3; ++j)
+              if (j < left) to[n + j] = result[4 * q + j];
           }
         }
       }
     }
 
-    __builtin_amdgcn_sched_barrier(0);
     const float before = factor;
     since += at < 0 ? kChunk - short_by : kChunk;
     factor = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, d.power(since))));
@@ -596,7 +660,7 @@ void launch_chunks(const Walks& walks, int count, const Slots& slots, hipStream_
   const Made made(walks.walk[0]);
   int32_t dc = 0;
   for (int i = 0; i < count; ++i) dc = std::max(dc, walks.walk[i].dc);
-  const dim3 grid((uint32_t)(slots.count * walks.walk[0].heads * ((dc + 32 * made.waves - 1) / (32 * made.waves))), (uint32_t)count);
+  const uint32_t grid = places(slots.count * walks.walk[0].heads * ((dc + 32 * made.waves - 1) / (32 * made.waves)), count);
   auto go = [&](auto rows, auto waves, auto narrow) {
     walk_chunks_kernel<T, decltype(rows)::value, decltype(waves)::value, OUT, decltype(narrow)::value><<<grid, 64 * decltype(waves)::value, 0, stream>>>(walks, slots);
   };
@@ -616,7 +680,7 @@ template <typename T>
 void launch_steps(const Walks& walks, int count, hipStream_t stream) {
   int64_t groups = 0;
   for (int i = 0; i < count; ++i) groups = std::max(groups, walk_workgroups(walks.walk[i].sequences, walks.walk[i].heads, walks.walk[i].dc));
-  walk_steps_kernel<T><<<dim3((uint32_t)groups, (uint32_t)count), kThreads, 0, stream>>>(walks);
+  walk_steps_kernel<T><<<places(groups, count), kThreads, 0, stream>>>(walks);
 }
 
 template <typename F>
@@ -657,6 +721,7 @@ void together(const WalkArgs* w, int count, F f) {
         walks.walk[n++] = w[j];
         done[j] = true;
       }
+    walks.count = n;
     f(walks, n);
   }
 }
@@ -691,6 +756,7 @@ hipError_t launch_walks(const WalkArgs* w, int count, int32_t dtype, hipStream_t
   } else {
     Walks walks{};
     for (int i = 0; i < count; ++i) walks.walk[i] = w[i];
+    walks.count = count;
     with_type(dtype, [&](auto t) { launch_steps<decltype(t)>(walks, count, stream); });
   }
   return hipGetLastError();

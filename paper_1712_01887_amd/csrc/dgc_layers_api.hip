@@ -55,7 +55,7 @@ dgc_status check_attention(const dgc_attention* s) {
     return DGC_ERR_CAPACITY;
   if (!s->row_offsets && s->sequences * s->max_length != s->rows) return DGC_ERR_INVALID_ARG;
   if (!aligned_to(s->row_offsets, 8)) return DGC_ERR_ALIGNMENT;
-  return walk_workgroups(s->sequences, s->heads, DGC_HEAD_MAX) < kIntLimit ? DGC_OK : DGC_ERR_CAPACITY;
+  return (walk_workgroups(s->sequences, s->heads, DGC_HEAD_MAX) + 8) * kWalksMax < kIntLimit ? DGC_OK : DGC_ERR_CAPACITY;
 }
 
 dgc_status check_vocab(const dgc_vocab* s) {

@@ -58,6 +58,9 @@ __device__ __forceinline__ float live_weight(const VocabArgs& v, int row, int& l
   return v.row_weight ? v.row_weight[row] : 1.0f;
 }
 
+// 16 bytes at any element's address, which loads take.
+typedef uint32_t Loose __attribute__((ext_vector_type(4), aligned(2)));
+
 __device__ __forceinline__ uint32_t finite_size(float x) {
   const uint32_t bits = __float_as_uint(x) & 0x7fffffffu;
   return bits < 0x7f800000u ? bits : 0u;
@@ -82,16 +85,31 @@ __global__ __launch_bounds__(1024) void weights_kernel(const VocabArgs v, uint32
   }
 }
 
-// The largest element of an array, over rows with a weight if `masked`.  The order of the maxima does not matter.
+// The largest element of an array, over rows with a weight if `masked`.  The order of the maxima does not matter.  A wavefront
+// to a row; one atomic a workgroup: with one a wavefront 2048 workgroups took 130 us for an array that is read in 12.
 __global__ __launch_bounds__(kThreads) void largest_kernel(const VocabArgs v, const float* x, int64_t stride, int rows, bool masked, uint32_t* largest) {
+  __shared__ uint32_t waves[kThreads / 64];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   uint32_t most = 0;
-  for (int r = blockIdx.x; r < rows; r += gridDim.x) {
+  for (int r = blockIdx.x * (kThreads / 64) + wave; r < rows; r += gridDim.x * (kThreads / 64)) {
     int label;
     if (masked && live_weight(v, r, label) == 0.0f) continue;
-    for (int i = threadIdx.x; i < v.width; i += kThreads) most = max(most, finite_size(x[r * stride + i]));
+    const float* row = x + r * stride;
+    int i = 4 * lane;
+    for (; i + 4 <= v.width; i += 256) {
+      const Loose four = *reinterpret_cast<const Loose*>(row + i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) most = max(most, finite_size(__uint_as_float(four[j])));
+    }
+    for (; i < v.width; ++i) most = max(most, finite_size(row[i]));  // the one lane whose four the row ends in
   }
   for (int m = 1; m < 64; m *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, m));
-  if (threadIdx.x % 64 == 0 && most) atomicMax(largest, most);
+  if (lane == 0) waves[wave] = most;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < kThreads / 64; ++i) most = max(most, waves[i]);
+    if (most) atomicMax(largest, most);
+  }
 }
 
 // ---- packed copies ---------------------------------------------------------------------------
@@ -110,15 +128,23 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const VocabArgs v, const
     const bool dead = masked && live_weight(v, row, label) == 0.0f;
     const T* from = x + row * stride + column;
     alignas(16) E parts[Inner<T>::kParts][8];
+    alignas(16) T from_memory[8];
+    if (column + 8 <= v.width) {
+#pragma unroll
+      for (int w = 0; w < (int)sizeof(T) / 2; ++w) reinterpret_cast<uint4*>(from_memory)[w] = __builtin_bit_cast(uint4, reinterpret_cast<const Loose*>(from)[w]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) from_memory[j] = column + j < v.width ? from[j] : (T)0.0f;
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const bool there = !dead && column + j < v.width;
+      const bool there = !dead;
       if constexpr (Inner<T>::kParts == 2) {
-        const float value = there ? from[j] * scale : 0.0f;
+        const float value = there ? from_memory[j] * scale : 0.0f;
         parts[0][j] = (E)value;
         parts[1][j] = (E)(value - (float)parts[0][j]);
       } else {
-        parts[0][j] = there ? from[j] : (T)0.0f;
+        parts[0][j] = there ? from_memory[j] : (T)0.0f;
       }
     }
 #pragma unroll
@@ -395,6 +421,14 @@ Shape shape_of(int64_t m, int64_t n) {
   return tiles(256) >= 200 ? kLarge : tiles(128) >= 200 ? kMiddle : kSmall;
 }
 
+// The same for sums over the vocabulary, which can be split into parts: the largest shape whose tiles fill the device in
+// as many parts as there is room for.
+Shape dhidden_shape(int64_t rows, int64_t width) {
+  const int64_t parts = Layout::splits_at_most(rows);
+  auto groups = [&](int64_t side) { return ((rows + side - 1) / side) * ((width + side - 1) / side) * parts; };
+  return rows > 128 && groups(256) >= 200 ? kLarge : rows > 64 && groups(128) >= 300 ? kMiddle : kSmall;
+}
+
 template <typename F>
 void with_shape(Shape s, F f) {
   if (s == kLarge) f(Large{});
@@ -439,8 +473,8 @@ struct Run {
     if (kParts == 2 || (backward && __is_same(E, _Float16))) weights_kernel<<<1, 1024, 0, stream>>>(v, largest);
     if constexpr (kParts == 2) {
       if (v.rows == 0) return;
-      largest_kernel<<<std::min(v.rows, 2048), kThreads, 0, stream>>>(v, static_cast<const float*>(v.hidden), v.hidden_stride, v.rows, backward, largest + kOfHidden);
-      largest_kernel<<<std::min(v.vocab, 2048), kThreads, 0, stream>>>(v, static_cast<const float*>(v.weight), v.weight_stride, v.vocab, false, largest + kOfWeight);
+      largest_kernel<<<std::min((v.rows + 3) / 4, 1024), kThreads, 0, stream>>>(v, static_cast<const float*>(v.hidden), v.hidden_stride, v.rows, backward, largest + kOfHidden);
+      largest_kernel<<<std::min((v.vocab + 3) / 4, 1024), kThreads, 0, stream>>>(v, static_cast<const float*>(v.weight), v.weight_stride, v.vocab, false, largest + kOfWeight);
     }
   }
 
@@ -488,11 +522,13 @@ struct Run {
           shares_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, w, (int)at.columns, first, columns, largest, shares, piece, plane);
         });
       if (v.rows > 0 && v.dhidden)
-        with_shape(shape_of(v.rows, v.width), [&](auto shape) {
+        with_shape(dhidden_shape(v.rows, v.width), [&](auto shape) {
           using S = decltype(shape);
           const uint32_t tiles = tiles_of(shape, v.rows, v.width);
           const int depth = (int)up(columns, kDepth);
-          if (first == 0) parts = (int)std::max<int64_t>(1, std::min<int64_t>({Layout::splits_at_most(v.rows), (int64_t)(512 / tiles), (int64_t)(depth / 512)}));
+          // as many parts of the sum as the device takes workgroups, of 512 terms at least
+          constexpr int kResident = S::kM == 256 ? 256 : S::kM == 128 ? 512 : 1024;
+          if (first == 0) parts = (int)std::max<int64_t>(1, std::min<int64_t>({Layout::splits_at_most(v.rows), (int64_t)(kResident / tiles), (int64_t)(depth / 512)}));
           const int part = (int)up((depth + parts - 1) / parts, kDepth);
           dhidden_kernel<T, S><<<dim3(tiles, parts), S::kThreads, 0, stream>>>(v, p, w, depth, part, first > 0, total);
         });
