@@ -6,9 +6,15 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "dgc_device.h"
+
 namespace dgc {
 
 typedef float Sums __attribute__((ext_vector_type(16)));
+typedef uint32_t Words2 __attribute__((ext_vector_type(2)));
+typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
+// 16 bytes at any element's address, which loads and stores take.
+typedef uint32_t Loose __attribute__((ext_vector_type(4), aligned(2)));
 
 template <typename E>
 struct Matrix;
@@ -33,7 +39,7 @@ struct Matrix<_Float16> {
 };
 
 // A matrix in memory, `rows` rows `stride` bytes apart, `row_bytes` of each there; `plane` bytes on lies its second part.
-// Every row starts at a multiple of 16 bytes.
+// Every row starts at a multiple of 4 bytes and has whole ones.
 struct Operand {
   const char* data;
   int64_t stride, plane;
@@ -96,6 +102,16 @@ struct Side {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (__attribute__((address_space(3))) void*)(lds + (wave * kLoads + i) * 512), 16, (int)offset[i], 0, 0, 0);
   }
 
+  // Elements from `left` on of every row in LDS, which are not the row's.
+  static __device__ __forceinline__ void clear(E* lds, int left, int threads) {
+    for (int i = threadIdx.x; i < SIDE * kPieces; i += threads) {
+      const int row = i / kPieces, piece = i % kPieces;
+      if (piece * 8 + 8 <= left) continue;
+      E* p = lds + row * kDepth + ((piece ^ exchange(row)) << 3);
+      for (int j = left > piece * 8 ? left - piece * 8 : 0; j < 8; ++j) p[j] = (E)0.0f;
+    }
+  }
+
   // What lane `lane` holds of 32 rows (or columns) from `at` on, 16 elements of the sum from `k` on: row lane % 32, eight
   // elements from 8 (lane / 32) on.
   static __device__ __forceinline__ typename Matrix<E>::Fragment fragment(const E* lds, int at, int k, int lane) {
@@ -112,8 +128,10 @@ struct Side {
 };
 
 // sums[i][j]: of rows m0 + 32 i + lane % 32 of a wavefront's part of the tile and its columns n0 + 32 j + 8 (e / 4) +
-// 4 (lane / 32) + e % 4 in element e, over `depth` (a multiple of kDepth, from `from` on) elements of the sum; with PARTS =
-// 2 operands of two parts, of which the product of the small ones is left out.
+// 4 (lane / 32) + e % 4 in element e, over `depth` elements of the sum from `from` on; with PARTS = 2 operands of two parts,
+// of which the product of the small ones is left out.  The sum goes by whole steps of kDepth.  Where neither operand is
+// ACROSS, what is behind the last one's end in LDS (the next row's elements, or whatever lies between rows) is cleared;
+// otherwise a row of zeros has to stand behind it on one side.
 //
 // While a tile in LDS is multiplied the next one is on its way to another; a barrier a tile.
 template <typename E, typename T, bool ACROSS_A, bool ACROSS_B, int PARTS>
@@ -133,15 +151,24 @@ __device__ __forceinline__ void multiply_tile(Sums (&sums)[T::kBlocksM][T::kBloc
     for (int j = 0; j < T::kBlocksN; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) sums[i][j][e] = 0.0f;
-  const int tiles = depth / kDepth, total = PARTS == 2 ? 3 * tiles : tiles;
+  const int tiles = (depth + kDepth - 1) / kDepth, total = PARTS == 2 ? 3 * tiles : tiles;
   int k = from, part = 0;  // of the tile that is loaded next
   auto load = [&](E* to_a, E* to_b) {
     side_a.load(to_a, k, PARTS == 2 && part == 2, wave);
     side_b.load(to_b, k, PARTS == 2 && part == 1, wave);
     k += kDepth;
-    if (PARTS == 2 && k == from + depth) {
+    if (PARTS == 2 && k >= from + depth) {
       k = from;
       ++part;
+    }
+  };
+  auto trim = [&](E* in_a, E* in_b) {
+    if constexpr (!ACROSS_A && !ACROSS_B && PARTS == 1) {
+      const int left = depth % kDepth;
+      if (left == 0) return;
+      A::clear(in_a, left, T::kThreads);
+      B::clear(in_b, left, T::kThreads);
+      __syncthreads();
     }
   };
   // The fragments of a step of 16 are read while the step before it is multiplied, and no sooner: more of them do not fit
@@ -165,7 +192,7 @@ __device__ __forceinline__ void multiply_tile(Sums (&sums)[T::kBlocksM][T::kBloc
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  if (total == 0) return;
+  if (total <= 0) return;
   load(a0, b0);
   int t = 0;
   for (; t + 2 < total; t += 2) {
@@ -178,9 +205,34 @@ __device__ __forceinline__ void multiply_tile(Sums (&sums)[T::kBlocksM][T::kBloc
   }
   __syncthreads();
   if (t + 1 < total) load(a1, b1);
+  else trim(a0, b0);
   compute(a0, b0);
+  if (t + 1 == total) return;
   __syncthreads();
-  if (t + 1 < total) compute(a1, b1);
+  trim(a1, b1);
+  compute(a1, b1);
+}
+
+// Stores a wavefront's block of 32 x 32 results in 16 bits, lane's row lane % 32 and columns 8 (e / 4) + 4 (lane / 32) + e % 4,
+// by way of LDS, so that a lane has 16 bytes and a store 64 of each row that it meets; as the lanes hold them it is 8 of 32
+// rows.  put(row, column, four words) gets eight elements.
+constexpr int kBlockPitch = 40;
+template <typename E, typename Put>
+__device__ __forceinline__ void store_block(E* mine, const float (&x)[16], int lane, Put put) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    typename Matrix<E>::Half four;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) four[j] = (E)x[4 * q + j];
+    *reinterpret_cast<Words2*>(mine + (lane & 31) * kBlockPitch + 8 * q + 4 * (lane >> 5)) = __builtin_bit_cast(Words2, four);
+  }
+  wave_lds_fence();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = i * 16 + lane / 4, column = lane % 4 * 8;
+    put(row, column, *reinterpret_cast<const Words4*>(mine + row * kBlockPitch + column));
+  }
+  wave_lds_fence();
 }
 
 // Which tile a workgroup takes.  Workgroups go to the eight dies in turn: a die gets neighbouring tiles, eight rows of tiles

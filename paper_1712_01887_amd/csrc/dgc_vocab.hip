@@ -58,9 +58,6 @@ __device__ __forceinline__ float live_weight(const VocabArgs& v, int row, int& l
   return v.row_weight ? v.row_weight[row] : 1.0f;
 }
 
-// 16 bytes at any element's address, which loads take.
-typedef uint32_t Loose __attribute__((ext_vector_type(4), aligned(2)));
-
 __device__ __forceinline__ uint32_t finite_size(float x) {
   const uint32_t bits = __float_as_uint(x) & 0x7fffffffu;
   return bits < 0x7f800000u ? bits : 0u;
@@ -127,29 +124,29 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const VocabArgs v, const
     int label;
     const bool dead = masked && live_weight(v, row, label) == 0.0f;
     const T* from = x + row * stride + column;
-    alignas(16) E parts[Inner<T>::kParts][8];
-    alignas(16) T from_memory[8];
+    float value[8];
     if (column + 8 <= v.width) {
 #pragma unroll
-      for (int w = 0; w < (int)sizeof(T) / 2; ++w) reinterpret_cast<uint4*>(from_memory)[w] = __builtin_bit_cast(uint4, reinterpret_cast<const Loose*>(from)[w]);
+      for (int w = 0; w < (int)sizeof(T) / 2; ++w) {
+        const auto some = __builtin_bit_cast(Pack<T, 16 / sizeof(T)>, reinterpret_cast<const Loose*>(from)[w]);
+#pragma unroll
+        for (int j = 0; j < (int)(16 / sizeof(T)); ++j) value[w * (16 / sizeof(T)) + j] = some.get(j);
+      }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) from_memory[j] = column + j < v.width ? from[j] : (T)0.0f;
+      for (int j = 0; j < 8; ++j) value[j] = column + j < v.width ? to_float(from[j]) : 0.0f;
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const bool there = !dead;
-      if constexpr (Inner<T>::kParts == 2) {
-        const float value = there ? from_memory[j] * scale : 0.0f;
-        parts[0][j] = (E)value;
-        parts[1][j] = (E)(value - (float)parts[0][j]);
-      } else {
-        parts[0][j] = there ? from_memory[j] : (T)0.0f;
+    for (int p = 0; p < Inner<T>::kParts; ++p) {
+      typename Matrix<E>::Fragment part;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (p == 0) value[j] = dead ? 0.0f : value[j] * scale;
+        part[j] = (E)value[j];
+        value[j] -= (float)part[j];
       }
+      *reinterpret_cast<Words4*>(out + p * plane + (int64_t)row * columns + column) = __builtin_bit_cast(Words4, part);
     }
-#pragma unroll
-    for (int p = 0; p < Inner<T>::kParts; ++p)
-      *reinterpret_cast<uint4*>(out + p * plane + (int64_t)row * columns + column) = *reinterpret_cast<const uint4*>(parts[p]);
   }
 }
 
@@ -250,6 +247,7 @@ __global__ __launch_bounds__(S::kThreads) void shares_kernel(const VocabArgs v, 
   const int m0 = tile_m * S::kM, n0 = tile_n * S::kN;
   Sums z[S::kBlocksM][S::kBlocksN];
   multiply_tile<E, S, false, false, kParts>(z, hidden, weight, m0, n0, 0, depth);
+  __shared__ __align__(16) E staged[S::kWaves][32 * kBlockPitch];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int wave_m = wave / S::kWavesN * (S::kBlocksM * 32), wave_n = wave % S::kWavesN * (S::kBlocksN * 32);
   const float unscale_hidden = kParts == 2 ? unscale_of(largest[kOfHidden]) : 1.0f;
@@ -264,24 +262,27 @@ __global__ __launch_bounds__(S::kThreads) void shares_kernel(const VocabArgs v, 
     if (v.diag_flags && first + n0 + wave_n == 0 && lane < 32 && row < v.rows && v.labels[row] >= v.vocab) atomicOr(v.diag_flags, (uint32_t)DGC_DIAG_BAD_INDEX);
     w *= scale;
 #pragma unroll
-    for (int j = 0; j < S::kBlocksN; ++j)
+    for (int j = 0; j < S::kBlocksN; ++j) {
+      float x[16];
 #pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        const int column = n0 + wave_n + 32 * j + 2 * e + 4 * (lane >> 5);
-        alignas(8) E four[kParts][4];
-#pragma unroll
-        for (int f = 0; f < 4; ++f) {
-          float x = z[i][j][e + f];
-          if constexpr (kParts == 2) x = x * unscale_hidden * unscale_weight;
-          float p = __builtin_amdgcn_exp2f((x - lse) * 1.44269504f);
-          if (first + column + f == label) p -= 1.0f;
-          p = w == 0.0f || column + f >= columns ? 0.0f : p * w;
-          four[0][f] = (E)p;
-          if constexpr (kParts == 2) four[1][f] = (E)(p - (float)four[0][f]);
-        }
-#pragma unroll
-        for (int p = 0; p < kParts; ++p) *reinterpret_cast<uint2*>(shares + p * plane + row * stride + column) = *reinterpret_cast<const uint2*>(four[p]);
+      for (int e = 0; e < 16; ++e) {
+        const int column = n0 + wave_n + 32 * j + 8 * (e / 4) + 4 * (lane >> 5) + e % 4;
+        float y = z[i][j][e];
+        if constexpr (kParts == 2) y = y * unscale_hidden * unscale_weight;
+        float p = __builtin_amdgcn_exp2f((y - lse) * 1.44269504f);
+        if (first + column == label) p -= 1.0f;
+        x[e] = w == 0.0f || column >= columns ? 0.0f : p * w;
       }
+      E* to = shares + (int64_t)(m0 + wave_m + 32 * i) * stride + n0 + wave_n + 32 * j;
+      const auto put = [&](int row, int column, Words4 eight) { *reinterpret_cast<Words4*>(to + row * stride + column) = eight; };
+      store_block(staged[wave], x, lane, put);
+      if constexpr (kParts == 2) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] -= (float)(E)x[e];
+        to += plane;
+        store_block(staged[wave], x, lane, put);
+      }
+    }
   }
 }
 
@@ -350,30 +351,45 @@ __global__ __launch_bounds__(S::kThreads) void dweight_kernel(const VocabArgs v,
   const int wave_m = wave / S::kWavesN * (S::kBlocksM * 32), wave_n = wave % S::kWavesN * (S::kBlocksN * 32);
   const float unscale_shares = __is_same(typename Inner<T>::E, _Float16) ? unscale_of(largest[kOfShares]) : 1.0f;
   const float unscale_hidden = Inner<T>::kParts == 2 ? unscale_of(largest[kOfHidden]) : 1.0f;
-  const bool wide = v.dweight_stride % 4 == 0 && reinterpret_cast<uintptr_t>(v.dweight) % (4 * sizeof(T)) == 0;
+  __shared__ __align__(16) T staged[sizeof(T) == 2 ? S::kWaves : 1][sizeof(T) == 2 ? 32 * kBlockPitch : 8];
 #pragma unroll
-  for (int i = 0; i < S::kBlocksM; ++i) {
-    const int row = m0 + wave_m + 32 * i + (lane & 31);
-    if (row >= columns) continue;
+  for (int i = 0; i < S::kBlocksM; ++i)
 #pragma unroll
-    for (int j = 0; j < S::kBlocksN; ++j)
+    for (int j = 0; j < S::kBlocksN; ++j) {
+      const int row0 = m0 + wave_m + 32 * i, column0 = n0 + wave_n + 32 * j;
+      T* to = static_cast<T*>(v.dweight) + (int64_t)(first + row0) * v.dweight_stride + column0;
+      float y[16];
 #pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        const int column = n0 + wave_n + 32 * j + 2 * e + 4 * (lane >> 5);
-        T* to = static_cast<T*>(v.dweight) + (int64_t)(first + row) * v.dweight_stride + column;
-        alignas(16) T four[4];
+      for (int e = 0; e < 16; ++e) y[e] = x[i][j][e] * unscale_shares * unscale_hidden;
+      if constexpr (sizeof(T) == 2) {
+        store_block(staged[wave], y, lane, [&](int row, int column, Words4 eight) {
+          const int left = v.width - column0 - column;
+          if (row0 + row >= columns || left <= 0) return;
+          T* at = to + row * v.dweight_stride + column;
+          if (left >= 8) {
+            *reinterpret_cast<Loose*>(at) = __builtin_bit_cast(Loose, eight);
+          } else {
 #pragma unroll
-        for (int f = 0; f < 4; ++f) four[f] = from_float<T>(x[i][j][e + f] * unscale_shares * unscale_hidden);
-        if (wide && column + 4 <= v.width) {
-          if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(four);
-          else *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(four);
-        } else {
+            for (int k = 0; k < 7; ++k)
+              if (k < left) at[k] = __builtin_bit_cast(T, (uint16_t)(eight[k / 2] >> (k % 2 * 16)));
+          }
+        });
+      } else if (row0 + (lane & 31) < columns) {
+        T* at = to + (lane & 31) * v.dweight_stride + 4 * (lane >> 5);
 #pragma unroll
-          for (int f = 0; f < 4; ++f)
-            if (column + f < v.width) to[f] = four[f];
+        for (int q = 0; q < 4; ++q) {
+          const int left = v.width - column0 - 8 * q - 4 * (lane >> 5);
+          if (left >= 4) {
+            const float4 four = make_float4(y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
+            *reinterpret_cast<Loose*>(at + 8 * q) = __builtin_bit_cast(Loose, four);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+              if (k < left) at[8 * q + k] = y[4 * q + k];
+          }
         }
       }
-  }
+    }
 }
 
 // ---- host ------------------------------------------------------------------------------------
@@ -451,9 +467,9 @@ struct Run {
   hipStream_t stream;
   uint32_t* largest = reinterpret_cast<uint32_t*>(workspace + at.largest);
 
-  // Whether an array can be read as it lies: pieces of 16 bytes, whole steps of the sum, rows that a buffer's 32 bits span.
+  // Whether an array can be read as it lies: rows of whole 4 bytes at multiples of them, that a buffer's 32 bits span.
   bool direct(const void* x, int64_t stride) const {
-    return kParts == 1 && v.width % kDepth == 0 && stride % 8 == 0 && stride <= 1 << 22 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
+    return kParts == 1 && v.width % 2 == 0 && stride % 2 == 0 && stride <= 1 << 22 && reinterpret_cast<uintptr_t>(x) % 4 == 0;
   }
   Operand as_it_lies(const void* x, int64_t stride, int first, int rows) const {
     return {static_cast<const char*>(x) + first * stride * 2, stride * 2, 0, rows, v.width * 2};
@@ -492,7 +508,7 @@ struct Run {
       const Operand w = weight(first, columns);
       with_shape(s, [&](auto shape) {
         using S = decltype(shape);
-        statistics_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, w, (int)at.columns, first, columns, largest, parts, at_label);
+        statistics_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, w, v.width, first, columns, largest, parts, at_label);
         tiles = (v.vocab + S::kN - 1) / S::kN;
       });
     }
@@ -519,7 +535,7 @@ struct Run {
       if (v.rows > 0)
         with_shape(shape_of(v.rows, columns), [&](auto shape) {
           using S = decltype(shape);
-          shares_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, w, (int)at.columns, first, columns, largest, shares, piece, plane);
+          shares_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, w, v.width, first, columns, largest, shares, piece, plane);
         });
       if (v.rows > 0 && v.dhidden)
         with_shape(dhidden_shape(v.rows, v.width), [&](auto shape) {
@@ -530,6 +546,7 @@ struct Run {
           constexpr int kResident = S::kM == 256 ? 256 : S::kM == 128 ? 512 : 1024;
           if (first == 0) parts = (int)std::max<int64_t>(1, std::min<int64_t>({Layout::splits_at_most(v.rows), (int64_t)(kResident / tiles), (int64_t)(depth / 512)}));
           const int part = (int)up((depth + parts - 1) / parts, kDepth);
+          if (first == 0) parts = (depth + part - 1) / part;  // none that begins behind the end; a last piece may have some
           dhidden_kernel<T, S><<<dim3(tiles, parts), S::kThreads, 0, stream>>>(v, p, w, depth, part, first > 0, total);
         });
       if (v.dweight)
