@@ -648,7 +648,7 @@ dgc_status dgc_linear_attention_workspace_bytes(const dgc_attention* shape, int3
  * Sums and states are binary32, also where the matrix units form them: operands are taken apart into bfloat16 parts whose
  * products are exact; what goes into a state, and 32-bit results, lose 2^-23 of a term at most, 16-bit results 2^-15 before
  * they are rounded.  An element that is not finite makes what follows it in its head, and its
- * neighbours up to 63 steps before it, not finite or unspecified.
+ * neighbours up to 31 steps before it, not finite or unspecified.
  * Errors: INVALID_ARG, ALIGNMENT, CAPACITY (workspace, a shape beyond the limits, a row stride of 2^24 or a head stride whose
  * product with the heads passes 2^60), HIP.
  */

@@ -1,5 +1,6 @@
 """MI355X-native hot path of Deep Gradient Compression (arXiv 1712.01887), and operators of the
-recurrent language models whose gradients it carries (top logits, distillation loss, gated scan).
+recurrent language models whose gradients it carries (top logits, distillation loss, gated scan; rotary
+positions, linear attention, vocabulary loss).
 
 `synthetic` lists gradient-set shapes and draws seeded inputs; `binding`
 wraps the C-ABI of libdgc (HIP kernels for gfx950); `build` compiles it.

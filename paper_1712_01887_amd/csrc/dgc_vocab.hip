@@ -5,6 +5,11 @@
 // they are; those of 32 are scaled by a power of two, so that the array's largest is some 2^14, and taken apart into two
 // parts of binary16, whose products (but that of the small parts) are summed: of an element x, 2^-22 |x| is lost at most,
 // and 2^-39 of the largest.
+//
+// Bound by the matrix units: 4096 rows, width 2048, vocabulary 131072 in bfloat16, forward and backward, are 8.8 TFLOP in 7.51 ms,
+// 1171 TFLOP/s (a library's product of that shape reaches 1293): statistics 1.99 ms, shares 2.12, dhidden 2.38, dweight 1.86 by
+// the profiler.  The logits are formed twice because dweight needs the log-sum-exp: 8 units of rows * vocab * width where 6
+// would do if logits were kept.
 
 #include "dgc_layers.h"
 #include "dgc_product.h"
@@ -431,7 +436,9 @@ struct Layout {
 
 enum Shape { kLarge, kMiddle, kSmall };
 
-// The largest shape whose tiles are enough for the device's 256 compute units; small ones take four to a unit.
+// The largest shape whose tiles are enough for most of the device's 256 compute units; small ones take four to a unit.  A tile
+// of 256 x 256 reads half as much for a product as four of 128 x 128: 4096 x 8192 x 2048 takes 116 to 133 us in large tiles
+// (dweight, shares), 4096 x 2048 x 8192, which has only 128 of them, 149 in middle ones (dhidden).
 Shape shape_of(int64_t m, int64_t n) {
   auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
   return tiles(256) >= 200 ? kLarge : tiles(128) >= 200 ? kMiddle : kSmall;

@@ -285,6 +285,27 @@ def test_captured_and_on_another_stream(length):
                 assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("lengths", [[5000], [2049, 0, 1], [700, 3], [2, 1]])
+def test_states_left_in_place(lengths):
+    """state_last in state0's place and dstate0 in dstate_last's, also where sequences are cut into segments that run at the same
+    time: what arrays of their own hold, to the bit."""
+    import torch
+    heads, d, n = 2, 64, sum(lengths)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    q, k, v, do = (torch.randn(n, heads, d, generator=gen, device="cuda").bfloat16() for _ in range(4))
+    rates = torch.tensor([-0.0001, -0.002], device="cuda")
+    offsets = torch.tensor(np.concatenate([[0], np.cumsum(lengths)])).cuda()
+    plan = B.LinearAttention(len(lengths), max(lengths), heads, d, d, torch.bfloat16, row_offsets=offsets, rows=n)
+    first, flow = (torch.randn(len(lengths), heads, d, d, generator=gen, device="cuda") for _ in range(2))
+    want, got = [torch.empty_like(q) for _ in range(4)], [torch.empty_like(q) for _ in range(4)]
+    last, d0 = torch.empty_like(first), torch.empty_like(first)
+    plan.dgc_linear_attention_forward(q, k, v, rates, first, want[0], last)
+    plan.dgc_linear_attention_backward(q, k, v, rates, first, do, flow, *want[1:], d0)
+    plan.dgc_linear_attention_backward(q, k, v, rates, first, do, flow, *got[1:], flow)
+    plan.dgc_linear_attention_forward(q, k, v, rates, first, got[0], first)
+    assert all(torch.equal(x, y) for x, y in zip(want, got)) and torch.equal(first, last) and torch.equal(flow, d0)
+
+
 def test_same_bits_on_every_run():
     import torch
     heads, d, n = 3, 64, 5000
