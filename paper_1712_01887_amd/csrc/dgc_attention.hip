@@ -31,28 +31,27 @@ __device__ __forceinline__ int64_t place(const Walks& walks, int& walk) {
 inline uint32_t places(int64_t groups, int count) { return (uint32_t)((groups + 7) / 8 * 8 * count); }
 
 // ---- steps -------------------------------------------------------------------------------------
-constexpr int kColumns = 32;  // columns of the state to a workgroup, four to a thread
+constexpr int kColumns = 32;  // columns of the state to a workgroup at least
 constexpr int kThreads = 256;
-constexpr int kRowThreads = kThreads * 4 / kColumns;
-constexpr int kRows = DGC_HEAD_MAX / kRowThreads;  // to a thread, kRowThreads apart
 
-// One step after the other: what bounds it is the state, which is read and written once.  A thread has four columns of up to
-// kRows of its rows in registers; o is summed over the eight rows of a wavefront by exchanges, over the wavefronts in LDS, in
-// their order.  Everything that a step reads is asked for at once.
-template <typename T>
+// One step after the other: what bounds it is the state, which is read and written once.  A thread has four of COLUMNS columns
+// and up to ROWS of their rows in registers; o is summed over the rows of a wavefront by exchanges, over the wavefronts in LDS,
+// in their order.  Everything that a step reads is asked for at once.
+template <typename T, int COLUMNS, int ROWS>
 __global__ __launch_bounds__(kThreads) void walk_steps_kernel(const Walks walks) {
+  constexpr int kRowThreads = kThreads * 4 / COLUMNS, kRows = ROWS;  // a thread's rows are kRowThreads apart
   int which;
   const int64_t group = place(walks, which);
   const WalkArgs& w = walks.walk[which];
-  __shared__ float4 sums[2][kThreads / 64][kColumns / 4];
-  const int tiles = (w.dc + kColumns - 1) / kColumns;
+  __shared__ float4 sums[2][kThreads / 64][COLUMNS / 4];
+  const int tiles = (w.dc + COLUMNS - 1) / COLUMNS;
   const int tile = (int)(group % tiles), head = (int)(group / tiles % w.heads);
   const int64_t sequence = group / tiles / w.heads;
   if (sequence >= w.sequences) return;  // whole rounds of the dies, and the walk with the most tiles
   const int64_t lo = w.row_offsets ? w.row_offsets[sequence] : sequence * w.max_length;
   const int64_t hi = w.row_offsets ? w.row_offsets[sequence + 1] : lo + w.max_length;
   const SequenceRows rows(lo, hi, w.rows, w.max_length);
-  const int column = tile * kColumns + 4 * ((int)threadIdx.x % (kColumns / 4)), row0 = (int)threadIdx.x / (kColumns / 4);
+  const int column = tile * COLUMNS + 4 * ((int)threadIdx.x % (COLUMNS / 4)), row0 = (int)threadIdx.x / (COLUMNS / 4);
   const int columns = w.dc - column;  // that are there, from this thread's first on
   const bool whole = columns >= 4 && w.state_c == 1 && w.state_a % 4 == 0;
   const bool whole_first = whole && reinterpret_cast<uintptr_t>(w.first) % 16 == 0, whole_last = whole && reinterpret_cast<uintptr_t>(w.last) % 16 == 0;
@@ -100,13 +99,13 @@ __global__ __launch_bounds__(kThreads) void walk_steps_kernel(const Walks walks)
           s[i][j] *= after;
         }
 #pragma unroll
-    for (int m = kColumns / 4; m < 64; m *= 2)
+    for (int m = COLUMNS / 4; m < 64; m *= 2)
 #pragma unroll
       for (int j = 0; j < 4; ++j) sum[j] += __shfl_xor(sum[j], m);
     // of two rows of sums the other one may still be read
-    if (threadIdx.x % 64 < kColumns / 4) sums[t & 1][threadIdx.x / 64][threadIdx.x % 64] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    if (threadIdx.x % 64 < COLUMNS / 4) sums[t & 1][threadIdx.x / 64][threadIdx.x % 64] = make_float4(sum[0], sum[1], sum[2], sum[3]);
     __syncthreads();
-    if (threadIdx.x < kColumns / 4) {
+    if (threadIdx.x < COLUMNS / 4) {
       for (int i = 1; i < kThreads / 64; ++i) {
         const float4 other = sums[t & 1][i][threadIdx.x];
         sum[0] += other.x, sum[1] += other.y, sum[2] += other.z, sum[3] += other.w;
@@ -684,9 +683,23 @@ void launch_chunks(const Walks& walks, int count, const Slots& slots, hipStream_
 
 template <typename T>
 void launch_steps(const Walks& walks, int count, hipStream_t stream) {
-  int64_t groups = 0;
-  for (int i = 0; i < count; ++i) groups = std::max(groups, walk_workgroups(walks.walk[i].sequences, walks.walk[i].heads, walks.walk[i].dc));
-  walk_steps_kernel<T><<<places(groups, count), kThreads, 0, stream>>>(walks);
+  // 128 columns to a workgroup where all walks have more than 64 of them, and up to 128 rows: 512 bytes of a row to a wavefront's
+  // load, and a thread has 8 or 16 loads on their way (64 x 16 states of 64 x 128: 17.2 us, 3.9 TB/s; by 32 columns 22.8)
+  int32_t rows = 0, least = DGC_HEAD_MAX, most = 0;
+  for (int i = 0; i < count; ++i) {
+    rows = std::max(rows, walks.walk[i].da);
+    least = std::min(least, walks.walk[i].dc);
+    most = std::max(most, walks.walk[i].dc);
+  }
+  const int64_t heads = walks.walk[0].sequences * walks.walk[0].heads;
+  auto go = [&](auto columns, auto held) {
+    constexpr int kWide = decltype(columns)::value;
+    walk_steps_kernel<T, kWide, decltype(held)::value><<<places(heads * ((most + kWide - 1) / kWide), count), kThreads, 0, stream>>>(walks);
+  };
+  if (least > 64 && rows <= 64) go(std::integral_constant<int, 128>(), std::integral_constant<int, 8>());
+  else if (least > 64 && rows <= 128) go(std::integral_constant<int, 128>(), std::integral_constant<int, 16>());
+  else if (rows <= 64) go(std::integral_constant<int, 32>(), std::integral_constant<int, 2>());
+  else go(std::integral_constant<int, 32>(), std::integral_constant<int, 8>());
 }
 
 template <typename F>

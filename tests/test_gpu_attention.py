@@ -78,6 +78,13 @@ def test_lengths(length, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("dk,dv", [(64, 128), (128, 128), (72, 66), (33, 256), (129, 130), (256, 256), (64, 65), (200, 7)])
+def test_single_steps_of_many_sizes(dk, dv, dtype):
+    check([1] * 5, 3, dk, dv, dtype, packed=False, seed=dk, decays=[-0.05, -2.0, 0.0])
+    check([3, 0, 4, 1], 2, dk, dv, dtype, seed=dv, decays=[-0.05, -0.7], layout=dict(gap=1))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_every_decay(dtype):
     check([150, 3, 40], 7, 20, 24, dtype)
 
