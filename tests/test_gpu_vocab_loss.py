@@ -83,6 +83,14 @@ def test_sizes(rows, vocab, width, dtype):
     check(rows, vocab, width, dtype)
 
 
+@pytest.mark.parametrize("rows,vocab,width,dtype", [(2100, 20000, 64, "f32"), (2100, 20000, 64, "bf16"), (10, 5000, 16385, "bf16"),
+                                                    (10, 5000, 16385, "f32"), (5000, 300, 64, "f16"), (3, 100001, 40, "f32")])
+def test_several_pieces(rows, vocab, width, dtype):
+    """More shares than are kept at a time, more of the weight than is packed at a time, and more rows than sums are kept in
+    parts for."""
+    check(rows, vocab, width, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("gap,lead", [(0, 0), (8, 8), (3, 1), (64, 0), (1, 0), (8, 1)])
 def test_strides_and_masks(gap, lead, dtype):
