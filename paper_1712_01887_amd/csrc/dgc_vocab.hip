@@ -162,7 +162,12 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const VocabArgs v, const
 }
 
 // ---- statistics ------------------------------------------------------------------------------
-// The largest logit and the sum of exponentials of every row of a tile, at [tile of columns][row]; a label's logit.
+// What largest logits have to be subtracted in exponents: where there is none, -inf, nothing is.
+__device__ __forceinline__ float shift_of(float top) { return top == -INFINITY ? 0.0f : top; }
+
+// The largest logit and the sum of exponentials of every row of a tile, at [tile of columns][row]; a label's logit.  A part
+// without a column, a wavefront's behind the vocabulary, has -inf and 0, which change nothing where parts are joined: any
+// finite number there would scale rows of very negative logits away.
 template <typename T, typename S>
 __global__ __launch_bounds__(S::kThreads) void statistics_kernel(const VocabArgs v, Operand hidden, Operand weight, int depth, int first, int columns,
                                                                  const uint32_t* largest, float2* parts, float* at_label) {
@@ -195,13 +200,13 @@ __global__ __launch_bounds__(S::kThreads) void statistics_kernel(const VocabArgs
         z[i][j][e] = x;
       }
     top = fmaxf(top, __shfl_xor(top, 32));
-    const float shift = top == -INFINITY ? 0.0f : top;
+    const float shift = shift_of(top);
 #pragma unroll
     for (int j = 0; j < S::kBlocksN; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f((z[i][j][e] - shift) * 1.44269504f);
     sum += __shfl_xor(sum, 32);
-    if (lane < 32) joined[wave % S::kWavesN][row] = make_float2(shift, sum);
+    if (lane < 32) joined[wave % S::kWavesN][row] = make_float2(top, sum);
   }
   __syncthreads();
   for (int row = threadIdx.x; row < S::kM; row += S::kThreads) {
@@ -209,10 +214,18 @@ __global__ __launch_bounds__(S::kThreads) void statistics_kernel(const VocabArgs
     float top = joined[0][row].x, sum = 0.0f;
 #pragma unroll
     for (int i = 1; i < S::kWavesN; ++i) top = fmaxf(top, joined[i][row].x);
+    const float shift = shift_of(top);
 #pragma unroll
-    for (int i = 0; i < S::kWavesN; ++i) sum += joined[i][row].y * __builtin_amdgcn_exp2f((joined[i][row].x - top) * 1.44269504f);
+    for (int i = 0; i < S::kWavesN; ++i) sum += joined[i][row].y * __builtin_amdgcn_exp2f((joined[i][row].x - shift) * 1.44269504f);
     parts[(int64_t)(first / S::kN + tile_n) * v.rows + m0 + row] = make_float2(top, sum);
   }
+}
+
+// Joins a part's largest logit and sum to those of the parts before it.
+__device__ __forceinline__ void join(float& top, float& sum, float2 part) {
+  const float larger = fmaxf(top, part.x), shift = shift_of(larger);
+  sum = sum * __builtin_amdgcn_exp2f((top - shift) * 1.44269504f) + part.y * __builtin_amdgcn_exp2f((part.x - shift) * 1.44269504f);
+  top = larger;
 }
 
 // A row to 8 threads, which take its tiles in turn.
@@ -221,23 +234,12 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const VocabArgs v, const
   __shared__ float2 joined[8][kThreads / 8];
   float top = -INFINITY, sum = 0.0f;
   if (row < v.rows)
-    for (int i = part; i < tiles; i += 8) {
-      const float2 p = parts[(int64_t)i * v.rows + row];
-      const float larger = fmaxf(top, p.x);
-      // -inf - -inf never meets a sum: the parts' maxima are finite
-      sum = sum * __builtin_amdgcn_exp2f((top - larger) * 1.44269504f) + p.y * __builtin_amdgcn_exp2f((p.x - larger) * 1.44269504f);
-      top = larger;
-    }
+    for (int i = part; i < tiles; i += 8) join(top, sum, parts[(int64_t)i * v.rows + row]);
   joined[part][threadIdx.x % (kThreads / 8)] = make_float2(top, sum);
   __syncthreads();
   if (part != 0 || row >= v.rows) return;
   const int n = tiles < 8 ? tiles : 8;
-  for (int i = 1; i < n; ++i) {
-    const float2 p = joined[i][threadIdx.x];
-    const float larger = fmaxf(top, p.x);
-    sum = sum * __builtin_amdgcn_exp2f((top - larger) * 1.44269504f) + p.y * __builtin_amdgcn_exp2f((p.x - larger) * 1.44269504f);
-    top = larger;
-  }
+  for (int i = 1; i < n; ++i) join(top, sum, joined[i][threadIdx.x]);
   const float lse = top + logf(sum);
   int label;
   const float w = live_weight(v, row, label);
