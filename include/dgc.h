@@ -694,9 +694,10 @@ dgc_status dgc_vocab_loss_workspace_bytes(const dgc_vocab* shape, int32_t backwa
  *   row_weight  device, float[rows], or NULL for ones.  A row of weight zero has loss zero, whatever else it holds
  *   loss, lse   device, float[rows], either may be NULL; lse is of every row, also of one without a label
  *   diag_flags_dev  device uint32 or NULL: DGC_DIAG_BAD_INDEX is ORed in for a label >= vocab, which counts as none
- * Products are summed in binary32.  Those of 16-bit elements are exact.  Binary32 elements are scaled by a power of two and
- * taken apart into two binary16 parts, and the product of the small parts is left out: 3 * 2^-22 of a product is lost at
- * most, and 2^-39 of what the array's largest element would make of it.
+ * Products are summed in binary32.  Those of 16-bit elements are exact.  Binary32 elements are taken apart into three
+ * bfloat16 parts, which hold all of them (of elements below 2^-102 some bits may be lost), and the three smallest of the nine
+ * products are left out: 2^-23 of a product at most, whatever other rows and columns hold.  An infinite binary32 element makes
+ * NaN of the logits that it goes into.
  * Errors: INVALID_ARG, ALIGNMENT, CAPACITY, HIP.
  */
 dgc_status dgc_vocab_loss_forward(const dgc_vocab* shape, const void* hidden, const void* weight, const int32_t* labels,

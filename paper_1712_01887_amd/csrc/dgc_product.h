@@ -38,7 +38,7 @@ struct Matrix<_Float16> {
   }
 };
 
-// A matrix in memory, `rows` rows `stride` bytes apart, `row_bytes` of each there; `plane` bytes on lies its second part.
+// A matrix in memory, `rows` rows `stride` bytes apart, `row_bytes` of each there; `plane` bytes on lies its next part.
 // Every row starts at a multiple of 4 bytes and has whole ones.
 struct Operand {
   const char* data;
@@ -46,7 +46,9 @@ struct Operand {
   int32_t rows, row_bytes;
 };
 
-constexpr int kDepth = 64;  // of the sum at a time
+constexpr int kDepth = 64;  // of the sum at a time; of operands of three parts, whose tiles have to fit LDS together, half of it
+template <int PARTS>
+constexpr int kDepthOf = PARTS == 1 ? kDepth : kDepth / 2;
 
 // A tile of rows x columns, by waves_m x waves_n wavefronts.
 template <int M, int N, int WAVES_M, int WAVES_N>
@@ -56,25 +58,27 @@ struct Tile {
   static constexpr int kBlocksM = M / WAVES_M / 32, kBlocksN = N / WAVES_N / 32;  // of 32 x 32 to a wavefront
 };
 
-// One side of a tile: SIDE rows (or, ACROSS, columns) of an operand, kDepth of the other kind at a time.
+// One side of a tile: SIDE rows (or, ACROSS, columns) of an operand, DEPTH of the other kind at a time.
 //
 // Loads go from memory to LDS without registers in between: 64 lanes leave 64 pieces of 16 bytes behind each other, so that
-// what is swizzled is which piece a lane asks for.  Along: 128 bytes to a row, whose eight pieces are exchanged by half the
-// row's number, so that the 16 rows that 16 lanes read lie in 16 different places of 256 bytes, all the banks there are.
+// what is swizzled is which piece a lane asks for.  Along: 128 (or 64) bytes to a row, whose eight (four) pieces are exchanged
+// by half (a quarter of) the row's number, so that the 16 rows that 16 lanes read lie in 16 different places of 256 bytes, all
+// the banks there are.
 // Across: the sum runs over the rows; blocks of 64 bytes are exchanged by the row's number, so that the four rows from which
 // 16 lanes take 4 elements of a column each lie in different banks.
-template <typename E, int SIDE, bool ACROSS, int WAVES>
+template <typename E, int SIDE, bool ACROSS, int WAVES, int DEPTH>
 struct Side {
-  static constexpr int kElements = SIDE * kDepth;
+  static_assert(DEPTH == 32 || DEPTH == 64, "the places of pieces");
+  static constexpr int kElements = SIDE * DEPTH;
   static constexpr int kLoads = kElements * 2 / 1024 / WAVES;  // to a wavefront, of 1024 bytes
   static_assert(kLoads * WAVES * 1024 == kElements * 2, "whole loads");
-  static constexpr int kPieces = (ACROSS ? SIDE : kDepth) / 8;  // of 16 bytes to a row in LDS
+  static constexpr int kPieces = (ACROSS ? SIDE : DEPTH) / 8;  // of 16 bytes to a row in LDS
   const char* base;
   int64_t stride, plane;
   int32_t rows, row_bytes;  // left from `base` on; rows of the array
   uint32_t offset[kLoads];
 
-  static __device__ __forceinline__ int exchange(int row) { return ACROSS ? (SIDE >= 128 ? row & 3 : (row >> 1) & 1) : (row >> 1) & 7; }
+  static __device__ __forceinline__ int exchange(int row) { return ACROSS ? (SIDE >= 128 ? row & 3 : (row >> 1) & 1) : DEPTH == 64 ? (row >> 1) & 7 : (row >> 2) & 3; }
 
   // The tile begins at row (or column) `first`.
   __device__ __forceinline__ void start(const Operand& o, int first, int wave, int lane) {
@@ -91,10 +95,10 @@ struct Side {
     }
   }
 
-  // Elements [k, k + kDepth) of the sum, of part `part`.  Behind the array's last row, zeros: the buffer ends there.
+  // Elements [k, k + DEPTH) of the sum, of part `part`.  Behind the array's last row, zeros: the buffer ends there.
   __device__ __forceinline__ void load(E* lds, int k, int part, int wave) const {
     const char* from = base + part * plane + (ACROSS ? (int64_t)k * stride : (int64_t)k * 2);
-    const int have = ACROSS ? rows - k : rows, most = ACROSS ? kDepth : SIDE;
+    const int have = ACROSS ? rows - k : rows, most = ACROSS ? DEPTH : SIDE;
     const int64_t bytes = have <= 0 ? 0 : (int64_t)((have < most ? have : most) - 1) * stride + row_bytes - (ACROSS ? 0 : k * 2);
     const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, (int)(uint32_t)bytes, 0x00020000);
 #pragma unroll
@@ -107,7 +111,7 @@ struct Side {
     for (int i = threadIdx.x; i < SIDE * kPieces; i += threads) {
       const int row = i / kPieces, piece = i % kPieces;
       if (piece * 8 + 8 <= left) continue;
-      E* p = lds + row * kDepth + ((piece ^ exchange(row)) << 3);
+      E* p = lds + row * DEPTH + ((piece ^ exchange(row)) << 3);
       for (int j = left > piece * 8 ? left - piece * 8 : 0; j < 8; ++j) p[j] = (E)0.0f;
     }
   }
@@ -122,23 +126,28 @@ struct Side {
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
       const int row = at + (lane & 31), piece = k / 8 + (lane >> 5);
-      return *reinterpret_cast<const typename Matrix<E>::Fragment*>(lds + row * kDepth + ((piece ^ exchange(row)) << 3));
+      return *reinterpret_cast<const typename Matrix<E>::Fragment*>(lds + row * DEPTH + ((piece ^ exchange(row)) << 3));
     }
   }
 };
 
 // sums[i][j]: of rows m0 + 32 i + lane % 32 of a wavefront's part of the tile and its columns n0 + 32 j + 8 (e / 4) +
-// 4 (lane / 32) + e % 4 in element e, over `depth` elements of the sum from `from` on; with PARTS = 2 operands of two parts,
-// of which the product of the small ones is left out.  The sum goes by whole steps of kDepth.  Where neither operand is
-// ACROSS, what is behind the last one's end in LDS (the next row's elements, or whatever lies between rows) is cleared;
-// otherwise a row of zeros has to stand behind it on one side.
+// 4 (lane / 32) + e % 4 in element e, over `depth` elements of the sum from `from` on.  The sum goes by whole steps of kDepthOf.
+// Of operands in one part of which neither is ACROSS, what is behind the last one's end in LDS (the next row's elements, or
+// whatever lies between rows) is cleared; otherwise a row of zeros has to stand behind it on one side.
+//
+// Operands in three parts: the six products of parts i and j with i + j < 3, the small ones first.  All the parts of a tile are
+// in LDS at a time, so that a fragment that is read is multiplied up to three times: read for each product by itself, as many
+// bytes of LDS would be wanted as it can give.
 //
 // While a tile in LDS is multiplied the next one is on its way to another; a barrier a tile.
 template <typename E, typename T, bool ACROSS_A, bool ACROSS_B, int PARTS>
 __device__ __forceinline__ void multiply_tile(Sums (&sums)[T::kBlocksM][T::kBlocksN], const Operand& a, const Operand& b, int m0, int n0, int from, int depth) {
-  using A = Side<E, T::kM, ACROSS_A, T::kWaves>;
-  using B = Side<E, T::kN, ACROSS_B, T::kWaves>;
-  __shared__ __align__(16) E a0[A::kElements], a1[A::kElements], b0[B::kElements], b1[B::kElements];
+  static_assert(PARTS == 1 || PARTS == 3, "parts");
+  constexpr int kStep = kDepthOf<PARTS>;
+  using A = Side<E, T::kM, ACROSS_A, T::kWaves, kStep>;
+  using B = Side<E, T::kN, ACROSS_B, T::kWaves, kStep>;
+  __shared__ __align__(16) E a0[PARTS * A::kElements], a1[PARTS * A::kElements], b0[PARTS * B::kElements], b1[PARTS * B::kElements];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int wave_m = wave / T::kWavesN * (T::kBlocksM * 32), wave_n = wave % T::kWavesN * (T::kBlocksN * 32);
   A side_a;
@@ -151,20 +160,19 @@ __device__ __forceinline__ void multiply_tile(Sums (&sums)[T::kBlocksM][T::kBloc
     for (int j = 0; j < T::kBlocksN; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) sums[i][j][e] = 0.0f;
-  const int tiles = (depth + kDepth - 1) / kDepth, total = PARTS == 2 ? 3 * tiles : tiles;
-  int k = from, part = 0;  // of the tile that is loaded next
+  const int tiles = (depth + kStep - 1) / kStep;
+  int k = from;  // of the tile that is loaded next
   auto load = [&](E* to_a, E* to_b) {
-    side_a.load(to_a, k, PARTS == 2 && part == 2, wave);
-    side_b.load(to_b, k, PARTS == 2 && part == 1, wave);
-    k += kDepth;
-    if (PARTS == 2 && k >= from + depth) {
-      k = from;
-      ++part;
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+      side_a.load(to_a + p * A::kElements, k, p, wave);
+      side_b.load(to_b + p * B::kElements, k, p, wave);
     }
+    k += kStep;
   };
   auto trim = [&](E* in_a, E* in_b) {
     if constexpr (!ACROSS_A && !ACROSS_B && PARTS == 1) {
-      const int left = depth % kDepth;
+      const int left = depth % kStep;
       if (left == 0) return;
       A::clear(in_a, left, T::kThreads);
       B::clear(in_b, left, T::kThreads);
@@ -174,28 +182,35 @@ __device__ __forceinline__ void multiply_tile(Sums (&sums)[T::kBlocksM][T::kBloc
   // The fragments of a step of 16 are read while the step before it is multiplied, and no sooner: more of them do not fit
   // beside the sums.
   auto compute = [&](const E* from_a, const E* from_b) {
-    typename Matrix<E>::Fragment fa[2][T::kBlocksM], fb[2][T::kBlocksN];
+    typename Matrix<E>::Fragment fa[2][PARTS][T::kBlocksM], fb[2][PARTS][T::kBlocksN];
     auto read = [&](int set, int d) {
 #pragma unroll
-      for (int j = 0; j < T::kBlocksN; ++j) fb[set][j] = B::fragment(from_b, wave_n + 32 * j, d, lane);
+      for (int p = 0; p < PARTS; ++p) {
 #pragma unroll
-      for (int i = 0; i < T::kBlocksM; ++i) fa[set][i] = A::fragment(from_a, wave_m + 32 * i, d, lane);
+        for (int j = 0; j < T::kBlocksN; ++j) fb[set][p][j] = B::fragment(from_b + p * B::kElements, wave_n + 32 * j, d, lane);
+#pragma unroll
+        for (int i = 0; i < T::kBlocksM; ++i) fa[set][p][i] = A::fragment(from_a + p * A::kElements, wave_m + 32 * i, d, lane);
+      }
     };
     read(0, 0);
 #pragma unroll
-    for (int step = 0; step < kDepth / 16; ++step) {
-      if (step + 1 < kDepth / 16) read((step + 1) % 2, 16 * step + 16);
+    for (int step = 0; step < kStep / 16; ++step) {
+      if (step + 1 < kStep / 16) read((step + 1) % 2, 16 * step + 16);
 #pragma unroll
-      for (int i = 0; i < T::kBlocksM; ++i)
+      for (int both = PARTS - 1; both >= 0; --both)
 #pragma unroll
-        for (int j = 0; j < T::kBlocksN; ++j) sums[i][j] = Matrix<E>::multiply(fb[step % 2][j], fa[step % 2][i], sums[i][j]);
+        for (int p = 0; p <= both; ++p)
+#pragma unroll
+          for (int i = 0; i < T::kBlocksM; ++i)
+#pragma unroll
+            for (int j = 0; j < T::kBlocksN; ++j) sums[i][j] = Matrix<E>::multiply(fb[step % 2][both - p][j], fa[step % 2][p][i], sums[i][j]);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  if (total <= 0) return;
+  if (tiles <= 0) return;
   load(a0, b0);
   int t = 0;
-  for (; t + 2 < total; t += 2) {
+  for (; t + 2 < tiles; t += 2) {
     __syncthreads();
     load(a1, b1);
     compute(a0, b0);
@@ -204,10 +219,10 @@ __device__ __forceinline__ void multiply_tile(Sums (&sums)[T::kBlocksM][T::kBloc
     compute(a1, b1);
   }
   __syncthreads();
-  if (t + 1 < total) load(a1, b1);
+  if (t + 1 < tiles) load(a1, b1);
   else trim(a0, b0);
   compute(a0, b0);
-  if (t + 1 == total) return;
+  if (t + 1 == tiles) return;
   __syncthreads();
   trim(a1, b1);
   compute(a1, b1);

@@ -2,14 +2,18 @@
 //
 // Four products: the logits hidden weight^T, formed once for their statistics and once for the shares P; P weight and
 // P^T hidden.  A piece of the vocabulary at a time, P of a piece is all that is kept.  Elements of 16 bits are multiplied as
-// they are; those of 32 are scaled by a power of two, so that the array's largest is some 2^14, and taken apart into two
-// parts of binary16, whose products (but that of the small parts) are summed: of an element x, 2^-22 |x| is lost at most,
-// and 2^-39 of the largest.
+// they are; those of 32 are taken apart into three parts of bfloat16 (24 bits in three times eight, none lost), of whose products
+// the six large ones are summed: 2^-23 of a product is left out at most.  bfloat16 has binary32's exponents, so that this is so
+// whatever other rows and columns hold.  Two parts of binary16 take half the products, but need a scale, and however that is
+// shared (by an array, by rows), some sum runs over rows of different ones: a row of 1e20 that counts nothing made zeros of
+// its neighbours.
 //
 // Bound by the matrix units: 4096 rows, width 2048, vocabulary 131072 in bfloat16, forward and backward, are 8.8 TFLOP in 7.51 ms,
 // 1171 TFLOP/s (a library's product of that shape reaches 1293): statistics 1.99 ms, shares 2.12, dhidden 2.38, dweight 1.86 by
 // the profiler.  The logits are formed twice because dweight needs the log-sum-exp: 8 units of rows * vocab * width where 6
 // would do if logits were kept.
+
+#include <type_traits>
 
 #include "dgc_layers.h"
 #include "dgc_product.h"
@@ -34,18 +38,21 @@ struct Inner {  // what an element is multiplied as
 };
 template <>
 struct Inner<float> {
-  using E = _Float16;
-  static constexpr int kParts = 2;
+  using E = __bf16;
+  static constexpr int kParts = 3;
 };
+// The upper 16 bits, a bfloat16 part that is no larger.
+__device__ __forceinline__ float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
 
 using Large = Tile<256, 256, 2, 4>;
 using Middle = Tile<128, 128, 2, 2>;
 using Small = Tile<64, 64, 2, 2>;
+// Of operands in three parts, of which LDS holds one workgroup's: with eight wavefronts, two to a SIMD, one multiplies while the
+// other reads.  700 x 10000 x 1500 in binary32, forward and backward: 615 us, with four wavefronts 656.
+using Middle3 = Tile<128, 128, 2, 4>;
 
-// ---- powers of two that elements are scaled by -----------------------------------------------
-// Bits of the largest absolute value: of row weights, of hidden and of weight.
-enum { kOfShares = 0, kOfHidden = 1, kOfWeight = 2, kScales = 3 };
-
+// ---- scale of shares in binary16 -------------------------------------------------------------
+// `largest`: the bits of the largest absolute row weight.
 __device__ __forceinline__ int exponent_of(uint32_t largest) {
   const int e = (int)(largest >> 23);
   return e < 28 ? 28 : e;  // scales and their inverses stay normal
@@ -74,7 +81,7 @@ __device__ __forceinline__ uint32_t finite_size(float x) {
   return bits < 0x7f800000u ? bits : 0u;
 }
 
-// The largest row weight, one workgroup; the other two words are cleared for largest_kernel.
+// The largest row weight, one workgroup.
 __global__ __launch_bounds__(1024) void weights_kernel(const VocabArgs v, uint32_t* largest) {
   __shared__ uint32_t waves[16];
   uint32_t most = 0;
@@ -87,49 +94,19 @@ __global__ __launch_bounds__(1024) void weights_kernel(const VocabArgs v, uint32
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int i = 1; i < 16; ++i) most = max(most, waves[i]);
-    largest[kOfShares] = most;
-    largest[kOfHidden] = 0;
-    largest[kOfWeight] = 0;
-  }
-}
-
-// The largest element of an array, over rows with a weight if `masked`.  The order of the maxima does not matter.  A wavefront
-// to a row; one atomic a workgroup: with one a wavefront 2048 workgroups took 130 us for an array that is read in 12.
-__global__ __launch_bounds__(kThreads) void largest_kernel(const VocabArgs v, const float* x, int64_t stride, int rows, bool masked, uint32_t* largest) {
-  __shared__ uint32_t waves[kThreads / 64];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  uint32_t most = 0;
-  for (int r = blockIdx.x * (kThreads / 64) + wave; r < rows; r += gridDim.x * (kThreads / 64)) {
-    int label;
-    if (masked && live_weight(v, r, label) == 0.0f) continue;
-    const float* row = x + r * stride;
-    int i = 4 * lane;
-    for (; i + 4 <= v.width; i += 256) {
-      const Loose four = *reinterpret_cast<const Loose*>(row + i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) most = max(most, finite_size(__uint_as_float(four[j])));
-    }
-    for (; i < v.width; ++i) most = max(most, finite_size(row[i]));  // the one lane whose four the row ends in
-  }
-  for (int m = 1; m < 64; m *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, m));
-  if (lane == 0) waves[wave] = most;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < kThreads / 64; ++i) most = max(most, waves[i]);
-    if (most) atomicMax(largest, most);
+    *largest = most;
   }
 }
 
 // ---- packed copies ---------------------------------------------------------------------------
 // Rows of an array as the products read them: `columns` elements to a row, a multiple of 64, zeros behind `width`; binary32
-// in two parts; rows without a weight as zeros if `masked`.
+// in three parts; rows without a weight as zeros if `masked`.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void pack_kernel(const VocabArgs v, const T* x, int64_t stride, int rows, bool masked, const uint32_t* largest,
+__global__ __launch_bounds__(kThreads) void pack_kernel(const VocabArgs v, const T* x, int64_t stride, int rows, bool masked,
                                                         typename Inner<T>::E* out, int columns, int64_t plane) {
   using E = typename Inner<T>::E;
   const int pieces = columns / 8;
   const int64_t total = (int64_t)rows * pieces;
-  const float scale = Inner<T>::kParts == 2 ? scale_of(*largest) : 1.0f;
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
     const int row = (int)(i / pieces), column = (int)(i % pieces) * 8;
     int label;
@@ -152,8 +129,8 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const VocabArgs v, const
       typename Matrix<E>::Fragment part;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if (p == 0) value[j] = dead ? 0.0f : value[j] * scale;
-        part[j] = (E)value[j];
+        if (p == 0) value[j] = dead ? 0.0f : value[j];
+        part[j] = (E)(p + 1 < Inner<T>::kParts ? cut(value[j]) : value[j]);
         value[j] -= (float)part[j];
       }
       *reinterpret_cast<Words4*>(out + p * plane + (int64_t)row * columns + column) = __builtin_bit_cast(Words4, part);
@@ -170,18 +147,15 @@ __device__ __forceinline__ float shift_of(float top) { return top == -INFINITY ?
 // finite number there would scale rows of very negative logits away.
 template <typename T, typename S>
 __global__ __launch_bounds__(S::kThreads) void statistics_kernel(const VocabArgs v, Operand hidden, Operand weight, int depth, int first, int columns,
-                                                                 const uint32_t* largest, float2* parts, float* at_label) {
-  constexpr int kParts = Inner<T>::kParts;
+                                                                 float2* parts, float* at_label) {
   __shared__ float2 joined[S::kWavesN][S::kM];
   int tile_m, tile_n;
   tile_of(blockIdx.x, (v.rows + S::kM - 1) / S::kM, (columns + S::kN - 1) / S::kN, tile_m, tile_n);
   const int m0 = tile_m * S::kM, n0 = tile_n * S::kN;
   Sums z[S::kBlocksM][S::kBlocksN];
-  multiply_tile<typename Inner<T>::E, S, false, false, kParts>(z, hidden, weight, m0, n0, 0, depth);
+  multiply_tile<typename Inner<T>::E, S, false, false, Inner<T>::kParts>(z, hidden, weight, m0, n0, 0, depth);
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int wave_m = wave / S::kWavesN * (S::kBlocksM * 32), wave_n = wave % S::kWavesN * (S::kBlocksN * 32);
-  const float unscale_hidden = kParts == 2 ? unscale_of(largest[kOfHidden]) : 1.0f;
-  const float unscale_weight = kParts == 2 ? unscale_of(largest[kOfWeight]) : 1.0f;
 #pragma unroll
   for (int i = 0; i < S::kBlocksM; ++i) {
     const int row = wave_m + 32 * i + (lane & 31);
@@ -193,7 +167,6 @@ __global__ __launch_bounds__(S::kThreads) void statistics_kernel(const VocabArgs
       for (int e = 0; e < 16; ++e) {
         const int column = wave_n + 32 * j + 8 * (e / 4) + 4 * (lane >> 5) + e % 4;
         float x = z[i][j][e];
-        if constexpr (kParts == 2) x = x * unscale_hidden * unscale_weight;
         if (n0 + column >= columns) x = -INFINITY;
         else if (column == label) at_label[m0 + row] = x;
         top = fmaxf(top, x);
@@ -263,9 +236,7 @@ __global__ __launch_bounds__(S::kThreads) void shares_kernel(const VocabArgs v, 
   __shared__ __align__(16) E staged[S::kWaves][32 * kBlockPitch];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int wave_m = wave / S::kWavesN * (S::kBlocksM * 32), wave_n = wave % S::kWavesN * (S::kBlocksN * 32);
-  const float unscale_hidden = kParts == 2 ? unscale_of(largest[kOfHidden]) : 1.0f;
-  const float unscale_weight = kParts == 2 ? unscale_of(largest[kOfWeight]) : 1.0f;
-  const float scale = __is_same(E, _Float16) ? shares_scale(largest[kOfShares]) : 1.0f;
+  const float scale = __is_same(T, _Float16) ? shares_scale(*largest) : 1.0f;
 #pragma unroll
   for (int i = 0; i < S::kBlocksM; ++i) {
     const int row = m0 + wave_m + 32 * i + (lane & 31);
@@ -280,20 +251,21 @@ __global__ __launch_bounds__(S::kThreads) void shares_kernel(const VocabArgs v, 
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int column = n0 + wave_n + 32 * j + 8 * (e / 4) + 4 * (lane >> 5) + e % 4;
-        float y = z[i][j][e];
-        if constexpr (kParts == 2) y = y * unscale_hidden * unscale_weight;
-        float p = __builtin_amdgcn_exp2f((y - lse) * 1.44269504f);
+        float p = __builtin_amdgcn_exp2f((z[i][j][e] - lse) * 1.44269504f);
         if (first + column == label) p -= 1.0f;
         x[e] = w == 0.0f || column >= columns ? 0.0f : p * w;
       }
       E* to = shares + (int64_t)(m0 + wave_m + 32 * i) * stride + n0 + wave_n + 32 * j;
       const auto put = [&](int row, int column, Words4 eight) { *reinterpret_cast<Words4*>(to + row * stride + column) = eight; };
-      store_block(staged[wave], x, lane, put);
-      if constexpr (kParts == 2) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] -= (float)(E)x[e];
-        to += plane;
-        store_block(staged[wave], x, lane, put);
+      for (int part = 0; part < kParts; ++part, to += plane) {
+        float y[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          y[e] = part + 1 < kParts ? cut(x[e]) : x[e];
+          x[e] -= y[e];
+        }
+        store_block(staged[wave], y, lane, put);
       }
     }
   }
@@ -336,8 +308,7 @@ __global__ __launch_bounds__(S::kThreads) void dhidden_kernel(const VocabArgs v,
 template <typename T>
 __global__ __launch_bounds__(kThreads) void finish_kernel(const VocabArgs v, const float* total, int parts, const uint32_t* largest) {
   const int64_t pitch = (v.width + 3) / 4 * 4, size = v.rows * pitch;
-  const float unscale_shares = __is_same(typename Inner<T>::E, _Float16) ? shares_unscale(largest[kOfShares]) : 1.0f;
-  const float unscale_weight = Inner<T>::kParts == 2 ? unscale_of(largest[kOfWeight]) : 1.0f;
+  const float unscale = __is_same(T, _Float16) ? shares_unscale(*largest) : 1.0f;
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < size / 4; i += (int64_t)gridDim.x * kThreads) {
     const int64_t row = i / (pitch / 4);
     const int column = (int)(i % (pitch / 4)) * 4;
@@ -349,7 +320,7 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(const VocabArgs v, con
     T* to = static_cast<T*>(v.dhidden) + row * v.dhidden_stride + column;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (column + j < v.width) to[j] = from_float<T>(x[j] * unscale_shares * unscale_weight);
+      if (column + j < v.width) to[j] = from_float<T>(x[j] * unscale);
   }
 }
 
@@ -362,8 +333,7 @@ __global__ __launch_bounds__(S::kThreads) void dweight_kernel(const VocabArgs v,
   multiply_tile<typename Inner<T>::E, S, true, true, Inner<T>::kParts>(x, shares, hidden, m0, n0, 0, (v.rows + kDepth - 1) / kDepth * kDepth);
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int wave_m = wave / S::kWavesN * (S::kBlocksM * 32), wave_n = wave % S::kWavesN * (S::kBlocksN * 32);
-  const float unscale_shares = __is_same(typename Inner<T>::E, _Float16) ? shares_unscale(largest[kOfShares]) : 1.0f;
-  const float unscale_hidden = Inner<T>::kParts == 2 ? unscale_of(largest[kOfHidden]) : 1.0f;
+  const float unscale = __is_same(T, _Float16) ? shares_unscale(*largest) : 1.0f;
   __shared__ __align__(16) T staged[sizeof(T) == 2 ? S::kWaves : 1][sizeof(T) == 2 ? 32 * kBlockPitch : 8];
 #pragma unroll
   for (int i = 0; i < S::kBlocksM; ++i)
@@ -373,7 +343,7 @@ __global__ __launch_bounds__(S::kThreads) void dweight_kernel(const VocabArgs v,
       T* to = static_cast<T*>(v.dweight) + (int64_t)(first + row0) * v.dweight_stride + column0;
       float y[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) y[e] = x[i][j][e] * unscale_shares * unscale_hidden;
+      for (int e = 0; e < 16; ++e) y[e] = x[i][j][e] * unscale;
       if constexpr (sizeof(T) == 2) {
         store_block(staged[wave], y, lane, [&](int row, int column, Words4 eight) {
           const int left = v.width - column0 - column;
@@ -406,7 +376,7 @@ __global__ __launch_bounds__(S::kThreads) void dweight_kernel(const VocabArgs v,
 }
 
 // ---- host ------------------------------------------------------------------------------------
-int parts_of(int32_t dtype) { return dtype == DGC_F32 ? 2 : 1; }
+int parts_of(int32_t dtype) { return dtype == DGC_F32 ? Inner<float>::kParts : 1; }
 
 // Where things lie in the workspace; sizes that do not fall when there are more rows.
 struct Layout {
@@ -426,7 +396,7 @@ struct Layout {
       at += whole(n);
       return here;
     };
-    largest = take(kScales * 4);
+    largest = take(4);
     hidden = take((size_t)rows * columns * 2 * p);
     weight = take((size_t)piece_packed * columns * 2 * p);
     if (backward) {
@@ -446,24 +416,26 @@ enum Shape { kLarge, kMiddle, kSmall };
 
 // The largest shape whose tiles are enough for most of the device's 256 compute units; small ones take four to a unit.  A tile
 // of 256 x 256 reads half as much for a product as four of 128 x 128: 4096 x 8192 x 2048 takes 116 to 133 us in large tiles
-// (dweight, shares), 4096 x 2048 x 8192, which has only 128 of them, 149 in middle ones (dhidden).
-Shape shape_of(int64_t m, int64_t n) {
+// (dweight, shares), 4096 x 2048 x 8192, which has only 128 of them, 149 in middle ones (dhidden).  Of operands in three parts
+// LDS has no room for large ones.
+Shape shape_of(int parts, int64_t m, int64_t n) {
   auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
-  return tiles(256) >= 200 ? kLarge : tiles(128) >= 200 ? kMiddle : kSmall;
+  return parts == 1 && tiles(256) >= 200 ? kLarge : tiles(128) >= 200 ? kMiddle : kSmall;
 }
 
 // The same for sums over the vocabulary, which can be split into parts: the largest shape whose tiles fill the device in
 // as many parts as there is room for.
-Shape dhidden_shape(int64_t rows, int64_t width) {
-  const int64_t parts = Layout::splits_at_most(rows);
-  auto groups = [&](int64_t side) { return ((rows + side - 1) / side) * ((width + side - 1) / side) * parts; };
-  return rows > 128 && groups(256) >= 200 ? kLarge : rows > 64 && groups(128) >= 300 ? kMiddle : kSmall;
+Shape dhidden_shape(int parts, int64_t rows, int64_t width) {
+  const int64_t splits = Layout::splits_at_most(rows);
+  auto groups = [&](int64_t side) { return ((rows + side - 1) / side) * ((width + side - 1) / side) * splits; };
+  return parts == 1 && rows > 128 && groups(256) >= 200 ? kLarge : rows > 64 && groups(128) >= (parts == 1 ? 300 : 200) ? kMiddle : kSmall;
 }
 
-template <typename F>
+template <int PARTS, typename F>
 void with_shape(Shape s, F f) {
-  if (s == kLarge) f(Large{});
-  else if (s == kMiddle) f(Middle{});
+  if constexpr (PARTS == 1)
+    if (s == kLarge) return f(Large{});
+  if (s == kMiddle) f(std::conditional_t<PARTS == 1, Middle, Middle3>{});
   else f(Small{});
 }
 
@@ -489,41 +461,32 @@ struct Run {
   Operand as_it_lies(const void* x, int64_t stride, int first, int rows) const {
     return {static_cast<const char*>(x) + first * stride * 2, stride * 2, 0, rows, v.width * 2};
   }
-  Operand pack(const void* x, int64_t stride, int first, int rows, bool masked, int scale, size_t to) const {
+  Operand pack(const void* x, int64_t stride, int first, int rows, bool masked, size_t to) const {
     E* out = reinterpret_cast<E*>(workspace + to);
     const int64_t plane = (int64_t)rows * at.columns;
     const uint32_t groups = (uint32_t)std::min<int64_t>((rows * at.columns / 8 + kThreads - 1) / kThreads, 8192);
-    pack_kernel<T><<<groups, kThreads, 0, stream>>>(v, static_cast<const T*>(x) + first * stride, stride, rows, masked, largest + scale, out, (int)at.columns, plane);
+    pack_kernel<T><<<groups, kThreads, 0, stream>>>(v, static_cast<const T*>(x) + first * stride, stride, rows, masked, out, (int)at.columns, plane);
     return {reinterpret_cast<const char*>(out), at.columns * 2, plane * 2, rows, (int32_t)at.columns * 2};
   }
   Operand weight(int first, int rows) const {
     return direct(v.weight, v.weight_stride) ? as_it_lies(v.weight, v.weight_stride, first, rows)
-                                             : pack(v.weight, v.weight_stride, first, rows, false, kOfWeight, at.weight);
-  }
-  void scales(bool backward) const {
-    if (kParts == 2 || (backward && __is_same(E, _Float16))) weights_kernel<<<1, 1024, 0, stream>>>(v, largest);
-    if constexpr (kParts == 2) {
-      if (v.rows == 0) return;
-      largest_kernel<<<std::min((v.rows + 3) / 4, 1024), kThreads, 0, stream>>>(v, static_cast<const float*>(v.hidden), v.hidden_stride, v.rows, backward, largest + kOfHidden);
-      largest_kernel<<<std::min((v.vocab + 3) / 4, 1024), kThreads, 0, stream>>>(v, static_cast<const float*>(v.weight), v.weight_stride, v.vocab, false, largest + kOfWeight);
-    }
+                                             : pack(v.weight, v.weight_stride, first, rows, false, at.weight);
   }
 
   hipError_t forward() const {
     float2* parts = reinterpret_cast<float2*>(workspace + at.parts);
     float* at_label = reinterpret_cast<float*>(workspace + at.at_label);
-    scales(false);
     const Operand hidden = direct(v.hidden, v.hidden_stride) ? as_it_lies(v.hidden, v.hidden_stride, 0, v.rows)
-                                                             : pack(v.hidden, v.hidden_stride, 0, v.rows, false, kOfHidden, at.hidden);
+                                                             : pack(v.hidden, v.hidden_stride, 0, v.rows, false, at.hidden);
     const int piece = direct(v.weight, v.weight_stride) ? v.vocab : (int)at.piece_packed;
-    const Shape s = shape_of(v.rows, std::min(piece, v.vocab));
+    const Shape s = shape_of(kParts, v.rows, std::min(piece, v.vocab));
     int tiles = 0;
     for (int first = 0; first < v.vocab; first += piece) {
       const int columns = std::min(piece, v.vocab - first);
       const Operand w = weight(first, columns);
-      with_shape(s, [&](auto shape) {
+      with_shape<kParts>(s, [&](auto shape) {
         using S = decltype(shape);
-        statistics_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, w, v.width, first, columns, largest, parts, at_label);
+        statistics_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, w, v.width, first, columns, parts, at_label);
         tiles = (v.vocab + S::kN - 1) / S::kN;
       });
     }
@@ -534,8 +497,8 @@ struct Run {
   hipError_t backward() const {
     E* shares = reinterpret_cast<E*>(workspace + at.shares);
     float* total = reinterpret_cast<float*>(workspace + at.total);
-    scales(true);
-    const Operand hidden = v.rows > 0 ? pack(v.hidden, v.hidden_stride, 0, v.rows, true, kOfHidden, at.hidden) : Operand{};
+    if (__is_same(T, _Float16)) weights_kernel<<<1, 1024, 0, stream>>>(v, largest);
+    const Operand hidden = v.rows > 0 ? pack(v.hidden, v.hidden_stride, 0, v.rows, true, at.hidden) : Operand{};
     const int64_t rows_pad = up(v.rows, kPad);
     int64_t piece = up(v.vocab, kPad);
     if (rows_pad > 0) piece = std::min({piece, at.shares_elements / rows_pad / kPad * kPad, (int64_t)1 << 22});  // a tile's rows in a buffer's 32 bits
@@ -548,24 +511,24 @@ struct Run {
       // whole tiles of shares were written, so that a sum over them may run to the next step's end
       const Operand p{reinterpret_cast<const char*>(shares), piece * 2, plane * 2, (int32_t)rows_pad, (int32_t)piece * 2};
       if (v.rows > 0)
-        with_shape(shape_of(v.rows, columns), [&](auto shape) {
+        with_shape<kParts>(shape_of(kParts, v.rows, columns), [&](auto shape) {
           using S = decltype(shape);
           shares_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, w, v.width, first, columns, largest, shares, piece, plane);
         });
       if (v.rows > 0 && v.dhidden)
-        with_shape(dhidden_shape(v.rows, v.width), [&](auto shape) {
+        with_shape<kParts>(dhidden_shape(kParts, v.rows, v.width), [&](auto shape) {
           using S = decltype(shape);
           const uint32_t tiles = tiles_of(shape, v.rows, v.width);
           const int depth = (int)up(columns, kDepth);
           // as many parts of the sum as the device takes workgroups, of 512 terms at least
-          constexpr int kResident = S::kM == 256 ? 256 : S::kM == 128 ? 512 : 1024;
+          constexpr int kResident = S::kM == 256 ? 256 : S::kM == 128 ? (kParts == 1 ? 512 : 256) : kParts == 1 ? 1024 : 768;
           if (first == 0) parts = (int)std::max<int64_t>(1, std::min<int64_t>({Layout::splits_at_most(v.rows), (int64_t)(kResident / tiles), (int64_t)(depth / 512)}));
           const int part = (int)up((depth + parts - 1) / parts, kDepth);
           if (first == 0) parts = (depth + part - 1) / part;  // none that begins behind the end; a last piece may have some
           dhidden_kernel<T, S><<<dim3(tiles, parts), S::kThreads, 0, stream>>>(v, p, w, depth, part, first > 0, total);
         });
       if (v.dweight)
-        with_shape(shape_of(columns, v.width), [&](auto shape) {
+        with_shape<kParts>(shape_of(kParts, columns, v.width), [&](auto shape) {
           using S = decltype(shape);
           dweight_kernel<T, S><<<tiles_of(shape, columns, v.width), S::kThreads, 0, stream>>>(v, p, hidden, first, columns, largest);
         });

@@ -98,25 +98,29 @@ def attention(q, k, v, log_decay, state0, scale, lengths, do=None, dstate_last=N
 
 
 # --- vocabulary loss ----------------------------------------------------------
-def vocab_loss(hidden, weight, labels, row_weight, dtype):
+def vocab_loss(hidden, weight, labels, row_weight, dtype, alone=False):
     """{name: (value, bound)}: loss, lse, dhidden, dweight.
 
     A logit is off by 2 EPS for each of its products; a share by that, the log-sum-exp's error, the rounding of its exponent
     and of the exponential; it is rounded to the element type after its product with the row's weight; then the sums.
 
-    In binary32 every element is held as two parts of binary16 of 11 bits each, 2^-22 of it being lost at most, and the
-    product of the small parts, 2^-22 of a product, is left out: 3 * 2^-22 = 12 EPS.  Shares in binary16, one part or two, and
-    the parts of binary32 are scaled so that the array's largest is 2^14 or more, where the smallest step is 2^-24: 2^-25 /
-    2^14 = 2^-39 of the largest may be lost whatever the element is."""
+    With `alone`: what a row may be off by itself, whatever the others hold.  In binary32 every element is held as three parts
+    of bfloat16, cut off, of which nothing is lost; of the products those of the parts 1 and 2, 2 and 1, 2 and 2 are left out,
+    2 * 2^-8 * 2^-16 and less: 2 EPS.
+
+    Without: as much as two parts of binary16 are off that share a scale, which is more.  2^-22 of an element is lost at most,
+    and the product of the small parts, 2^-22 of a product, is left out: 3 * 2^-22 = 12 EPS.  Shares in binary16, one part or
+    two, and the parts of binary32 are scaled so that the array's largest is 2^14 or more, where the smallest step is 2^-24:
+    2^-25 / 2^14 = 2^-39 of the largest may be lost whatever the element is."""
     rows, vocab, width = hidden.shape[0], weight.shape[0], hidden.shape[1]
     w = np.where((labels < 0) | (labels >= vocab), 0.0, np.ones(rows) if row_weight is None else row_weight)
     y = np.where((labels < 0) | (labels >= vocab), 0, labels)
     dead = w == 0.0
     seen = np.where(dead[:, None] & ~np.isfinite(hidden), 0.0, hidden)   # counts nothing in a row without weight
     z = seen @ weight.T
-    off = (2 * width + (16 if dtype == "f32" else 4)) * EPS * (np.abs(seen) @ np.abs(weight).T)
+    off = (2 * width + ((6 if alone else 16) if dtype == "f32" else 4)) * EPS * (np.abs(seen) @ np.abs(weight).T)
     step = 2.0 ** -39
-    most = lambda x: step * np.abs(x).max(initial=0.0) if dtype == "f32" else 0.0
+    most = lambda x: step * np.abs(x).max(initial=0.0) if dtype == "f32" and not alone else 0.0
     sizes = (np.abs(seen).sum(1, keepdims=True), np.abs(weight).sum(1))
     off = off + sizes[0] * most(weight) + sizes[1] * most(seen)
     top = z.max(1, keepdims=True)
@@ -133,7 +137,7 @@ def vocab_loss(hidden, weight, labels, row_weight, dtype):
     share_off = p * (off + lse_off[:, None] + (4 + 2 * far) * EPS) + 2 * EPS * np.abs(share)
     unit = 4 * EPS if dtype == "f32" else UNIT[dtype] + 2.0 ** -24
     share_off = share_off + unit * np.abs(share)
-    if dtype != "bf16":
+    if dtype == "f16" or dtype == "f32" and not alone:
         share_off = share_off + step * (np.abs(w).max(initial=0.0) / np.where(dead, 1.0, np.abs(w)))[:, None]
     a = np.abs
     dhidden = w[:, None] * (share @ weight)

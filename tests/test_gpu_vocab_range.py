@@ -47,3 +47,63 @@ def test_logits_far_from_zero(centre, rows, vocab, dtype):
     want = L.vocab_loss(hidden, weight, labels, w, dtype)
     for name, got in run(hidden, weight, labels, w, dtype).items():
         close(got, *want[name], kind(name, dtype), name)
+
+
+def small(rows, vocab, width, dtype, seed):
+    rng = np.random.default_rng(seed)
+    hidden = rounded_inputs(rng.normal(size=(rows, width)), dtype)
+    weight = rounded_inputs(rng.normal(size=(vocab, width)) * 2.0 * width ** -0.5, dtype)
+    return hidden, weight, rng.integers(0, vocab, rows), np.full(rows, 1.0 / rows, np.float32)
+
+
+HUGE = [("f16", 6e4), ("bf16", 1e12), ("bf16", -3e38), ("f32", 1e12), ("f32", 1e30), ("f32", -3e38)]
+
+
+@pytest.mark.parametrize("dtype,huge", HUGE)
+@pytest.mark.parametrize("rows,vocab", [(20, 500), (300, 9000)])
+def test_rows_without_a_weight_hold_anything(rows, vocab, dtype, huge):
+    """Large finite numbers in rows without a label or of weight zero: the others are as they are without these rows."""
+    say(f"[vocabulary loss] {rows} x {vocab} {dtype} rows of {huge} that count nothing")
+    hidden, weight, labels, w = small(rows, vocab, 48, dtype, 3)
+    dead = np.zeros(rows, bool)
+    dead[1::7] = dead[4::7] = True
+    labels[1::7], w[4::7] = -1, 0.0
+    hidden[dead] = rounded_inputs(np.full(1, huge), dtype)
+    got = run(hidden, weight, labels, w, dtype)
+    want = L.vocab_loss(hidden[~dead], weight, labels[~dead], w[~dead], dtype, alone=True)
+    import torch
+    for name in ("lse", "loss", "dhidden"):
+        close(got[name][torch.from_numpy(~dead).cuda()], *want[name], kind(name, dtype), name)
+    close(got["dweight"], *want["dweight"], dtype, "dweight")
+    dead = torch.from_numpy(dead).cuda()
+    assert bool((got["loss"][dead] == 0).all()) and bool((got["dhidden"][dead] == 0).all())
+
+
+@pytest.mark.parametrize("dtype,huge", [("f16", 3e4), ("bf16", 1e12), ("bf16", 1e30), ("f32", 2.0 ** 20), ("f32", 1e12), ("f32", 1e30)])
+@pytest.mark.parametrize("rows,vocab", [(20, 500), (300, 9000)])
+def test_one_row_of_the_weight_far_larger(rows, vocab, dtype, huge):
+    """A row of the weight whose logits are all far below the others': its share is zero, and nothing else changes."""
+    say(f"[vocabulary loss] {rows} x {vocab} {dtype} a row of the weight of {huge}")
+    hidden, weight, labels, w = small(rows, vocab, 48, dtype, 5)
+    hidden[:, 7] = 1.0
+    weight[11] = 0.0
+    weight[11, 7] = rounded_inputs(np.full(1, -huge), dtype)[0]
+    labels[labels == 11] = 12
+    want = L.vocab_loss(hidden, weight, labels, w, dtype, alone=True)
+    for name, got in run(hidden, weight, labels, w, dtype).items():
+        close(got, *want[name], kind(name, dtype), name)
+
+
+@pytest.mark.parametrize("rows,vocab", [(40, 500), (300, 9000)])
+def test_rows_of_many_sizes(rows, vocab):
+    """Rows of hidden, rows of the weight and row weights from 2^-40 of the largest to the largest, in 32 bits: losses and
+    dhidden are as near as the row alone would be; of dweight too, each element by the rows that it is made of."""
+    say(f"[vocabulary loss] {rows} x {vocab} f32 rows of many sizes")
+    hidden, weight, labels, w = small(rows, vocab, 48, "f32", 7)
+    rng = np.random.default_rng(8)
+    hidden *= np.exp2(-rng.integers(0, 41, rows))[:, None]
+    weight *= np.exp2(-rng.integers(0, 41, vocab))[:, None]
+    w *= np.exp2(-rng.integers(0, 41, rows)).astype(np.float32)
+    want = L.vocab_loss(hidden, weight, labels, w, "f32", alone=True)
+    for name, got in run(hidden, weight, labels, w, "f32").items():
+        close(got, *want[name], "f32", name)
