@@ -810,11 +810,12 @@ class VocabularyLoss(_Plan):
         self.lib = load()
         self.rows, self.vocab, self.width, self.dtype = int(rows), int(vocab), int(width), dtype
         self._code = _dtype_code(dtype)
-        need = C.c_size_t()
-        _check(self.lib.dgc_vocab_loss_workspace_bytes(self._shape(self.rows, self.width, self.width), int(backward),
-                                                       C.byref(need)), "dgc_vocab_loss_workspace_bytes")
+        need = [C.c_size_t() for _ in range(1 + bool(backward))]      # either call may want the more
+        for of_backward, n in enumerate(need):
+            _check(self.lib.dgc_vocab_loss_workspace_bytes(self._shape(self.rows, self.width, self.width), of_backward,
+                                                           C.byref(n)), "dgc_vocab_loss_workspace_bytes")
         self._on(device)
-        self._own(int(need.value))
+        self._own(max(int(n.value) for n in need))
 
     def _shape(self, rows: int, hidden_stride: int, weight_stride: int):
         return C.byref(DgcVocab(self._code, 0, rows, self.vocab, self.width, hidden_stride, weight_stride))

@@ -107,3 +107,27 @@ def test_rows_of_many_sizes(rows, vocab):
     want = L.vocab_loss(hidden, weight, labels, w, "f32", alone=True)
     for name, got in run(hidden, weight, labels, w, "f32").items():
         close(got, *want[name], "f32", name)
+
+
+@pytest.mark.parametrize("rows,vocab,width,dtype", [(8192, 131072, 32, "bf16"), (4096, 256000, 64, "f16"), (16384, 131072, 16, "f32")])
+def test_large_plans_run_both_calls(rows, vocab, width, dtype):
+    """Shapes whose forward call wants more workspace than their backward call.  lse against torch's, in 64 bits, of some rows;
+    a row's gradient against the products of its shares."""
+    import torch
+    say(f"[vocabulary loss] {rows} x {vocab} x {width} {dtype}, one plan for both calls")
+    t, gen = dtype_of(dtype), torch.Generator(device="cuda").manual_seed(4)
+    h = torch.randn(rows, width, generator=gen, device="cuda").to(t)
+    m = (torch.randn(vocab, width, generator=gen, device="cuda") * 2.0 * width ** -0.5).to(t)
+    y = torch.randint(0, vocab, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    plan = B.VocabularyLoss(rows, vocab, width, t)
+    loss, lse = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    dh, dm = torch.empty_like(h), torch.empty_like(m)
+    plan.dgc_vocab_loss_forward(h, m, y, loss, lse)
+    plan.dgc_vocab_loss_backward(h, m, y, lse, dh, dm)
+    some = torch.tensor([0, 1, rows // 2, rows - 1])
+    hidden, weight, labels = h[some].cpu().double().numpy(), m.cpu().double().numpy(), y[some].cpu().numpy()
+    want = L.vocab_loss(hidden, weight, labels, None, dtype, alone=True)
+    close(lse[some], *want["lse"], "f32", "lse")
+    close(loss[some], *want["loss"], "f32", "loss")
+    close(dh[some], *want["dhidden"], dtype, "dhidden")
+    assert bool(torch.isfinite(dm).all())
