@@ -8,6 +8,7 @@
 // passes the type's end, and the last one is rounded: two parts leave 2^-15 of a value out, three 2^-23.  A result in 16 bits,
 // which is rounded to 2^-9 or 2^-12 at the end, is formed from two, one in 32 bits and every state from three.
 
+#include <algorithm>
 #include <type_traits>
 
 #include "dgc_device.h"
@@ -19,16 +20,29 @@ namespace {
 struct Walks {  // of one launch
   WalkArgs walk[kWalksMax];
   int32_t count;
+  uint32_t first;  // place of the launch's first workgroup
 };
 
 // Which walk a workgroup takes part in, and as which of a walk's workgroups.  Those of several walks that read the same rows
 // stand side by side, on one die (workgroups go to the eight dies in turn), so that one's rows are in its cache for the others.
 __device__ __forceinline__ int64_t place(const Walks& walks, int& walk) {
-  const uint32_t round = 8 * (uint32_t)walks.count, in = blockIdx.x % round;
+  const uint32_t at = walks.first + blockIdx.x, round = 8 * (uint32_t)walks.count, in = at % round;
   walk = (int)(in / 8);
-  return (int64_t)(blockIdx.x / round) * 8 + in % 8;
+  return (int64_t)(at / round) * 8 + in % 8;
 }
 inline uint32_t places(int64_t groups, int count) { return (uint32_t)((groups + 7) / 8 * 8 * count); }
+
+// A launch has less than 2^32 threads: workgroups beyond them, of very many sequences, are launched behind the others.
+template <int THREADS, typename... More>
+void launch_places(void (*kernel)(Walks, More...), Walks walks, uint32_t places, hipStream_t stream, More... more) {
+  constexpr uint32_t kMost = UINT32_MAX / THREADS;
+  for (uint32_t left = places; left > 0;) {
+    const uint32_t groups = std::min(left, kMost);
+    walks.first = places - left;
+    kernel<<<groups, THREADS, 0, stream>>>(walks, more...);
+    left -= groups;
+  }
+}
 
 // ---- steps -------------------------------------------------------------------------------------
 constexpr int kColumns = 32;  // columns of the state to a workgroup at least
@@ -667,7 +681,7 @@ void launch_chunks(const Walks& walks, int count, const Slots& slots, hipStream_
   for (int i = 0; i < count; ++i) dc = std::max(dc, walks.walk[i].dc);
   const uint32_t grid = places(slots.count * walks.walk[0].heads * ((dc + 32 * made.waves - 1) / (32 * made.waves)), count);
   auto go = [&](auto rows, auto waves, auto narrow) {
-    walk_chunks_kernel<T, decltype(rows)::value, decltype(waves)::value, OUT, decltype(narrow)::value><<<grid, 64 * decltype(waves)::value, 0, stream>>>(walks, slots);
+    launch_places<64 * decltype(waves)::value>(walk_chunks_kernel<T, decltype(rows)::value, decltype(waves)::value, OUT, decltype(narrow)::value>, walks, grid, stream, slots);
   };
   auto with_waves = [&](auto rows) {
     if (made.waves == 1) go(rows, std::integral_constant<int, 1>(), std::false_type());
@@ -694,7 +708,7 @@ void launch_steps(const Walks& walks, int count, hipStream_t stream) {
   const int64_t heads = walks.walk[0].sequences * walks.walk[0].heads;
   auto go = [&](auto columns, auto held) {
     constexpr int kWide = decltype(columns)::value;
-    walk_steps_kernel<T, kWide, decltype(held)::value><<<places(heads * ((most + kWide - 1) / kWide), count), kThreads, 0, stream>>>(walks);
+    launch_places<kThreads>(walk_steps_kernel<T, kWide, decltype(held)::value>, walks, places(heads * ((most + kWide - 1) / kWide), count), stream);
   };
   if (least > 64 && rows <= 64) go(std::integral_constant<int, 128>(), std::integral_constant<int, 8>());
   else if (least > 64 && rows <= 128) go(std::integral_constant<int, 128>(), std::integral_constant<int, 16>());

@@ -1,0 +1,58 @@
+"""The layers of models with matrix states where a call has more threads than one launch may have, 2^32: the same results at
+both sides of the seams, and nothing left out.  Run with `-m gpu` on an MI355X."""
+
+import numpy as np
+import pytest
+
+from paper_1712_01887_amd import binding as B
+from tests import layers_reference as L
+from tests.parity import say
+from tests.test_gpu_rotary import close, dtype_of
+
+pytestmark = pytest.mark.gpu
+
+
+def room(gib):
+    import torch
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < gib << 30:
+        pytest.skip(f"{gib} GiB of device memory wanted")
+
+
+@pytest.mark.parametrize("length,train", [(1, False), (2, True), (5, True)])
+def test_attention_of_very_many_sequences(length, train):
+    """2^24 pairs of sequence and head and more, one workgroup each: step by step and by chunks."""
+    import torch
+    room(24)
+    count, heads, dk, dv, dtype = (1 << 20) + 3, 16, 4, 8, "bf16"
+    say(f"[attention] {count} sequences of {length} steps, {heads} heads of {dk} x {dv}")
+    gen, n, t = torch.Generator(device="cuda").manual_seed(length), count * length, dtype_of(dtype)
+
+    def normal(*shape, to=t):
+        x = torch.empty(*shape, dtype=to, device="cuda")
+        return x.normal_(generator=gen)
+
+    q, k, v = normal(n, heads, dk), normal(n, heads, dk), normal(n, heads, dv)
+    state0 = normal(count, heads, dk, dv, to=torch.float32)
+    rates = torch.full((heads,), -0.1, device="cuda")
+    plan = B.LinearAttention(count, length, heads, dk, dv, t, scale=0.5, backward=train)
+    out = dict(o=torch.full_like(v, float("nan")), state_last=torch.full_like(state0, float("nan")))
+    plan.dgc_linear_attention_forward(q, k, v, rates, state0, out["o"], out["state_last"])
+    do = flow = None
+    if train:
+        do, flow = normal(n, heads, dv), normal(count, heads, dk, dv, to=torch.float32)
+        for name, x in (("dq", q), ("dk", k), ("dv", v), ("dstate0", state0)):
+            out[name] = torch.full_like(x, float("nan"))
+        plan.dgc_linear_attention_backward(q, k, v, rates, state0, do, flow, out["dq"], out["dk"], out["dv"], out["dstate0"])
+    # (2^24 - 1) workgroups of one, two or three walks to a launch, of 16 sequences' heads each
+    seams = [(1 << 20) * i // walks for walks in (1, 2, 3) for i in range(1, walks + 1)]
+    some = sorted({min(max(s + d, 0), count - 1) for s in [0, count - 1] + seams for d in (-2, -1, 0, 1, 2)})
+    at = torch.tensor(some, device="cuda")
+    rows = (at[:, None] * length + torch.arange(length, device="cuda")).flatten()
+    host = lambda x, which: None if x is None else x[which].cpu().double().numpy()
+    want = L.attention(host(q, rows), host(k, rows), host(v, rows), rates.cpu().numpy(), host(state0, at), 0.5,
+                       [length] * len(some), host(do, rows), host(flow, at), dtype)
+    for name, x in out.items():
+        state = "state" in name
+        close(x[at if state else rows], *want[name], "f32" if state else dtype, name)
+        assert all(bool(torch.isfinite(part).all()) for part in x.split(1 << 18)), name
