@@ -3,6 +3,8 @@
 // Bound by memory: every element is read and written once.  65536 rows of 32 heads of 128 in bfloat16, 1074 MB, take 264 us,
 // 4.1 TB/s; with a thread to a pair, which forms its angle for every head, they took 552.
 
+#include <algorithm>
+
 #include "dgc_layers.h"
 
 namespace dgc {
@@ -133,7 +135,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, in
 }
 
 template <typename T>
-hipError_t launch(const RotaryArgs& a, hipStream_t stream) {
+void launch_rows(const RotaryArgs& a, hipStream_t stream) {
   constexpr int N = kElements<T>;
   const int turned = ((a.half ? a.rotary_dim / 2 : a.rotary_dim) + N - 1) / N, pieces = turned + (a.head_dim - a.rotary_dim + N - 1) / N;
   int heads = 0;
@@ -144,6 +146,23 @@ hipError_t launch(const RotaryArgs& a, hipStream_t stream) {
   const dim3 grid((uint32_t)groups, (uint32_t)((heads + group - 1) / group));
   if (a.half) rotary_kernel<T, true><<<grid, kThreads, 0, stream>>>(a, pieces, turned, group);
   else rotary_kernel<T, false><<<grid, kThreads, 0, stream>>>(a, pieces, turned, group);
+}
+
+// A launch has less than 2^32 threads, a row up to DGC_HEAD_MAX of them: rows beyond that are launched behind the others.
+template <typename T>
+hipError_t launch(const RotaryArgs& all, hipStream_t stream) {
+  constexpr int32_t kMost = (1 << 24) - 1;
+  static_assert((int64_t)kMost * DGC_HEAD_MAX + kThreads - 1 <= UINT32_MAX, "threads of a launch");
+  RotaryArgs a = all;
+  for (int32_t left = all.rows; left > 0; left -= a.rows) {
+    a.rows = std::min(left, kMost);
+    launch_rows<T>(a, stream);
+    a.positions += a.rows;
+    for (int i = 0; i < a.count; ++i) {
+      a.x[i].data = static_cast<T*>(a.x[i].data) + a.rows * a.x[i].row_stride;
+      a.out[i].data = static_cast<T*>(a.out[i].data) + a.rows * a.out[i].row_stride;
+    }
+  }
   return hipGetLastError();
 }
 

@@ -56,3 +56,27 @@ def test_attention_of_very_many_sequences(length, train):
         state = "state" in name
         close(x[at if state else rows], *want[name], "f32" if state else dtype, name)
         assert all(bool(torch.isfinite(part).all()) for part in x.split(1 << 18)), name
+
+
+@pytest.mark.parametrize("rows,dim,heads,dtype,gib", [((1 << 25) + 5, 8, (2, 1), "f32", 8), ((1 << 31) - 1, 3, (1,), "bf16", 36)])
+def test_rotary_of_very_many_rows(rows, dim, heads, dtype, gib):
+    """More rows than a launch takes; 2^31 - 1 of them in two pieces each are 2^32 threads.  All heads of all rows share a vector."""
+    import torch
+    room(gib)
+    say(f"[rotary] {rows} rows of {heads} heads of {dim} {dtype}")
+    turned, t = dim // 2 * 2, dtype_of(dtype)
+    rng = np.random.default_rng(1)
+    one = torch.from_numpy(rng.normal(size=(len(heads), dim))).to(t).cuda()
+    x = [v.expand(rows, h, dim) for v, h in zip(one, heads)]
+    out = [torch.full((rows, h, dim), float("nan"), dtype=t, device="cuda") for h in heads]
+    positions = torch.arange(rows, device="cuda")
+    plan = B.Rotary(dim, t, half=True)
+    plan.dgc_rotary(positions, x, out)
+    most = (1 << 24) - 1
+    some = sorted({min(max(s + d, 0), rows - 1) for s in [0, rows // 2, rows - 1, 1 << 30] + [most * i for i in (1, 2, 3, 127, 128)]
+                   for d in (-2, -1, 0, 1, 2)})
+    at = torch.tensor(some, device="cuda")
+    for i, h in enumerate(heads):
+        want = L.rotary(one[i].cpu().double().expand(len(some), h, dim).numpy(), np.array(some), L.frequencies(turned), True, 1.0, False)
+        close(out[i][at], *want, dtype, i)
+        assert all(bool(torch.isfinite(part).all()) for part in out[i].split(1 << 26)), i
