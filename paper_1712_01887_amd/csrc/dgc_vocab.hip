@@ -478,18 +478,18 @@ struct Run {
     float* at_label = reinterpret_cast<float*>(workspace + at.at_label);
     const Operand hidden = direct(v.hidden, v.hidden_stride) ? as_it_lies(v.hidden, v.hidden_stride, 0, v.rows)
                                                              : pack(v.hidden, v.hidden_stride, 0, v.rows, false, at.hidden);
-    const int piece = direct(v.weight, v.weight_stride) ? v.vocab : (int)at.piece_packed;
-    const Shape s = shape_of(kParts, v.rows, std::min(piece, v.vocab));
+    const int64_t whole = direct(v.weight, v.weight_stride) ? v.vocab : at.piece_packed;
     int tiles = 0;
-    for (int first = 0; first < v.vocab; first += piece) {
-      const int columns = std::min(piece, v.vocab - first);
-      const Operand w = weight(first, columns);
-      with_shape<kParts>(s, [&](auto shape) {
-        using S = decltype(shape);
-        statistics_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, w, v.width, first, columns, parts, at_label);
-        tiles = (v.vocab + S::kN - 1) / S::kN;
-      });
-    }
+    with_shape<kParts>(shape_of(kParts, v.rows, std::min<int64_t>(whole, v.vocab)), [&](auto shape) {
+      using S = decltype(shape);
+      // a launch has less than 2^32 threads (shares, a piece at a time, and gradients that fit memory, stay far below)
+      const int piece = (int)std::min<int64_t>(whole, UINT32_MAX / S::kThreads / ((v.rows + S::kM - 1) / S::kM) * S::kN);
+      for (int first = 0; first < v.vocab; first += piece) {
+        const int columns = std::min(piece, v.vocab - first);
+        statistics_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, weight(first, columns), v.width, first, columns, parts, at_label);
+      }
+      tiles = (v.vocab + S::kN - 1) / S::kN;
+    });
     join_kernel<<<(v.rows + kThreads / 8 - 1) / (kThreads / 8), kThreads, 0, stream>>>(v, parts, at_label, tiles);
     return hipGetLastError();
   }

@@ -80,3 +80,23 @@ def test_rotary_of_very_many_rows(rows, dim, heads, dtype, gib):
         want = L.rotary(one[i].cpu().double().expand(len(some), h, dim).numpy(), np.array(some), L.frequencies(turned), True, 1.0, False)
         close(out[i][at], *want, dtype, i)
         assert all(bool(torch.isfinite(part).all()) for part in out[i].split(1 << 26)), i
+
+
+def test_vocabulary_loss_of_very_many_logits():
+    """2^39 logits: a thread for each 128 of them in the largest tiles, 2^32."""
+    import torch
+    room(80)
+    rows, vocab, width, t = (1 << 24) - 1, 1 << 15, 2, torch.bfloat16
+    say(f"[vocabulary loss] {rows} x {vocab} x {width} bf16, the loss alone")
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    h = torch.randn(rows, width, generator=gen, device="cuda").to(t)
+    m = torch.randn(vocab, width, generator=gen, device="cuda").to(t)
+    y = torch.randint(-1, vocab, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    loss, lse = torch.full((rows,), float("nan"), device="cuda"), torch.full((rows,), float("nan"), device="cuda")
+    plan = B.VocabularyLoss(rows, vocab, width, t, backward=False)
+    plan.dgc_vocab_loss_forward(h, m, y, loss, lse)
+    at = torch.tensor([0, 1, 255, 256, rows // 2, rows - 257, rows - 2, rows - 1], device="cuda")
+    want = L.vocab_loss(h[at].cpu().double().numpy(), m.cpu().double().numpy(), y[at].cpu().numpy(), None, "bf16", alone=True)
+    close(lse[at], *want["lse"], "f32", "lse")
+    close(loss[at], *want["loss"], "f32", "loss")
+    assert bool(torch.isfinite(lse).all()) and bool(torch.isfinite(loss).all())
