@@ -378,10 +378,39 @@ __global__ __launch_bounds__(S::kThreads) void dweight_kernel(const VocabArgs v,
 // ---- host ------------------------------------------------------------------------------------
 int parts_of(int32_t dtype) { return dtype == DGC_F32 ? Inner<float>::kParts : 1; }
 
+enum Shape { kLarge, kMiddle, kSmall };
+constexpr int64_t kTilesLeast = 200;
+
+// The largest shape whose tiles are enough for most of the device's 256 compute units; small ones take four to a unit.  A tile
+// of 256 x 256 reads half as much for a product as four of 128 x 128: 4096 x 8192 x 2048 takes 116 to 133 us in large tiles
+// (dweight, shares), 4096 x 2048 x 8192, which has only 128 of them, 149 in middle ones (dhidden).  Of operands in three parts
+// LDS has no room for large ones.
+Shape shape_of(int parts, int64_t m, int64_t n) {
+  auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
+  return parts == 1 && tiles(256) >= kTilesLeast ? kLarge : tiles(128) >= kTilesLeast ? kMiddle : kSmall;
+}
+
+constexpr int64_t side_of(Shape s) { return s == kLarge ? 256 : s == kMiddle ? 128 : 64; }
+
+// Pairs of a row and a tile of columns that calls of up to `rows` rows leave statistics of, at most: fewer rows may go by smaller
+// tiles, and the most rows of either smaller kind are the other two candidates.  `columns`: that tiles are chosen by.
+int64_t pairs_of(int parts, int64_t rows, int64_t vocab, int64_t columns) {
+  int64_t most = 0, r = rows;
+  for (const Shape now : {kLarge, kMiddle, kSmall}) {
+    const int64_t tiles = (columns + side_of(now) - 1) / side_of(now);
+    const Shape s = shape_of(parts, r, columns);
+    if (s == now) {
+      most = std::max(most, r * ((vocab + side_of(s) - 1) / side_of(s)));
+      r = std::min(r, (kTilesLeast - 1) / tiles * side_of(now));
+    }
+  }
+  return most;
+}
+
 // Where things lie in the workspace; sizes that do not fall when there are more rows.
 struct Layout {
   int64_t columns;        // of a packed row
-  int64_t shares_elements, piece_packed;
+  int64_t shares_elements, piece_packed, pairs = 0;
   size_t largest, parts, at_label, hidden, weight, shares, total, bytes;
 
   Layout(int32_t dtype, int64_t rows, int64_t vocab, int64_t width, bool backward) {
@@ -403,7 +432,8 @@ struct Layout {
       shares = take((size_t)shares_elements * 2 * p);
       total = take((size_t)std::min(kSplitMax * rows, std::max<int64_t>(4096, rows)) * up(width, 4) * 4);
     } else {
-      parts = take((size_t)rows * ((vocab + 63) / 64) * 8);
+      pairs = std::max(pairs_of(p, rows, vocab, vocab), pairs_of(p, rows, vocab, std::min(piece_packed, vocab)));
+      parts = take((size_t)pairs * 8);
       at_label = take((size_t)rows * 4);
     }
     bytes = at;
@@ -411,17 +441,6 @@ struct Layout {
   // Parts of the sums over a piece: more than one only where there are few rows, 4096 rows in all at most.
   static int64_t splits_at_most(int64_t rows) { return rows == 0 ? 0 : std::max<int64_t>(1, std::min<int64_t>(kSplitMax, 4096 / rows)); }
 };
-
-enum Shape { kLarge, kMiddle, kSmall };
-
-// The largest shape whose tiles are enough for most of the device's 256 compute units; small ones take four to a unit.  A tile
-// of 256 x 256 reads half as much for a product as four of 128 x 128: 4096 x 8192 x 2048 takes 116 to 133 us in large tiles
-// (dweight, shares), 4096 x 2048 x 8192, which has only 128 of them, 149 in middle ones (dhidden).  Of operands in three parts
-// LDS has no room for large ones.
-Shape shape_of(int parts, int64_t m, int64_t n) {
-  auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
-  return parts == 1 && tiles(256) >= 200 ? kLarge : tiles(128) >= 200 ? kMiddle : kSmall;
-}
 
 // The same for sums over the vocabulary, which can be split into parts: the largest shape whose tiles fill the device in
 // as many parts as there is room for.
@@ -478,18 +497,20 @@ struct Run {
     float* at_label = reinterpret_cast<float*>(workspace + at.at_label);
     const Operand hidden = direct(v.hidden, v.hidden_stride) ? as_it_lies(v.hidden, v.hidden_stride, 0, v.rows)
                                                              : pack(v.hidden, v.hidden_stride, 0, v.rows, false, at.hidden);
-    const int64_t whole = direct(v.weight, v.weight_stride) ? v.vocab : at.piece_packed;
+    const int64_t at_once = direct(v.weight, v.weight_stride) ? v.vocab : at.piece_packed;
     int tiles = 0;
-    with_shape<kParts>(shape_of(kParts, v.rows, std::min<int64_t>(whole, v.vocab)), [&](auto shape) {
+    with_shape<kParts>(shape_of(kParts, v.rows, std::min<int64_t>(at_once, v.vocab)), [&](auto shape) {
       using S = decltype(shape);
+      tiles = (v.vocab + S::kN - 1) / S::kN;
+      if ((int64_t)tiles * v.rows > at.pairs) return;  // never: the layout counts them the same way
       // a launch has less than 2^32 threads (shares, a piece at a time, and gradients that fit memory, stay far below)
-      const int piece = (int)std::min<int64_t>(whole, UINT32_MAX / S::kThreads / ((v.rows + S::kM - 1) / S::kM) * S::kN);
+      const int piece = (int)std::min<int64_t>(at_once, UINT32_MAX / S::kThreads / ((v.rows + S::kM - 1) / S::kM) * S::kN);
       for (int first = 0; first < v.vocab; first += piece) {
         const int columns = std::min(piece, v.vocab - first);
         statistics_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, weight(first, columns), v.width, first, columns, parts, at_label);
       }
-      tiles = (v.vocab + S::kN - 1) / S::kN;
     });
+    if ((int64_t)tiles * v.rows > at.pairs) return hipErrorInvalidValue;
     join_kernel<<<(v.rows + kThreads / 8 - 1) / (kThreads / 8), kThreads, 0, stream>>>(v, parts, at_label, tiles);
     return hipGetLastError();
   }

@@ -194,6 +194,27 @@ def test_vocab_workspaces_grow_with_the_rows(dgc_lib):
                     before = size.value
 
 
+def test_vocab_statistics_take_what_their_tiles_leave(dgc_lib):
+    """Two floats a row and tile of 256 columns where there are many of both, beside the packed arrays; and enough of them for
+    the smaller tiles of fewer rows."""
+    def forward_bytes(rows, vocab, width, dtype):
+        size = C.c_size_t()
+        shape = vocab_shape(dtype=dtype, rows=rows, vocab=vocab, width=width, hidden_stride=width, weight_stride=width)
+        assert dgc_lib.dgc_vocab_loss_workspace_bytes(ref(shape), 0, C.byref(size)) == B.DGC_OK
+        return size.value
+
+    rows, vocab, width = 8192, 131072, 1024
+    packed = 2 * rows * width + 2 * (1 << 26)
+    assert forward_bytes(rows, vocab, width, B.DGC_BF16) <= packed + rows * (vocab // 256) * 8 + rows * 4 + 4096
+    for dtype, parts in ((B.DGC_F32, 3), (B.DGC_F16, 1), (B.DGC_BF16, 1)):
+        for vocab in (29, 300, 10000, 25600, 60000, 131072):
+            for rows in (1, 60, 64, 128, 200, 500, 1000, 1279, 1280, 5000):
+                tiles = lambda side: -(-rows // side) * -(-vocab // side)
+                side = 256 if parts == 1 and tiles(256) >= 200 else 128 if tiles(128) >= 200 else 64
+                packed = parts * 64 * 2 * rows + parts * 64 * 2 * -(-vocab // 256) * 256
+                assert forward_bytes(rows, vocab, 64, dtype) >= packed + rows * -(-vocab // side) * 8 + rows * 4
+
+
 def test_definitions_against_differences():
     """The gradients that the GPU tests compare with, against central differences of the definitions themselves."""
     rng = np.random.default_rng(4)
