@@ -711,7 +711,9 @@ dgc_status dgc_vocab_loss_forward(const dgc_vocab* shape, const void* hidden, co
  * whatever else it holds.
  *   row_weight  as above; times the incoming gradient of the rows' losses
  *   dhidden, dweight  device, of the inputs' type, either may be NULL; must not overlap an input
- * With 16-bit inputs the P_rj, and the w_r P_rj of dweight, are rounded once to that type for the second products.
+ * For the second products the shares are rounded once to a 16-bit inputs' type: in bfloat16 w_r P_rj over the largest weight, in
+ * binary16 that for dweight (steps of 2^-38 of the largest at least) and P_rj for dhidden (of 2^-38).  A row's dhidden does not
+ * depend on what other rows hold or weigh, but for this rounding.  Binary32 shares are taken apart like binary32 elements.
  */
 dgc_status dgc_vocab_loss_backward(const dgc_vocab* shape, const void* hidden, const void* weight, const int32_t* labels,
                                    const float* row_weight, const float* lse, void* dhidden, int64_t dhidden_stride,

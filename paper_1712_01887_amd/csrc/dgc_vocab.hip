@@ -51,20 +51,25 @@ using Small = Tile<64, 64, 2, 2>;
 // other reads.  700 x 10000 x 1500 in binary32, forward and backward: 615 us, with four wavefronts 656.
 using Middle3 = Tile<128, 128, 2, 4>;
 
-// ---- scale of shares in binary16 -------------------------------------------------------------
+// ---- scale of shares in 16 bits ----------------------------------------------------------------
+// w_r P_rj, which both gradients are sums over, is rounded to the 16-bit type, after a scaling by 2^14 over the largest weight:
+// where all rows weigh the same, as in a mean, a share is rounded as it is, and what is most of a label's row of dweight, a share
+// of nearly -1, hardly at all.  20 x 10000 x 1500 in bfloat16: 1.67e-3 of dhidden's norm away from 64 bits, without the scaling 1.95e-3;
+// 104 rows, 119301 x 48 in binary16: 2.1e-4 of dweight's, with a power of two 3.1e-4.  binary16 holds 2^-38 of the largest: rows
+// that weigh less are lost in dweight, where the others' terms are that much larger, but not in their own row of dhidden: that is
+// formed from P_rj 2^14, and w_r comes in at the end.  bfloat16 holds all weights, and takes the one matrix for both.
+//
 // `largest`: the bits of the largest absolute row weight.
 __device__ __forceinline__ int exponent_of(uint32_t largest) {
   const int e = (int)(largest >> 23);
   return e < 28 ? 28 : e;  // scales and their inverses stay normal
 }
-__device__ __forceinline__ float scale_of(uint32_t largest) { return __uint_as_float((uint32_t)(268 - exponent_of(largest)) << 23); }
-__device__ __forceinline__ float unscale_of(uint32_t largest) { return __uint_as_float((uint32_t)(exponent_of(largest) - 14) << 23); }
-
-// Shares times their rows' weights are scaled by 2^14 over the largest weight: where all rows weigh the same, as in a mean, a
-// share is then rounded as it is, and what is most of a label's row of dweight, a share of nearly -1, hardly at all (104 rows,
-// 119301 x 48 in binary16, scaled by a power of two: 3.1e-4 of dweight's norm away from 64 bits, the plain form 2.1e-4).
-__device__ __forceinline__ float shares_scale(uint32_t largest) { return largest < 0x0d800000u ? scale_of(largest) : 16384.0f / __uint_as_float(largest); }
-__device__ __forceinline__ float shares_unscale(uint32_t largest) { return largest < 0x0d800000u ? unscale_of(largest) : __uint_as_float(largest) * (1.0f / 16384.0f); }
+__device__ __forceinline__ float shares_scale(uint32_t largest) {
+  return largest < 0x0d800000u ? __uint_as_float((uint32_t)(268 - exponent_of(largest)) << 23) : 16384.0f / __uint_as_float(largest);
+}
+__device__ __forceinline__ float shares_unscale(uint32_t largest) {
+  return largest < 0x0d800000u ? __uint_as_float((uint32_t)(exponent_of(largest) - 14) << 23) : __uint_as_float(largest) * (1.0f / 16384.0f);
+}
 
 // A row's weight, zero where it has no label; `label` is -1 then.
 __device__ __forceinline__ float live_weight(const VocabArgs& v, int row, int& label) {
@@ -81,33 +86,44 @@ __device__ __forceinline__ uint32_t finite_size(float x) {
   return bits < 0x7f800000u ? bits : 0u;
 }
 
-// The largest row weight, one workgroup.
-__global__ __launch_bounds__(1024) void weights_kernel(const VocabArgs v, uint32_t* largest) {
-  __shared__ uint32_t waves[16];
+// The largest row weight, by one workgroup.
+__device__ void largest_weight(const VocabArgs& v, uint32_t* largest) {
+  constexpr int kAhead = 4;
+  __shared__ uint32_t waves[kThreads / 64];
   uint32_t most = 0;
-  for (int r = threadIdx.x; r < v.rows; r += 1024) {
-    int label;
-    most = max(most, finite_size(live_weight(v, r, label)));
+  for (int r = threadIdx.x; r < v.rows; r += kAhead * kThreads) {
+    float w[kAhead];
+    int label[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int row = r + i * kThreads < v.rows ? r + i * kThreads : r;
+      label[i] = v.labels[row];
+      w[i] = v.row_weight ? v.row_weight[row] : 1.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (label[i] >= 0 && label[i] < v.vocab) most = max(most, finite_size(w[i]));
   }
   for (int m = 1; m < 64; m *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, m));
   if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = most;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < 16; ++i) most = max(most, waves[i]);
-    *largest = most;
-  }
+  if (threadIdx.x != 0) return;
+  for (int i = 1; i < kThreads / 64; ++i) most = max(most, waves[i]);
+  *largest = most;
 }
 
 // ---- packed copies ---------------------------------------------------------------------------
 // Rows of an array as the products read them: `columns` elements to a row, a multiple of 64, zeros behind `width`; binary32
-// in three parts; rows without a weight as zeros if `masked`.
+// in three parts; rows without a weight as zeros if `masked`.  The last workgroup finds the largest row weight, if that is wanted.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void pack_kernel(const VocabArgs v, const T* x, int64_t stride, int rows, bool masked,
-                                                        typename Inner<T>::E* out, int columns, int64_t plane) {
+                                                        typename Inner<T>::E* out, int columns, int64_t plane, uint32_t* largest) {
   using E = typename Inner<T>::E;
+  const int groups = gridDim.x - (largest != nullptr);
+  if ((int)blockIdx.x == groups) return largest_weight(v, largest);
   const int pieces = columns / 8;
   const int64_t total = (int64_t)rows * pieces;
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)groups * kThreads) {
     const int row = (int)(i / pieces), column = (int)(i % pieces) * 8;
     int label;
     const bool dead = masked && live_weight(v, row, label) == 0.0f;
@@ -222,10 +238,12 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const VocabArgs v, const
 }
 
 // ---- gradients -------------------------------------------------------------------------------
-// w_r P_rj of a piece, rounded to what it is multiplied as: whole tiles, zeros outside the rows and the vocabulary.
+// Shares of a piece, rounded to what they are multiplied as: whole tiles, zeros outside the rows and the vocabulary.  In binary16
+// P_rj for dhidden and w_r P_rj for dweight, either of which may be null or the other one; else w_r P_rj, at `weighted`.
 template <typename T, typename S>
 __global__ __launch_bounds__(S::kThreads) void shares_kernel(const VocabArgs v, Operand hidden, Operand weight, int depth, int first, int columns,
-                                                             const uint32_t* largest, typename Inner<T>::E* shares, int64_t stride, int64_t plane) {
+                                                             const uint32_t* largest, typename Inner<T>::E* plain, typename Inner<T>::E* weighted,
+                                                             int64_t stride, int64_t plane) {
   using E = typename Inner<T>::E;
   constexpr int kParts = Inner<T>::kParts;
   int tile_m, tile_n;
@@ -236,7 +254,7 @@ __global__ __launch_bounds__(S::kThreads) void shares_kernel(const VocabArgs v, 
   __shared__ __align__(16) E staged[S::kWaves][32 * kBlockPitch];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int wave_m = wave / S::kWavesN * (S::kBlocksM * 32), wave_n = wave % S::kWavesN * (S::kBlocksN * 32);
-  const float scale = __is_same(T, _Float16) ? shares_scale(*largest) : 1.0f;
+  const float scale = sizeof(T) == 2 ? shares_scale(*largest) : 1.0f;
 #pragma unroll
   for (int i = 0; i < S::kBlocksM; ++i) {
     const int row = m0 + wave_m + 32 * i + (lane & 31);
@@ -244,28 +262,42 @@ __global__ __launch_bounds__(S::kThreads) void shares_kernel(const VocabArgs v, 
     float w = row < v.rows ? live_weight(v, row, label) : 0.0f;
     const float lse = w != 0.0f ? v.lse[row] : 0.0f;
     if (v.diag_flags && first + n0 + wave_n == 0 && lane < 32 && row < v.rows && v.labels[row] >= v.vocab) atomicOr(v.diag_flags, (uint32_t)DGC_DIAG_BAD_INDEX);
+    const bool live = w != 0.0f;
     w *= scale;
 #pragma unroll
     for (int j = 0; j < S::kBlocksN; ++j) {
-      float x[16];
+      const int64_t corner = (int64_t)(m0 + wave_m + 32 * i) * stride + n0 + wave_n + 32 * j;
+      float p[16];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int column = n0 + wave_n + 32 * j + 8 * (e / 4) + 4 * (lane >> 5) + e % 4;
-        float p = __builtin_amdgcn_exp2f((z[i][j][e] - lse) * 1.44269504f);
-        if (first + column == label) p -= 1.0f;
-        x[e] = w == 0.0f || column >= columns ? 0.0f : p * w;
+        p[e] = __builtin_amdgcn_exp2f((z[i][j][e] - lse) * 1.44269504f);
+        if (first + column == label) p[e] -= 1.0f;
+        if (!live || column >= columns) p[e] = 0.0f;
       }
-      E* to = shares + (int64_t)(m0 + wave_m + 32 * i) * stride + n0 + wave_n + 32 * j;
-      const auto put = [&](int row, int column, Words4 eight) { *reinterpret_cast<Words4*>(to + row * stride + column) = eight; };
+      auto store = [&](E* to, const float (&x)[16]) {
+        store_block(staged[wave], x, lane, [&](int row, int column, Words4 eight) { *reinterpret_cast<Words4*>(to + corner + row * stride + column) = eight; });
+      };
+      float x[16];
+      if constexpr (__is_same(T, _Float16)) {
 #pragma unroll
-      for (int part = 0; part < kParts; ++part, to += plane) {
-        float y[16];
+        for (int e = 0; e < 16; ++e) x[e] = p[e] * 16384.0f;
+        if (plain) store(plain, x);
+        if (weighted == plain) continue;
+      }
+      if (weighted) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          y[e] = part + 1 < kParts ? cut(x[e]) : x[e];
-          x[e] -= y[e];
+        for (int e = 0; e < 16; ++e) x[e] = p[e] == 0.0f ? 0.0f : p[e] * w;
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+          float y[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            y[e] = part + 1 < kParts ? cut(x[e]) : x[e];
+            x[e] -= y[e];
+          }
+          store(weighted + part * plane, y);
         }
-        store_block(staged[wave], y, lane, put);
       }
     }
   }
@@ -308,7 +340,7 @@ __global__ __launch_bounds__(S::kThreads) void dhidden_kernel(const VocabArgs v,
 template <typename T>
 __global__ __launch_bounds__(kThreads) void finish_kernel(const VocabArgs v, const float* total, int parts, const uint32_t* largest) {
   const int64_t pitch = (v.width + 3) / 4 * 4, size = v.rows * pitch;
-  const float unscale = __is_same(T, _Float16) ? shares_unscale(*largest) : 1.0f;
+  const float unscale = __is_same(T, _Float16) ? 1.0f / 16384.0f : __is_same(T, __bf16) ? shares_unscale(*largest) : 1.0f;
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < size / 4; i += (int64_t)gridDim.x * kThreads) {
     const int64_t row = i / (pitch / 4);
     const int column = (int)(i % (pitch / 4)) * 4;
@@ -317,10 +349,12 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(const VocabArgs v, con
       const float4 y = *reinterpret_cast<const float4*>(total + p * size + i * 4);
       x[0] += y.x, x[1] += y.y, x[2] += y.z, x[3] += y.w;
     }
+    int label;
+    const float w = __is_same(T, _Float16) ? live_weight(v, (int)row, label) * unscale : unscale;
     T* to = static_cast<T*>(v.dhidden) + row * v.dhidden_stride + column;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (column + j < v.width) to[j] = from_float<T>(x[j] * unscale);
+      if (column + j < v.width) to[j] = from_float<T>(x[j] * w);
   }
 }
 
@@ -333,7 +367,7 @@ __global__ __launch_bounds__(S::kThreads) void dweight_kernel(const VocabArgs v,
   multiply_tile<typename Inner<T>::E, S, true, true, Inner<T>::kParts>(x, shares, hidden, m0, n0, 0, (v.rows + kDepth - 1) / kDepth * kDepth);
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int wave_m = wave / S::kWavesN * (S::kBlocksM * 32), wave_n = wave % S::kWavesN * (S::kBlocksN * 32);
-  const float unscale = __is_same(T, _Float16) ? shares_unscale(*largest) : 1.0f;
+  const float unscale = sizeof(T) == 2 && v.rows > 0 ? shares_unscale(*largest) : 1.0f;
   __shared__ __align__(16) T staged[sizeof(T) == 2 ? S::kWaves : 1][sizeof(T) == 2 ? 32 * kBlockPitch : 8];
 #pragma unroll
   for (int i = 0; i < S::kBlocksM; ++i)
@@ -377,6 +411,7 @@ __global__ __launch_bounds__(S::kThreads) void dweight_kernel(const VocabArgs v,
 
 // ---- host ------------------------------------------------------------------------------------
 int parts_of(int32_t dtype) { return dtype == DGC_F32 ? Inner<float>::kParts : 1; }
+int planes_of_shares(int32_t dtype) { return dtype == DGC_F16 ? 2 : parts_of(dtype); }
 
 enum Shape { kLarge, kMiddle, kSmall };
 constexpr int64_t kTilesLeast = 200;
@@ -429,7 +464,7 @@ struct Layout {
     hidden = take((size_t)rows * columns * 2 * p);
     weight = take((size_t)piece_packed * columns * 2 * p);
     if (backward) {
-      shares = take((size_t)shares_elements * 2 * p);
+      shares = take((size_t)shares_elements * 2 * planes_of_shares(dtype));
       total = take((size_t)std::min(kSplitMax * rows, std::max<int64_t>(4096, rows)) * up(width, 4) * 4);
     } else {
       pairs = std::max(pairs_of(p, rows, vocab, vocab), pairs_of(p, rows, vocab, std::min(piece_packed, vocab)));
@@ -480,11 +515,11 @@ struct Run {
   Operand as_it_lies(const void* x, int64_t stride, int first, int rows) const {
     return {static_cast<const char*>(x) + first * stride * 2, stride * 2, 0, rows, v.width * 2};
   }
-  Operand pack(const void* x, int64_t stride, int first, int rows, bool masked, size_t to) const {
+  Operand pack(const void* x, int64_t stride, int first, int rows, bool masked, size_t to, uint32_t* largest_weight = nullptr) const {
     E* out = reinterpret_cast<E*>(workspace + to);
     const int64_t plane = (int64_t)rows * at.columns;
     const uint32_t groups = (uint32_t)std::min<int64_t>((rows * at.columns / 8 + kThreads - 1) / kThreads, 8192);
-    pack_kernel<T><<<groups, kThreads, 0, stream>>>(v, static_cast<const T*>(x) + first * stride, stride, rows, masked, out, (int)at.columns, plane);
+    pack_kernel<T><<<groups + (largest_weight != nullptr), kThreads, 0, stream>>>(v, static_cast<const T*>(x) + first * stride, stride, rows, masked, out, (int)at.columns, plane, largest_weight);
     return {reinterpret_cast<const char*>(out), at.columns * 2, plane * 2, rows, (int32_t)at.columns * 2};
   }
   Operand weight(int first, int rows) const {
@@ -518,23 +553,27 @@ struct Run {
   hipError_t backward() const {
     E* shares = reinterpret_cast<E*>(workspace + at.shares);
     float* total = reinterpret_cast<float*>(workspace + at.total);
-    if (__is_same(T, _Float16)) weights_kernel<<<1, 1024, 0, stream>>>(v, largest);
-    const Operand hidden = v.rows > 0 ? pack(v.hidden, v.hidden_stride, 0, v.rows, true, at.hidden) : Operand{};
+    const Operand hidden = v.rows > 0 ? pack(v.hidden, v.hidden_stride, 0, v.rows, true, at.hidden, sizeof(T) == 2 ? largest : nullptr) : Operand{};
     const int64_t rows_pad = up(v.rows, kPad);
     int64_t piece = up(v.vocab, kPad);
     if (rows_pad > 0) piece = std::min({piece, at.shares_elements / rows_pad / kPad * kPad, (int64_t)1 << 22});  // a tile's rows in a buffer's 32 bits
     if (!direct(v.weight, v.weight_stride)) piece = std::min(piece, at.piece_packed);
     const int64_t plane = rows_pad * piece;
+    // what either gradient is formed from: the same, but in binary16 where rows may weigh differently
+    const bool apart = __is_same(T, _Float16) && v.row_weight;
+    E* const for_dweight = shares + (apart && v.dhidden && v.dweight ? plane : 0);
+    E* const plain = apart && !v.dhidden ? nullptr : shares;
+    E* const weighted = apart && !v.dweight ? nullptr : for_dweight;
     int parts = 1;
     for (int first = 0; first < v.vocab; first += (int)piece) {
       const int columns = (int)std::min<int64_t>(piece, v.vocab - first);
       const Operand w = v.rows > 0 ? weight(first, columns) : Operand{};
       // whole tiles of shares were written, so that a sum over them may run to the next step's end
-      const Operand p{reinterpret_cast<const char*>(shares), piece * 2, plane * 2, (int32_t)rows_pad, (int32_t)piece * 2};
+      const auto whole_tiles = [&](const E* x) { return Operand{reinterpret_cast<const char*>(x), piece * 2, plane * 2, (int32_t)rows_pad, (int32_t)piece * 2}; };
       if (v.rows > 0)
         with_shape<kParts>(shape_of(kParts, v.rows, columns), [&](auto shape) {
           using S = decltype(shape);
-          shares_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, w, v.width, first, columns, largest, shares, piece, plane);
+          shares_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, w, v.width, first, columns, largest, plain, weighted, piece, plane);
         });
       if (v.rows > 0 && v.dhidden)
         with_shape<kParts>(dhidden_shape(kParts, v.rows, v.width), [&](auto shape) {
@@ -546,12 +585,12 @@ struct Run {
           if (first == 0) parts = (int)std::max<int64_t>(1, std::min<int64_t>({Layout::splits_at_most(v.rows), (int64_t)(kResident / tiles), (int64_t)(depth / 512)}));
           const int part = (int)up((depth + parts - 1) / parts, kDepth);
           if (first == 0) parts = (depth + part - 1) / part;  // none that begins behind the end; a last piece may have some
-          dhidden_kernel<T, S><<<dim3(tiles, parts), S::kThreads, 0, stream>>>(v, p, w, depth, part, first > 0, total);
+          dhidden_kernel<T, S><<<dim3(tiles, parts), S::kThreads, 0, stream>>>(v, whole_tiles(shares), w, depth, part, first > 0, total);
         });
       if (v.dweight)
         with_shape<kParts>(shape_of(kParts, columns, v.width), [&](auto shape) {
           using S = decltype(shape);
-          dweight_kernel<T, S><<<tiles_of(shape, columns, v.width), S::kThreads, 0, stream>>>(v, p, hidden, first, columns, largest);
+          dweight_kernel<T, S><<<tiles_of(shape, columns, v.width), S::kThreads, 0, stream>>>(v, whole_tiles(for_dweight), hidden, first, columns, largest);
         });
     }
     if (v.rows > 0 && v.dhidden) finish_kernel<T><<<(uint32_t)std::min<int64_t>(((int64_t)v.rows * up(v.width, 4) / 4 + kThreads - 1) / kThreads, 8192), kThreads, 0, stream>>>(v, total, parts, largest);

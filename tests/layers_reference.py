@@ -106,7 +106,8 @@ def vocab_loss(hidden, weight, labels, row_weight, dtype, alone=False):
 
     With `alone`: what a row may be off by itself, whatever the others hold.  In binary32 every element is held as three parts
     of bfloat16, cut off, of which nothing is lost; of the products those of the parts 1 and 2, 2 and 1, 2 and 2 are left out,
-    2 * 2^-8 * 2^-16 and less: 2 EPS.
+    2 * 2^-8 * 2^-16 and less: 2 EPS.  In binary16 a share is scaled by 2^14 for dhidden, whatever its row weighs, and for dweight
+    by 2^14 over the largest weight: 2^-39 is lost at most, of one or of the largest weight.
 
     Without: as much as two parts of binary16 are off that share a scale, which is more.  2^-22 of an element is lost at most,
     and the product of the small parts, 2^-22 of a product, is left out: 3 * 2^-22 = 12 EPS.  Shares in binary16, one part or
@@ -137,11 +138,13 @@ def vocab_loss(hidden, weight, labels, row_weight, dtype, alone=False):
     share_off = p * (off + lse_off[:, None] + (4 + 2 * far) * EPS) + 2 * EPS * np.abs(share)
     unit = 4 * EPS if dtype == "f32" else UNIT[dtype] + 2.0 ** -24
     share_off = share_off + unit * np.abs(share)
+    over = step * (np.abs(w).max(initial=0.0) / np.where(dead, 1.0, np.abs(w)))[:, None]
+    own = share_off + step if dtype == "f16" else share_off
     if dtype == "f16" or dtype == "f32" and not alone:
-        share_off = share_off + step * (np.abs(w).max(initial=0.0) / np.where(dead, 1.0, np.abs(w)))[:, None]
+        share_off = share_off + over
     a = np.abs
     dhidden = w[:, None] * (share @ weight)
-    dhidden_off = a(w)[:, None] * (share_off @ a(weight) + 2 * (vocab + 8) * EPS * (a(share) @ a(weight)) +
+    dhidden_off = a(w)[:, None] * ((own if alone else share_off) @ a(weight) + 2 * (vocab + 8) * EPS * (a(share) @ a(weight)) +
                                  a(share).sum(1, keepdims=True) * most(weight))
     h = np.where(dead[:, None], 0.0, seen)
     dweight = (share * w[:, None]).T @ h

@@ -131,3 +131,48 @@ def test_large_plans_run_both_calls(rows, vocab, width, dtype):
     close(loss[some], *want["loss"], "f32", "loss")
     close(dh[some], *want["dhidden"], dtype, "dhidden")
     assert bool(torch.isfinite(dm).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(40, 700), (300, 20000)])
+def test_row_weights_of_many_sizes(rows, vocab, dtype):
+    """Weights from 1e-8 of the largest to the largest: a row's dhidden is as near as if it were alone, also in binary16, where
+    most of its shares times its weight would be subnormal; either gradient alone is the same."""
+    import torch
+    say(f"[vocabulary loss] {rows} x {vocab} {dtype} row weights of many sizes")
+    hidden, weight, labels, _ = small(rows, vocab, 64, dtype, 9)
+    w = (65536.0 * 10.0 ** np.random.default_rng(2).uniform(-8.0, 0.0, rows)).astype(np.float32)
+    w[3::11] = 0.0
+    want = L.vocab_loss(hidden, weight, labels, w, dtype, alone=True)
+    got = run(hidden, weight, labels, w, dtype)
+    for name in got:
+        value, bound = want[name]
+        # binary16 ends at 65504: what is 65520 and more, by more than the bound, is infinite there, and what may be is not looked at
+        most = 65520.0 if kind(name, dtype) == "f16" else np.inf
+        beyond, inside = np.abs(value) - bound >= most, np.abs(value) + bound < most
+        here = got[name].cpu().double().numpy()
+        assert np.array_equal(here[beyond], np.copysign(np.inf, value[beyond])), name
+        close(got[name][torch.from_numpy(inside).cuda()], value[inside], bound[inside], kind(name, dtype), name)
+    t = dtype_of(dtype)
+    h, m = torch.from_numpy(hidden).to(t).cuda(), torch.from_numpy(weight).to(t).cuda()
+    y, row_weight = torch.from_numpy(labels.astype(np.int32)).cuda(), torch.from_numpy(w).cuda()
+    plan, one, two = B.VocabularyLoss(rows, vocab, 64, t), torch.empty_like(h), torch.empty_like(m)
+    plan.dgc_vocab_loss_backward(h, m, y, got["lse"], one, None, row_weight=row_weight)
+    plan.dgc_vocab_loss_backward(h, m, y, got["lse"], None, two, row_weight=row_weight)
+    assert torch.equal(one, got["dhidden"]) and torch.equal(two, got["dweight"])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_equal_weights_round_the_shares_themselves(dtype):
+    """A mean over 20 rows, whose weight 1 / 20 has no short form in the type: both gradients are 1 / 20 of those of weight one,
+    up to a rounding of the results (half a step each) and four of binary32."""
+    rows, vocab = 20, 10000
+    hidden, weight, labels, _ = small(rows, vocab, 96, dtype, 4)
+    size = np.float32(1.0 / rows)
+    one = run(hidden, weight, labels, None, dtype)
+    mean = run(hidden, weight, labels, np.full(rows, size), dtype)
+    for name in ("dhidden", "dweight"):
+        a, b = one[name].cpu().double().numpy() * float(size), mean[name].cpu().double().numpy()
+        unit = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8}[dtype]
+        tiny = 2.0 ** -25 * 1.05 if dtype == "f16" else 0.0
+        assert np.all(np.abs(a - b) <= (2 * unit + unit ** 2 + 2.0 ** -21) * np.abs(a) + 2 * tiny), name
