@@ -196,3 +196,21 @@ def test_captured_and_on_another_stream():
         plan.dgc_rotary(positions, [x], [want])
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,heads,key_heads,dim,turned", [(9000, 6, 2, 80, 64), (3, 6, 2, 75, 50), (70000, 1, 1, 64, 64)])
+def test_slices_of_one_projection(rows, heads, key_heads, dim, turned, dtype):
+    """q and k as parts of q | k | v, turned in place; rows enough that a thread takes all heads, and few."""
+    import torch
+    say(f"[rotary] q | k | v of {rows} x {heads} + 2 x {key_heads} x {dim} {dtype}")
+    rng = np.random.default_rng(rows)
+    values = rounded_inputs(rng.normal(size=(rows, heads + 2 * key_heads, dim)), dtype)
+    whole = torch.from_numpy(values).to(dtype_of(dtype)).cuda()
+    q, k = whole[:, :heads], whole[:, heads:heads + key_heads]
+    positions = rng.integers(0, 1 << 18, rows)
+    plan = B.Rotary(dim, dtype_of(dtype), rotary_dim=turned, half=True)
+    plan.dgc_rotary(torch.from_numpy(positions).cuda(), [q, k], [q, k])
+    want = L.rotary(values[:, :heads + key_heads], positions, L.frequencies(turned), True, 1.0, False)
+    close(whole[:, :heads + key_heads], *want, dtype, "q | k")
+    assert np.array_equal(whole[:, heads + key_heads:].cpu().double().numpy(), values[:, heads + key_heads:])
