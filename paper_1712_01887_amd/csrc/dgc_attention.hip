@@ -698,7 +698,9 @@ void launch_chunks(const Walks& walks, int count, const Slots& slots, hipStream_
 template <typename T>
 void launch_steps(const Walks& walks, int count, hipStream_t stream) {
   // 128 columns to a workgroup where all walks have more than 64 of them, and up to 128 rows: 512 bytes of a row to a wavefront's
-  // load, and a thread has 8 or 16 loads on their way (64 x 16 states of 64 x 128: 17.2 us, 3.9 TB/s; by 32 columns 22.8)
+  // load, and a thread has 8 or 16 loads on their way (64 x 16 states of 64 x 128: 17.2 us, 3.9 TB/s; by 32 columns 22.8).  Of 64
+  // columns half the threads would have none: 64 x 16 states of 64 x 64 by 32 columns 10.4 us, 3.2 TB/s, by 128 13.0; 256 x 16 30.7
+  // and 40.6
   int32_t rows = 0, least = DGC_HEAD_MAX, most = 0;
   for (int i = 0; i < count; ++i) {
     rows = std::max(rows, walks.walk[i].da);
@@ -726,12 +728,23 @@ void with_type(int32_t dtype, F f) {
 // A step that goes by itself costs a reduction and a barrier, a chunk of up to 32 some 5 us whatever it holds.
 constexpr int64_t kStepsAtMost = 4;      // of sequences that go step by step
 constexpr int64_t kWorkgroups = 512;     // that fill the device
-constexpr int64_t kSegmentLeast = 256;   // steps; a state of 128 x 128 is as many bytes as 128 rows of k and v in bfloat16
+constexpr int64_t kSegmentLeast = 128;   // steps; a state of 128 x 128 is as many bytes as 128 rows of k and v in bfloat16
+constexpr int64_t kCutLongerThan = 512;  // steps of the longest sequence
+constexpr int64_t kCutBelow = 136, kCutRaggedBelow = 256;  // workgroups without cutting, of sequences of one length and of different ones
 
-Slots slots_of(int64_t rows, int64_t sequences, int64_t max_length, int32_t heads, int32_t dims) {
+// Cutting sequences into segments fills the device and shortens the longest one's chain of chunks, and reads k and v a second time.
+// Both sides in us, cut and whole, forward / forward and backward:
+//   equal sequences of 4096 x 128 x 128 bfloat16   64 workgroups 132 and 300 / 470 and 599, 128: 243 and 301 / 843 and 751,
+//                                                  144: 327 and 302 / 1033 and 786, 192: 402 and 303 / 1283 and 1032
+//   different ones, up to 4000 x 64 x 64 binary16  160: 176 and 355 / 556 and 736, 256: 323 and 358 / 974 and 1022,
+//                  up to 1500                      384: 216 and 169 / 627 and 492
+//   short ones                                     8 x 300 x 12 x 64 x 64 bfloat16 36 and 28 / 81 and 62, 2 x 512 x 16 x 128 x 128 43 and 47 / 99 and 94
+//   segments of 128, and of 256 at least           1024 x 16 x 128 x 128 bfloat16 40 and 51 / 90 and 105, 4096 x 4 x 64 x 64 30 and 39 / 65 and 79;
+//                  of 64                           35 / 96 and 28 / 64
+Slots slots_of(int64_t rows, int64_t sequences, int64_t max_length, int32_t heads, int32_t dims, bool ragged) {
   Slots s{sequences, 0};
   const int64_t tiles = (dims + 127) / 128, whole = sequences * heads * tiles;
-  if (max_length <= 2 * kSegmentLeast || whole >= kWorkgroups / 2) return s;
+  if (max_length <= kCutLongerThan || whole >= (ragged ? kCutRaggedBelow : kCutBelow)) return s;
   // as many segments as fill the device, of kSegmentLeast steps at least
   const int64_t wanted = std::max<int64_t>(1, kWorkgroups / (heads * tiles));
   s.steps = std::max(kSegmentLeast, (rows / wanted + kChunk - 1) / kChunk * kChunk);
@@ -740,7 +753,7 @@ Slots slots_of(int64_t rows, int64_t sequences, int64_t max_length, int32_t head
   return s;
 }
 
-Slots slots_of(const WalkArgs& w) { return slots_of(w.rows, w.sequences, w.max_length, w.heads, std::max(w.da, w.dc)); }
+Slots slots_of(const WalkArgs& w) { return slots_of(w.rows, w.sequences, w.max_length, w.heads, std::max(w.da, w.dc), w.row_offsets != nullptr); }
 
 // Calls f(walks, count) for the walks that one kernel can take together.
 template <typename F>
@@ -766,8 +779,8 @@ int64_t walk_workgroups(int64_t sequences, int32_t heads, int32_t dc) {
   return sequences * heads * ((dc + kColumns - 1) / kColumns);
 }
 
-size_t walk_workspace_bytes(int64_t rows, int64_t sequences, int64_t max_length, int32_t heads, int32_t da, int32_t dc) {
-  const Slots s = slots_of(rows, sequences, max_length, heads, std::max(da, dc));
+size_t walk_workspace_bytes(int64_t rows, int64_t sequences, int64_t max_length, int32_t heads, int32_t da, int32_t dc, bool ragged) {
+  const Slots s = slots_of(rows, sequences, max_length, heads, std::max(da, dc), ragged);
   return s.steps == 0 ? 0 : ((size_t)(s.count + 1) * heads * da * dc * 4 + 255) / 256 * 256;
 }
 

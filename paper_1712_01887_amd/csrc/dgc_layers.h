@@ -60,7 +60,7 @@ constexpr int kWalksMax = 3;
 // launch_walks reads, from `states`, as they lie with a walk's own state_a and state_c.
 hipError_t launch_walk_states(const WalkArgs* w, int count, int32_t dtype, hipStream_t stream);
 hipError_t launch_walks(const WalkArgs* w, int count, int32_t dtype, hipStream_t stream);
-size_t walk_workspace_bytes(int64_t rows, int64_t sequences, int64_t max_length, int32_t heads, int32_t da, int32_t dc);
+size_t walk_workspace_bytes(int64_t rows, int64_t sequences, int64_t max_length, int32_t heads, int32_t da, int32_t dc, bool ragged);
 int64_t walk_workgroups(int64_t sequences, int32_t heads, int32_t dc);
 hipError_t launch_vocab_forward(const VocabArgs& a, void* workspace, int32_t dtype, hipStream_t stream);
 hipError_t launch_vocab_backward(const VocabArgs& a, void* workspace, int32_t dtype, hipStream_t stream);

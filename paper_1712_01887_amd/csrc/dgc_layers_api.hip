@@ -154,7 +154,7 @@ dgc_status dgc_linear_attention_workspace_bytes(const dgc_attention* shape, int3
   const dgc_status st = check_attention(shape);
   if (st != DGC_OK) return st;
   if (!bytes || (backward != 0 && backward != 1)) return DGC_ERR_INVALID_ARG;
-  *bytes = walk_workspace_bytes(shape->rows, shape->sequences, shape->max_length, shape->heads, shape->key_dim, shape->value_dim) * (backward ? 2 : 1);
+  *bytes = walk_workspace_bytes(shape->rows, shape->sequences, shape->max_length, shape->heads, shape->key_dim, shape->value_dim, shape->row_offsets != nullptr) * (backward ? 2 : 1);
   return DGC_OK;
 }
 
