@@ -227,29 +227,42 @@ def cpu_baseline(name, cfg_kw, n_workers, budget_s=12.0):
 
 # ---------------------------------------------------------------------------
 # HBM traffic of the streaming kernel: read from the rocprofv3 summary under profiles/, and
-# only if that summary was made from the kernel sources as they are now
+# only if that summary was made from the kernel's sources as they are now
 # ---------------------------------------------------------------------------
-def source_hash() -> str:
+CSRC = os.path.join(ROOT, "paper_1712_01887_amd", "csrc")
+
+
+def source_hash(names=None) -> str:
+    """Of the named kernel sources, or of all of them."""
     h = hashlib.sha256()
-    csrc = os.path.join(ROOT, "paper_1712_01887_amd", "csrc")
-    for name in sorted(os.listdir(csrc)):
+    for name in sorted(os.listdir(CSRC)) if names is None else names:
         if name.endswith((".hip", ".h")):
-            h.update(open(os.path.join(csrc, name), "rb").read())
+            h.update(open(os.path.join(CSRC, name), "rb").read())
     return h.hexdigest()[:16]
+
+
+def stream_sources() -> list:
+    """The streaming kernel's file and the headers beside it that it includes, one way or another."""
+    names = ["dgc_compress.hip"]
+    for name in names:                                                 # grows while it is walked
+        for other in re.findall(r'^#include "([^"]+)"', open(os.path.join(CSRC, name)).read(), re.M):
+            if other not in names and os.path.exists(os.path.join(CSRC, other)):
+                names.append(other)
+    return sorted(names)
 
 
 def measured_traffic(workload: str):
     """Bytes one stream_kernel launch moved through HBM according to
     profiles/stream_kernel_<workload>_hbm_traffic.txt, or None when there is no such summary or
-    it was made from other kernel sources (its `source_hash` line)."""
+    it was made from other sources of that kernel (its `stream_source_hash` line)."""
     path = os.path.join(ROOT, "profiles", f"stream_kernel_{workload}_hbm_traffic.txt")
     try:
         text = open(path).read()
     except OSError:
         return None
-    m_hash = re.search(r"^source_hash:\s*([0-9a-f]+)", text, re.M)
+    m_hash = re.search(r"^stream_source_hash:\s*([0-9a-f]+)", text, re.M)
     m_bytes = re.search(r"^stream_kernel traffic per launch = ([0-9,]+) bytes", text, re.M)
-    if not m_hash or not m_bytes or m_hash.group(1) != source_hash():
+    if not m_hash or not m_bytes or m_hash.group(1) != source_hash(stream_sources()):
         return None
     return int(m_bytes.group(1).replace(",", ""))
 
