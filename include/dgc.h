@@ -611,6 +611,7 @@ dgc_status dgc_rotary_frequencies(int32_t rotary_dim, double base, double factor
  *   magnitude    m, finite
  *   count, heads 1 .. DGC_ROTARY_MAX arrays (queries and keys, say) and the heads of each (1 .. 65535)
  *   x, out       host, `count` descriptions of device arrays; out[i] may be x[i], address and strides, and overlaps no other
+ *                (one that begins where another x or out does is refused)
  * Errors: INVALID_ARG, ALIGNMENT, CAPACITY (rows, heads, or strides whose products with rows or heads pass 2^60), HIP.
  */
 dgc_status dgc_rotary(const dgc_rotary_shape* shape, const int64_t* positions, const uint64_t* frequencies,

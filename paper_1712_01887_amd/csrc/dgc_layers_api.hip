@@ -138,6 +138,9 @@ dgc_status dgc_rotary(const dgc_rotary_shape* s, const int64_t* positions, const
     a.heads[i] = heads[i];
   }
   if (s->rows == 0) return DGC_OK;
+  for (int32_t i = 0; i < count; ++i)  // an array that is turned twice, or read while it is turned
+    for (int32_t j = 0; j < count; ++j)
+      if (i != j && (out[i].data == out[j].data || out[i].data == x[j].data)) return DGC_ERR_INVALID_ARG;
   a.count = count;
   a.rows = (int32_t)s->rows;
   a.head_dim = s->head_dim;

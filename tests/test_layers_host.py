@@ -253,3 +253,14 @@ def test_definitions_against_differences():
             down = value()
             y[name][at] = keep
             assert abs((up - down) / (2 * step) - got["d" + name][0][at]) < 1e-7, (name, at)
+
+
+def test_rotary_refuses_an_array_twice(dgc_lib):
+    """An array that is listed twice would be turned by two workgroups at once."""
+    def call(x, out, rows=10):
+        return rotary(dgc_lib, rotary_shape(rows=rows), count=2, heads=(C.c_int32 * 2)(8, 8), x=(B.DgcHeads * 2)(*x), out=(B.DgcHeads * 2)(*out))
+
+    a, b, c = heads(P), heads(2 * P), heads(3 * P)
+    assert call((a, a), (b, b)) == BAD and call((a, a), (a, a)) == BAD
+    assert call((a, b), (b, c)) == BAD and call((a, b), (c, a)) == BAD and call((a, b), (a, a)) == BAD
+    assert call((a, a), (b, b), rows=0) == B.DGC_OK
