@@ -664,7 +664,8 @@ dgc_status dgc_linear_attention_forward(const dgc_attention* shape, const dgc_he
  *   dq_t = scale S_t do_t,   dk_t = G_t v_t,   dv_t = G_t^T k_t,   dstate0 = d G_0
  * The states are formed again from the inputs.  A head that shares its vectors with others (a stride of 0) has gradients of
  * its own: their sum is the shared vector's.
- *   dstate_last  device, float[as state0], or NULL for zeros;  dstate0 device, float[same], or NULL; may be dstate_last
+ *   dstate_last  device, float[as state0], or NULL for zeros;  dstate0 device, float[same], or NULL; may be dstate_last,
+ *                and not state0
  *   dq, dk, dv   must not overlap an input or each other
  */
 dgc_status dgc_linear_attention_backward(const dgc_attention* shape, const dgc_heads* q, const dgc_heads* k,

@@ -227,6 +227,7 @@ dgc_status dgc_linear_attention_backward(const dgc_attention* s, const dgc_heads
         if (x->data == y->data) return DGC_ERR_INVALID_ARG;
     if (dq->data == dk->data || dq->data == dv->data || dk->data == dv->data) return DGC_ERR_INVALID_ARG;
   }
+  if (dstate0 && dstate0 == state0) return DGC_ERR_INVALID_ARG;  // which dq's walk reads while dv's leaves dstate0
   if (!aligned_to(log_decay, 4) || !aligned_to(state0, 4) || !aligned_to(dstate_last, 4) || !aligned_to(dstate0, 4)) return DGC_ERR_ALIGNMENT;
   size_t need = 0;
   dgc_linear_attention_workspace_bytes(s, 1, &need);

@@ -264,3 +264,9 @@ def test_rotary_refuses_an_array_twice(dgc_lib):
     assert call((a, a), (b, b)) == BAD and call((a, a), (a, a)) == BAD
     assert call((a, b), (b, c)) == BAD and call((a, b), (c, a)) == BAD and call((a, b), (a, a)) == BAD
     assert call((a, a), (b, b), rows=0) == B.DGC_OK
+
+
+def test_attention_refuses_gradients_in_the_first_states(dgc_lib):
+    """dq's walk reads the first states while dv's leaves dstate0."""
+    assert backward(dgc_lib, attention_shape(), state0=8 * P, d0=8 * P) == BAD
+    assert backward(dgc_lib, attention_shape(), state0=8 * P, dlast=8 * P, d0=8 * P) == BAD
