@@ -48,7 +48,9 @@ using Large = Tile<256, 256, 2, 4>;
 using Middle = Tile<128, 128, 2, 2>;
 using Small = Tile<64, 64, 2, 2>;
 // Of operands in three parts, of which LDS holds one workgroup's: with eight wavefronts, two to a SIMD, one multiplies while the
-// other reads.  700 x 10000 x 1500 in binary32, forward and backward: 615 us, with four wavefronts 656.
+// other reads.  700 x 10000 x 1500 in binary32, forward and backward: 615 us, with four wavefronts 656, with the large tile, whose
+// fragments are read half as often, where there is room for it 578.
+using Large3 = Tile<256, 128, 4, 2>;
 using Middle3 = Tile<128, 128, 2, 4>;
 
 // ---- scale of shares in 16 bits ----------------------------------------------------------------
@@ -416,28 +418,32 @@ int planes_of_shares(int32_t dtype) { return dtype == DGC_F16 ? 2 : parts_of(dty
 enum Shape { kLarge, kMiddle, kSmall };
 constexpr int64_t kTilesLeast = 200;
 
+// Sides of a tile; `parts` of the operands.
+constexpr int64_t side_m(Shape s) { return s == kLarge ? 256 : s == kMiddle ? 128 : 64; }
+constexpr int64_t side_n(int parts, Shape s) { return parts != 1 && s == kLarge ? 128 : side_m(s); }
+int64_t tiles_of(int parts, Shape s, int64_t m, int64_t n) { return (m + side_m(s) - 1) / side_m(s) * ((n + side_n(parts, s) - 1) / side_n(parts, s)); }
+
+// Large tiles of operands in three parts are taken for more than 512 rows only; below, too much of the last one is not there.
+// Large and middle, us, of all products of rows x 20000 x 1024: 300 rows 510 and 446, 512: 611 and 604, 640: 744 and 758, 896: 972
+// and 1014, 1408: 1446 and 1577.
+bool large_fit(int parts, int64_t m) { return parts == 1 || m > 512; }
+
 // The largest shape whose tiles are enough for most of the device's 256 compute units; small ones take four to a unit.  A tile
 // of 256 x 256 reads half as much for a product as four of 128 x 128: 4096 x 8192 x 2048 takes 116 to 133 us in large tiles
-// (dweight, shares), 4096 x 2048 x 8192, which has only 128 of them, 149 in middle ones (dhidden).  Of operands in three parts
-// LDS has no room for large ones.
+// (dweight, shares), 4096 x 2048 x 8192, which has only 128 of them, 149 in middle ones (dhidden).
 Shape shape_of(int parts, int64_t m, int64_t n) {
-  auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
-  return parts == 1 && tiles(256) >= kTilesLeast ? kLarge : tiles(128) >= kTilesLeast ? kMiddle : kSmall;
+  return large_fit(parts, m) && tiles_of(parts, kLarge, m, n) >= kTilesLeast ? kLarge : tiles_of(parts, kMiddle, m, n) >= kTilesLeast ? kMiddle : kSmall;
 }
-
-constexpr int64_t side_of(Shape s) { return s == kLarge ? 256 : s == kMiddle ? 128 : 64; }
 
 // Pairs of a row and a tile of columns that calls of up to `rows` rows leave statistics of, at most: fewer rows may go by smaller
 // tiles, and the most rows of either smaller kind are the other two candidates.  `columns`: that tiles are chosen by.
 int64_t pairs_of(int parts, int64_t rows, int64_t vocab, int64_t columns) {
   int64_t most = 0, r = rows;
   for (const Shape now : {kLarge, kMiddle, kSmall}) {
-    const int64_t tiles = (columns + side_of(now) - 1) / side_of(now);
-    const Shape s = shape_of(parts, r, columns);
-    if (s == now) {
-      most = std::max(most, r * ((vocab + side_of(s) - 1) / side_of(s)));
-      r = std::min(r, (kTilesLeast - 1) / tiles * side_of(now));
-    }
+    if (shape_of(parts, r, columns) != now) continue;
+    const int64_t side = side_n(parts, now);
+    most = std::max(most, r * ((vocab + side - 1) / side));
+    r = std::min(r, (kTilesLeast - 1) / ((columns + side - 1) / side) * side_m(now));
   }
   return most;
 }
@@ -465,7 +471,7 @@ struct Layout {
     weight = take((size_t)piece_packed * columns * 2 * p);
     if (backward) {
       shares = take((size_t)shares_elements * 2 * planes_of_shares(dtype));
-      total = take((size_t)std::min(kSplitMax * rows, std::max<int64_t>(4096, rows)) * up(width, 4) * 4);
+      total = take((size_t)std::min(kSplitMax * rows, std::max(split_rows(p), rows)) * up(width, 4) * 4);
     } else {
       pairs = std::max(pairs_of(p, rows, vocab, vocab), pairs_of(p, rows, vocab, std::min(piece_packed, vocab)));
       parts = take((size_t)pairs * 8);
@@ -473,23 +479,28 @@ struct Layout {
     }
     bytes = at;
   }
-  // Parts of the sums over a piece: more than one only where there are few rows, 4096 rows in all at most.
-  static int64_t splits_at_most(int64_t rows) { return rows == 0 ? 0 : std::max<int64_t>(1, std::min<int64_t>(kSplitMax, 4096 / rows)); }
+  // Parts of the sums over a piece: more than one only where there are few rows, 4096 rows in all at most, or, of operands in
+  // three parts, 8192 (700 x 10000 x 1500: 252 workgroups instead of 180, 546 us instead of 578).
+  static int64_t split_rows(int parts) { return parts == 1 ? 4096 : 8192; }
+  static int64_t splits_at_most(int parts, int64_t rows) {
+    return rows == 0 ? 0 : std::max<int64_t>(1, std::min<int64_t>(kSplitMax, split_rows(parts) / rows));
+  }
 };
 
 // The same for sums over the vocabulary, which can be split into parts: the largest shape whose tiles fill the device in
 // as many parts as there is room for.
 Shape dhidden_shape(int parts, int64_t rows, int64_t width) {
-  const int64_t splits = Layout::splits_at_most(rows);
-  auto groups = [&](int64_t side) { return ((rows + side - 1) / side) * ((width + side - 1) / side) * splits; };
-  return parts == 1 && rows > 128 && groups(256) >= 200 ? kLarge : rows > 64 && groups(128) >= (parts == 1 ? 300 : 200) ? kMiddle : kSmall;
+  const int64_t splits = Layout::splits_at_most(parts, rows);
+  if (rows > 128 && large_fit(parts, rows) && tiles_of(parts, kLarge, rows, width) * splits >= kTilesLeast) return kLarge;
+  return rows > 64 && tiles_of(parts, kMiddle, rows, width) * splits >= (parts == 1 ? 300 : kTilesLeast) ? kMiddle : kSmall;
 }
 
-template <int PARTS, typename F>
+// ROOM: whether the kernel leaves LDS to a large tile of operands in three parts.
+template <int PARTS, bool ROOM, typename F>
 void with_shape(Shape s, F f) {
-  if constexpr (PARTS == 1)
-    if (s == kLarge) return f(Large{});
-  if (s == kMiddle) f(std::conditional_t<PARTS == 1, Middle, Middle3>{});
+  using L = std::conditional_t<PARTS == 1, Large, std::conditional_t<ROOM, Large3, Middle3>>;
+  if (s == kLarge) f(L{});
+  else if (s == kMiddle) f(std::conditional_t<PARTS == 1, Middle, Middle3>{});
   else f(Small{});
 }
 
@@ -534,7 +545,7 @@ struct Run {
                                                              : pack(v.hidden, v.hidden_stride, 0, v.rows, false, at.hidden);
     const int64_t at_once = direct(v.weight, v.weight_stride) ? v.vocab : at.piece_packed;
     int tiles = 0;
-    with_shape<kParts>(shape_of(kParts, v.rows, std::min<int64_t>(at_once, v.vocab)), [&](auto shape) {
+    with_shape<kParts, true>(shape_of(kParts, v.rows, std::min<int64_t>(at_once, v.vocab)), [&](auto shape) {
       using S = decltype(shape);
       tiles = (v.vocab + S::kN - 1) / S::kN;
       if ((int64_t)tiles * v.rows > at.pairs) return;  // never: the layout counts them the same way
@@ -571,24 +582,24 @@ struct Run {
       // whole tiles of shares were written, so that a sum over them may run to the next step's end
       const auto whole_tiles = [&](const E* x) { return Operand{reinterpret_cast<const char*>(x), piece * 2, plane * 2, (int32_t)rows_pad, (int32_t)piece * 2}; };
       if (v.rows > 0)
-        with_shape<kParts>(shape_of(kParts, v.rows, columns), [&](auto shape) {
+        with_shape<kParts, false>(shape_of(kParts, v.rows, columns), [&](auto shape) {
           using S = decltype(shape);
           shares_kernel<T, S><<<tiles_of(shape, v.rows, columns), S::kThreads, 0, stream>>>(v, hidden, w, v.width, first, columns, largest, plain, weighted, piece, plane);
         });
       if (v.rows > 0 && v.dhidden)
-        with_shape<kParts>(dhidden_shape(kParts, v.rows, v.width), [&](auto shape) {
+        with_shape<kParts, true>(dhidden_shape(kParts, v.rows, v.width), [&](auto shape) {
           using S = decltype(shape);
           const uint32_t tiles = tiles_of(shape, v.rows, v.width);
           const int depth = (int)up(columns, kDepth);
           // as many parts of the sum as the device takes workgroups, of 512 terms at least
           constexpr int kResident = S::kM == 256 ? 256 : S::kM == 128 ? (kParts == 1 ? 512 : 256) : kParts == 1 ? 1024 : 768;
-          if (first == 0) parts = (int)std::max<int64_t>(1, std::min<int64_t>({Layout::splits_at_most(v.rows), (int64_t)(kResident / tiles), (int64_t)(depth / 512)}));
+          if (first == 0) parts = (int)std::max<int64_t>(1, std::min<int64_t>({Layout::splits_at_most(kParts, v.rows), (int64_t)(kResident / tiles), (int64_t)(depth / 512)}));
           const int part = (int)up((depth + parts - 1) / parts, kDepth);
           if (first == 0) parts = (depth + part - 1) / part;  // none that begins behind the end; a last piece may have some
           dhidden_kernel<T, S><<<dim3(tiles, parts), S::kThreads, 0, stream>>>(v, whole_tiles(shares), w, depth, part, first > 0, total);
         });
       if (v.dweight)
-        with_shape<kParts>(shape_of(kParts, columns, v.width), [&](auto shape) {
+        with_shape<kParts, true>(shape_of(kParts, columns, v.width), [&](auto shape) {
           using S = decltype(shape);
           dweight_kernel<T, S><<<tiles_of(shape, columns, v.width), S::kThreads, 0, stream>>>(v, whole_tiles(for_dweight), hidden, first, columns, largest);
         });
