@@ -370,9 +370,9 @@ struct Slots {
 // Of a chunk every wavefront forms a b^T for itself, as 32 x 32 shares whose layout is that of the operand they are next, and
 // so is the state's: neither goes through LDS.  While a chunk is worked on the next one's rows are on their way to registers.
 //
-// Bound by memory and by issue alike: 65536 steps of 16 heads of 128 x 128 in bfloat16, forward and backward, read 18 and write
-// 4 arrays of 268 MB in 1590 us; without loads 1340, without stores 1410, with neither product 1170 to 1280.  By the profiler's
-// counters vector instructions take 60 % of the cycles and products 39 %.
+// Bound by memory and by issue alike: 65536 steps of 16 heads of 128 x 128 in bfloat16, forward and backward, ask for 18 and write
+// 4 arrays of 268 MB (4.5 GB come from memory) in 1560 to 1620 us; without loads 1340, without stores 1410, with neither product
+// 1170 to 1280.  By the profiler's counters vector instructions take 60 % of the cycles and products 43 %.
 template <typename T, int DA, int WAVES, bool OUT, bool NARROW>
 __global__ __launch_bounds__(64 * WAVES, DA <= 128 && sizeof(T) == 2 ? 2 : 1) void walk_chunks_kernel(const Walks walks, const Slots slots) {
   int which;

@@ -1,7 +1,7 @@
 // Rotary positions: the pairs of every head turned by their row's position times the pair's frequency.
 //
-// Bound by memory: every element is read and written once.  65536 rows of 32 heads of 128 in bfloat16, 1074 MB, take 264 us,
-// 4.1 TB/s; with a thread to a pair, which forms its angle for every head, they took 552.
+// Bound by memory: every element is read and written once.  65536 rows of 32 heads of 128 in bfloat16, 1074 MB, take 252 to 264
+// us, 4.1 to 4.3 TB/s; with a thread to a pair, which forms its angle for every head, they took 552.
 
 #include <algorithm>
 

@@ -8,10 +8,10 @@
 // shared (by an array, by rows), some sum runs over rows of different ones: a row of 1e20 that counts nothing made zeros of
 // its neighbours.
 //
-// Bound by the matrix units: 4096 rows, width 2048, vocabulary 131072 in bfloat16, forward and backward, are 8.8 TFLOP in 7.51 ms,
-// 1171 TFLOP/s (a library's product of that shape reaches 1293): statistics 1.99 ms, shares 2.12, dhidden 2.38, dweight 1.86 by
-// the profiler.  The logits are formed twice because dweight needs the log-sum-exp: 8 units of rows * vocab * width where 6
-// would do if logits were kept.
+// Bound by the matrix units: 4096 rows, width 2048, vocabulary 131072 in bfloat16, forward and backward, are 8.8 TFLOP in 7.55 to
+// 7.81 ms, 1130 to 1165 TFLOP/s (a library's product of that shape reaches 1293).  Under the profiler, where all takes 7.8: statistics
+// 1.85 ms, shares 1.99, dhidden 2.20, dweight 1.70.  The logits are formed twice because dweight needs the log-sum-exp: 8 units of
+// rows * vocab * width where 6 would do if logits were kept.
 
 #include <type_traits>
 
