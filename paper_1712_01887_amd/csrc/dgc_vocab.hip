@@ -59,7 +59,9 @@ using Middle3 = Tile<128, 128, 2, 4>;
 // of nearly -1, hardly at all.  20 x 10000 x 1500 in bfloat16: 1.67e-3 of dhidden's norm away from 64 bits, without the scaling 1.95e-3;
 // 104 rows, 119301 x 48 in binary16: 2.1e-4 of dweight's, with a power of two 3.1e-4.  binary16 holds 2^-38 of the largest: rows
 // that weigh less are lost in dweight, where the others' terms are that much larger, but not in their own row of dhidden: that is
-// formed from P_rj 2^14, and w_r comes in at the end.  bfloat16 holds all weights, and takes the one matrix for both.
+// formed from P_rj 2^14, and w_r comes in at the end.  bfloat16 holds all weights, and takes the one matrix for both.  A second part
+// of the shares would be half as much again of all products; it would change vocabularies of some hundreds, whose shares are neither
+// nearly 0 nor nearly -1: 30 x 68 x 107 in bfloat16 is 2.1e-3 from 64 bits, what the rounding of the results alone leaves 1.7e-3.
 //
 // `largest`: the bits of the largest absolute row weight.
 __device__ __forceinline__ int exponent_of(uint32_t largest) {

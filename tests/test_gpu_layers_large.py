@@ -85,7 +85,7 @@ def test_rotary_of_very_many_rows(rows, dim, heads, dtype, gib):
 def test_vocabulary_loss_of_very_many_logits():
     """2^39 logits: a thread for each 128 of them in the largest tiles, 2^32."""
     import torch
-    room(80)
+    room(40)
     rows, vocab, width, t = (1 << 24) - 1, 1 << 15, 2, torch.bfloat16
     say(f"[vocabulary loss] {rows} x {vocab} x {width} bf16, the loss alone")
     gen = torch.Generator(device="cuda").manual_seed(2)

@@ -176,3 +176,37 @@ def test_equal_weights_round_the_shares_themselves(dtype):
         unit = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8}[dtype]
         tiny = 2.0 ** -25 * 1.05 if dtype == "f16" else 0.0
         assert np.all(np.abs(a - b) <= (2 * unit + unit ** 2 + 2.0 ** -21) * np.abs(a) + 2 * tiny), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_no_rows_leave_zeros(dtype):
+    """No rows: dweight is zero, whatever the workspace holds."""
+    import torch
+    t = dtype_of(dtype)
+    plan = B.VocabularyLoss(9, 70, 24, t)
+    plan.workspace.fill_(255)                                          # NaN in every type
+    h, m = torch.empty(0, 24, dtype=t, device="cuda"), torch.ones(70, 24, dtype=t, device="cuda")
+    y, none = torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty(0, device="cuda")
+    dm = torch.full_like(m, 5.0)
+    plan.dgc_vocab_loss_backward(h, m, y, none, torch.empty_like(h), dm, row_weight=none)
+    assert bool((dm == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,vocab,width", [(1, 29, 8), (90, 300, 65), (640, 9000, 130)])
+def test_workspaces_that_hold_anything(rows, vocab, width, dtype):
+    """Nothing is read from the workspace that the call has not written: the same bits after it was filled with NaN."""
+    import torch
+    t, gen = dtype_of(dtype), torch.Generator(device="cuda").manual_seed(3)
+    h, m = torch.randn(rows, width, generator=gen, device="cuda").to(t), torch.randn(vocab, width, generator=gen, device="cuda").to(t)
+    y = torch.randint(-1, vocab, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    w = torch.rand(rows, generator=gen, device="cuda")
+    plan, seen = B.VocabularyLoss(rows, vocab, width, t), []
+    for fill in (0, 255):
+        plan.workspace.fill_(fill)
+        loss, lse, dh, dm = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(h), torch.empty_like(m)
+        plan.dgc_vocab_loss_forward(h, m, y, loss, lse, row_weight=w)
+        plan.workspace.fill_(fill)
+        plan.dgc_vocab_loss_backward(h, m, y, lse, dh, dm, row_weight=w)
+        seen.append((loss, lse, dh, dm))
+    assert all(torch.equal(a, b) for a, b in zip(*seen)) and all(bool(torch.isfinite(a).all()) for a in seen[1])
